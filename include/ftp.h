@@ -67,7 +67,8 @@ typedef enum {
   FTP_UNIT_LOSS = 4    /* softmax cross-entropy, mean over the batch             */
 } ftp_unit_kind;
 
-typedef enum { FTP_ACT_NONE = 0, FTP_ACT_RELU = 1, FTP_ACT_RELU6 = 2 } ftp_act;
+/* Units take the first three; the token operators below take all (GELU in its tanh form). */
+typedef enum { FTP_ACT_NONE = 0, FTP_ACT_RELU = 1, FTP_ACT_RELU6 = 2, FTP_ACT_SILU = 3, FTP_ACT_GELU = 4 } ftp_act;
 
 typedef struct {
   int32_t kind;          /* ftp_unit_kind                                        */
@@ -311,6 +312,124 @@ int ftp_renumber_workers(const int32_t* worker_ids, int n, const int32_t* failed
  * device to device on `stream`, and refreshes dst's bfloat16 working copy of
  * them.  Pending gradients are not copied. */
 int ftp_stage_copy_units(ftp_stage* dst, const ftp_stage* src, int unit_lo, int unit_hi, void* stream);
+
+/* ---- token operators --------------------------------------------------------------- */
+
+/* What a stage of a token model is made of, on buffers the caller owns: the table lookup of the first stage, linear
+ * layers, gated feed-forward blocks, and the 8-bit form in which a stage can hold the activations of its batches in
+ * flight (section "Async Pipeline Training": stage i of n keeps n-i of them).  A call takes a record of sizes, pointers
+ * and options (zero it first: a NULL pointer or 0 is "not wanted"); the caller keeps it for as long as its buffers live.
+ *   - Matrices are row-major; ld... is the distance between rows in elements (bytes for 8-bit forms), at least the
+ *     row's length, at most 2^20.  Pointers are aligned to their elements; sizes, strides and offsets are otherwise
+ *     free, but an operand whose rows do not start and end on 16 bytes is first copied into the workspace.
+ *   - `rows` counts tokens, 0 .. 2^30; with 0 a forward does nothing and a backward writes zero gradients
+ *     (accumulate: leaves them).
+ *   - `dtype` is the type of activations, their gradients and the weights.  Sums, activations and scales are fp32;
+ *     what is stored between two products (hidden, its gradients) is rounded to dtype once, as their operands.
+ *   - Weight gradients are [out][in] one row behind the other, fp32 or of dtype (grad_dtype), overwritten, or with
+ *     `accumulate` (fp32 only) added to.
+ *   - ws: device memory of at least the bytes the ..._workspace function names for the same record and direction (it
+ *     goes by sizes, strides and the pointers' alignment), on 16 bytes; contents are free between calls; calls that may
+ *     overlap need one each.  Nothing is allocated, everything is enqueued on `stream`, calls can be captured into a
+ *     graph.  Results do not depend on what else runs: the same inputs give the same bits.
+ *   - Outputs may not overlap inputs, except that y may be the residual's buffer. */
+
+/* out[t] = scale * table[ids[t]]; an id that is none of 0 .. vocab-1 gives a row of NaN.
+ * Gradient: dtable[v] = scale * (sum of dy[t] over the tokens t with ids[t] = v), fp32, all vocab rows written, or with
+ * `accumulate` added to the rows that came up.  Tokens whose id is pad_id (-1: none) or not the table's add nothing.
+ * Sorted by id, each id's tokens added in their order. */
+typedef struct {
+  int64_t rows;
+  int32_t vocab, width;
+  int32_t dtype;          /* ftp_dtype of table, out, dy                            */
+  int32_t ids64;          /* ids are int64 (otherwise int32)                        */
+  int32_t accumulate;
+  float scale;            /* finite                                                 */
+  int64_t pad_id;
+  const void* ids;
+  const void* table; int64_t ldt;
+  void* out; int64_t ldo;
+  const void* dy; int64_t lddy;
+  float* dtable; int64_t lddt;
+  void* ws; size_t ws_bytes;
+} ftp_embed_args;
+int ftp_embed_forward(const ftp_embed_args*, void* stream);
+int ftp_embed_backward_workspace(const ftp_embed_args*, size_t* bytes);
+int ftp_embed_backward(const ftp_embed_args*, void* stream);
+
+/* Forward: y = act(z) + residual, z = x w^T + bias; x [rows][n_in], w [n_out][n_in], bias fp32 [n_out] or NULL, residual
+ * or NULL; z is written where it is wanted (the backward of an activation needs it).
+ * Backward: dz = dy * act'(z); dx = dz w, dw = dz^T x, dbias = sum of dz over the rows; each where wanted.  Derivatives of
+ * ReLU and ReLU6 are 1 strictly inside.  (dy is also the residual's gradient.)
+ * x_scales: x is held in 8 bits (ftp_act8_pack), its scales ldxs apart. */
+typedef struct {
+  int64_t rows;
+  int32_t n_in, n_out;
+  int32_t dtype, act;
+  int32_t grad_dtype, accumulate;
+  const void* x; int64_t ldx;
+  const uint8_t* x_scales; int64_t ldxs;
+  const void* w; int64_t ldw;
+  const float* bias;
+  const void* residual; int64_t ldr;
+  void* y; int64_t ldy;
+  void* z; int64_t ldz;
+  const void* dy; int64_t lddy;
+  void* dx; int64_t lddx;
+  void* dw;
+  void* dbias;
+  void* ws; size_t ws_bytes;
+} ftp_linear_args;
+int ftp_linear_workspace(const ftp_linear_args*, int backward, size_t* bytes);
+int ftp_linear_forward(const ftp_linear_args*, void* stream);
+int ftp_linear_backward(const ftp_linear_args*, void* stream);
+
+/* Gated feed-forward block: gate = x w_gate^T, up = x w_up^T, hidden = act(gate) * up, y = hidden w_down^T + residual;
+ * w_gate, w_up [hidden][width], w_down [width][hidden].  The hidden rows are the workspace's.
+ * save: FTP_SAVE_FULL keeps gate and up in dtype, [rows][hidden]; FTP_SAVE_ACT8 in 8 bits with gate_scales, up_scales
+ * [rows][ceil(hidden / 32)], formed from the fp32 sums: 33/64 of the bytes a bfloat16 stash takes.
+ * Backward, from what was kept: dhidden = dy w_down; dgate = dhidden * up * act'(gate); dup = dhidden * act(gate);
+ * dx = dgate w_gate + dup w_up (+ dy with dx_residual: the block's residual was x); dw_gate = dgate^T x, dw_up = dup^T x,
+ * dw_down = dy^T hidden, the three together or none.  x_scales as above. */
+typedef enum { FTP_SAVE_NONE = 0, FTP_SAVE_FULL = 1, FTP_SAVE_ACT8 = 2 } ftp_save;
+typedef struct {
+  int64_t rows;
+  int32_t width, hidden;
+  int32_t dtype, act;
+  int32_t save;           /* ftp_save                                               */
+  int32_t grad_dtype, accumulate, dx_residual;
+  const void* x; int64_t ldx;
+  const uint8_t* x_scales; int64_t ldxs;
+  const void* w_gate; int64_t ldwg;
+  const void* w_up; int64_t ldwu;
+  const void* w_down; int64_t ldwd;
+  const void* residual; int64_t ldr;
+  void* y; int64_t ldy;
+  void *gate, *up;
+  uint8_t *gate_scales, *up_scales;
+  const void* dy; int64_t lddy;
+  void* dx; int64_t lddx;
+  void *dw_gate, *dw_up, *dw_down;
+  void* ws; size_t ws_bytes;
+} ftp_ffn_args;
+int ftp_ffn_workspace(const ftp_ffn_args*, int backward, size_t* bytes);
+int ftp_ffn_forward(const ftp_ffn_args*, void* stream);
+int ftp_ffn_backward(const ftp_ffn_args*, void* stream);
+
+/* Activations in 8 bits: groups of 32 columns share a scale 2^(s-127), the smallest (s >= 0) with which the group's
+ * largest finite magnitude is at most 448; q holds value / scale as e4m3 (4 exponent bits, 3 mantissa bits, no infinity),
+ * to nearest even.  Infinities and NaN become NaN.  q [rows][ldq], scales [rows][lds], lds >= ceil(cols / 32).
+ * pack: x -> q, scales.  unpack: q, scales -> y. */
+typedef struct {
+  int64_t rows;
+  int32_t cols, dtype;
+  const void* x; int64_t ldx;
+  uint8_t* q; int64_t ldq;
+  uint8_t* scales; int64_t lds;
+  void* y; int64_t ldy;
+} ftp_act8_args;
+int ftp_act8_pack(const ftp_act8_args*, void* stream);
+int ftp_act8_unpack(const ftp_act8_args*, void* stream);
 
 /* ---- diagnostics ---------------------------------------------------------------- */
 

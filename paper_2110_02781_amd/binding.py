@@ -16,7 +16,8 @@ _LIB_PATH = os.path.join(_HERE, "libftp_hip.so")
 
 F32, BF16 = 0, 1
 UNIT_CONV, UNIT_INVRES, UNIT_GAP, UNIT_FC, UNIT_LOSS = range(5)
-ACT_NONE, ACT_RELU, ACT_RELU6 = range(3)
+ACT_NONE, ACT_RELU, ACT_RELU6, ACT_SILU, ACT_GELU = range(5)
+SAVE_NONE, SAVE_FULL, SAVE_ACT8 = range(3)
 
 
 class FtpError(RuntimeError):
@@ -37,6 +38,25 @@ class KtraceRow(C.Structure):
 
 class Sgd(C.Structure):
     _fields_ = [("lr", C.c_float), ("momentum", C.c_float), ("weight_decay", C.c_float)]
+
+
+def _record(name, doc, *fields):
+    kinds = {"i": C.c_int32, "l": C.c_int64, "f": C.c_float, "p": C.c_void_p, "z": C.c_size_t}
+    return type(name, (C.Structure,), {"__doc__": doc, "_fields_": [(n, kinds[k]) for k, names in fields for n in names.split()]})
+
+
+EmbedArgs = _record("EmbedArgs", "ftp_embed_args", ("l", "rows"), ("i", "vocab width dtype ids64 accumulate"), ("f", "scale"), ("l", "pad_id"),
+                    ("p", "ids table"), ("l", "ldt"), ("p", "out"), ("l", "ldo"), ("p", "dy"), ("l", "lddy"), ("p", "dtable"), ("l", "lddt"),
+                    ("p", "ws"), ("z", "ws_bytes"))
+LinearArgs = _record("LinearArgs", "ftp_linear_args", ("l", "rows"), ("i", "n_in n_out dtype act grad_dtype accumulate"), ("p", "x"), ("l", "ldx"),
+                     ("p", "x_scales"), ("l", "ldxs"), ("p", "w"), ("l", "ldw"), ("p", "bias residual"), ("l", "ldr"), ("p", "y"), ("l", "ldy"),
+                     ("p", "z"), ("l", "ldz"), ("p", "dy"), ("l", "lddy"), ("p", "dx"), ("l", "lddx"), ("p", "dw dbias ws"), ("z", "ws_bytes"))
+FfnArgs = _record("FfnArgs", "ftp_ffn_args", ("l", "rows"), ("i", "width hidden dtype act save grad_dtype accumulate dx_residual"), ("p", "x"),
+                  ("l", "ldx"), ("p", "x_scales"), ("l", "ldxs"), ("p", "w_gate"), ("l", "ldwg"), ("p", "w_up"), ("l", "ldwu"), ("p", "w_down"),
+                  ("l", "ldwd"), ("p", "residual"), ("l", "ldr"), ("p", "y"), ("l", "ldy"), ("p", "gate up gate_scales up_scales dy"),
+                  ("l", "lddy"), ("p", "dx"), ("l", "lddx"), ("p", "dw_gate dw_up dw_down ws"), ("z", "ws_bytes"))
+Act8Args = _record("Act8Args", "ftp_act8_args", ("l", "rows"), ("i", "cols dtype"), ("p", "x"), ("l", "ldx"), ("p", "q"), ("l", "ldq"),
+                   ("p", "scales"), ("l", "lds"), ("p", "y"), ("l", "ldy"))
 
 
 def _load():
@@ -97,6 +117,17 @@ _SIGS = {
     "ftp_stage_timing_read": (_i, [_vp, _dp, C.POINTER(C.c_int)]),
     "ftp_calibration_copy": (_i, [_vp, _vp, _sz, _vp]),
     "ftp_diag_fail_next_launch_plan": (_i, []),
+    "ftp_embed_forward": (_i, [C.POINTER(EmbedArgs), _vp]),
+    "ftp_embed_backward_workspace": (_i, [C.POINTER(EmbedArgs), C.POINTER(_sz)]),
+    "ftp_embed_backward": (_i, [C.POINTER(EmbedArgs), _vp]),
+    "ftp_linear_workspace": (_i, [C.POINTER(LinearArgs), _i, C.POINTER(_sz)]),
+    "ftp_linear_forward": (_i, [C.POINTER(LinearArgs), _vp]),
+    "ftp_linear_backward": (_i, [C.POINTER(LinearArgs), _vp]),
+    "ftp_ffn_workspace": (_i, [C.POINTER(FfnArgs), _i, C.POINTER(_sz)]),
+    "ftp_ffn_forward": (_i, [C.POINTER(FfnArgs), _vp]),
+    "ftp_ffn_backward": (_i, [C.POINTER(FfnArgs), _vp]),
+    "ftp_act8_pack": (_i, [C.POINTER(Act8Args), _vp]),
+    "ftp_act8_unpack": (_i, [C.POINTER(Act8Args), _vp]),
     "ftp_ktrace_begin": (_i, [_i]),
     "ftp_ktrace_end": (_i, [C.POINTER(KtraceRow), _i, C.POINTER(_i)]),
 }
@@ -300,6 +331,83 @@ def estimate_capacity(stage_time, layer_costs, start, end):
     out = C.c_double()
     _chk(lib.ftp_estimate_capacity(stage_time, cp, c.size, start, end, C.byref(out)))
     return out.value
+
+
+# ---- token operators ---------------------------------------------------------------
+# The ..._args functions fill a record from keywords (tensors stand for their addresses; what is left out is zero, i.e. not
+# wanted; the caller keeps the tensors alive).  Fields can be set later: a.ws, a.ws_bytes = ws.data_ptr(), ws.numel().
+def _fill(record, kw):
+    for k, v in kw.items():
+        if not hasattr(record, k):
+            raise TypeError(f"{type(record).__name__} has no field {k}")
+        setattr(record, k, v.data_ptr() if hasattr(v, "data_ptr") else v)
+    return record
+
+
+def embed_args(**kw):
+    return _fill(EmbedArgs(pad_id=-1, scale=1.0), kw)
+
+
+def embed_forward(args, stream=None):
+    _chk(lib.ftp_embed_forward(C.byref(args), stream))
+
+
+def embed_backward_workspace(args):
+    n = _sz(0)
+    _chk(lib.ftp_embed_backward_workspace(C.byref(args), C.byref(n)))
+    return n.value
+
+
+def embed_backward(args, stream=None):
+    _chk(lib.ftp_embed_backward(C.byref(args), stream))
+
+
+def linear_args(**kw):
+    return _fill(LinearArgs(), kw)
+
+
+def linear_workspace(args, backward=False):
+    n = _sz(0)
+    _chk(lib.ftp_linear_workspace(C.byref(args), 1 if backward else 0, C.byref(n)))
+    return n.value
+
+
+def linear_forward(args, stream=None):
+    _chk(lib.ftp_linear_forward(C.byref(args), stream))
+
+
+def linear_backward(args, stream=None):
+    _chk(lib.ftp_linear_backward(C.byref(args), stream))
+
+
+def ffn_args(**kw):
+    return _fill(FfnArgs(), kw)
+
+
+def ffn_workspace(args, backward=False):
+    n = _sz(0)
+    _chk(lib.ftp_ffn_workspace(C.byref(args), 1 if backward else 0, C.byref(n)))
+    return n.value
+
+
+def ffn_forward(args, stream=None):
+    _chk(lib.ftp_ffn_forward(C.byref(args), stream))
+
+
+def ffn_backward(args, stream=None):
+    _chk(lib.ftp_ffn_backward(C.byref(args), stream))
+
+
+def act8_args(**kw):
+    return _fill(Act8Args(), kw)
+
+
+def act8_pack(args, stream=None):
+    _chk(lib.ftp_act8_pack(C.byref(args), stream))
+
+
+def act8_unpack(args, stream=None):
+    _chk(lib.ftp_act8_unpack(C.byref(args), stream))
 
 
 # ---- diagnostics ---------------------------------------------------------------------

@@ -20,6 +20,9 @@ SOURCES = [
     ("k_gemm.hip", ["-x", "hip"]),
     ("k_fused.hip", ["-x", "hip"]),
     ("k_gemm_deep.hip", ["-x", "hip"]),
+    ("k_token_gemm.hip", ["-x", "hip"]),
+    ("k_token.hip", ["-x", "hip"]),
+    ("token.cpp", ["-x", "hip"]),
     ("stage.cpp", ["-x", "hip"]),
     ("ktrace.cpp", ["-x", "hip"]),
     ("solver.cpp", ["-x", "c++", "-ffp-contract=off"]),

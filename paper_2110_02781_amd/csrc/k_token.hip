@@ -1,0 +1,547 @@
+// Memory-bound token kernels: table lookup and its gradient by sorted tokens, the 8-bit form of activations, the gradient behind a
+// linear layer's activation, rows copied into the alignment that the matrix products need.
+// Rows may start at any element: vectors of 16 bytes are accessed at the element's alignment (global memory takes them unaligned).
+#include <algorithm>
+
+#include "token_dev.h"
+
+namespace ftp {
+
+// 16 or 8 bytes at any element-aligned address as one access
+typedef uint32_t u4v_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u2v_t __attribute__((ext_vector_type(2)));
+template <int A> struct TkAt;
+template <> struct TkAt<1> { typedef u2v_t v8 __attribute__((aligned(1))); };
+template <> struct TkAt<2> { typedef u4v_t v16 __attribute__((aligned(2))); };
+template <> struct TkAt<4> { typedef u4v_t v16 __attribute__((aligned(4))); };
+template <typename E> __device__ __forceinline__ u4v_t tk_ld16(const E* p) { return *reinterpret_cast<const typename TkAt<sizeof(E)>::v16*>(p); }
+template <typename E> __device__ __forceinline__ void tk_st16(E* p, u4v_t v) { *reinterpret_cast<typename TkAt<sizeof(E)>::v16*>(p) = v; }
+
+template <typename E>
+__device__ __forceinline__ void tk_load8(const E* p, int left, float v[8]) {     // left: elements that are there
+  if (left >= 8) {
+    const u4v_t a = tk_ld16<E>(p);
+    if constexpr (sizeof(E) == 2) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(a[i] << 16);
+        v[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
+      }
+    } else {
+      const u4v_t b = tk_ld16<E>(p + 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { v[i] = __uint_as_float(a[i]); v[i + 4] = __uint_as_float(b[i]); }
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < left ? to_f32(p[e]) : 0.f;
+  }
+}
+template <typename E>
+__device__ __forceinline__ void tk_store8(E* p, int left, const float v[8]) {
+  if (left >= 8) {
+    if constexpr (sizeof(E) == 2) {
+      tk_st16<E>(p, u4v_t{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4], v[5]), f32x2_to_bf16x2(v[6], v[7])});
+    } else {
+      tk_st16<E>(p, u4v_t{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
+      tk_st16<E>(p + 4, u4v_t{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])});
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < left) p[e] = from_f32<E>(v[e]);
+  }
+}
+
+// Calls go out in slices of rows whose vectors are numbered below 2^30, so that the division into row and place is a 32-bit one.
+template <typename F>
+static void by_rows(int64_t rows, int64_t per_row, F f) {
+  const int64_t step = std::max<int64_t>(1, ((int64_t)1 << 30) / std::max<int64_t>(per_row, 1));
+  for (int64_t r = 0; r < rows; r += step) f(r, (int)std::min(step, rows - r));
+}
+static inline unsigned blocks_of(int64_t n, int most) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>((n + 255) / 256, most)); }
+
+// ---------------------------------------------------------------- table lookup
+// out[t] = scale * table[id], 8 columns a thread; a row of NaN where the id is none of the table's
+template <typename E, typename I>
+__global__ __launch_bounds__(256) void embed_fwd_k(const I* __restrict__ ids, int64_t t0, int rows, int vocab, int width, float scale,
+                                                   const E* __restrict__ table, int64_t ldt, E* __restrict__ out, int64_t ldo) {
+  const uint32_t per = (width + 7) / 8, all = (uint32_t)rows * per;
+  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += gridDim.x * 256) {
+    const uint32_t r = i / per, c = (i - r * per) * 8;
+    const int64_t t = t0 + r;
+    const int64_t id = (int64_t)ids[t];
+    float v[8];
+    if (id >= 0 && id < vocab) {
+      tk_load8<E>(table + id * ldt + c, width - (int)c, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] *= scale;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(0x7fc00000u);
+    }
+    tk_store8<E>(out + t * ldo + c, width - (int)c, v);
+  }
+}
+
+void tk_embed(int dt, hipStream_t st, const void* ids, int ids64, int64_t n, int vocab, int width, float scale, const void* table,
+              int64_t ldt, void* out, int64_t ldo) {
+  const int es = dt == 1 ? 2 : 4;
+  KScope ks(st, "tok_embed", 2.0 * n * width * es + 4.0 * n, (double)n * width, n, vocab, width);
+  by_rows(n, (width + 7) / 8, [&](int64_t t0, int rows) {
+    const unsigned b = blocks_of((int64_t)rows * ((width + 7) / 8), 1 << 20);
+    auto go = [&](auto k, auto* id, auto* tab, auto* o) {
+      hipLaunchKernelGGL(k, dim3(b), dim3(256), 0, st, id, t0, rows, vocab, width, scale, tab, ldt, o, ldo);
+    };
+    if (dt == 1 && ids64) go(embed_fwd_k<bf16_t, int64_t>, (const int64_t*)ids, (const bf16_t*)table, (bf16_t*)out);
+    else if (dt == 1) go(embed_fwd_k<bf16_t, int32_t>, (const int32_t*)ids, (const bf16_t*)table, (bf16_t*)out);
+    else if (ids64) go(embed_fwd_k<float, int64_t>, (const int64_t*)ids, (const float*)table, (float*)out);
+    else go(embed_fwd_k<float, int32_t>, (const int32_t*)ids, (const float*)table, (float*)out);
+  });
+}
+
+// ---------------------------------------------------------------- its gradient
+// Tokens are sorted by id, equal ids in the order of the tokens; then every kRun of them are one block's: it walks them with a running
+// sum per column and writes a row of the gradient where the id changes.  What an id has in other runs as well goes to memory as partial
+// sums, which embed_join_k adds in the order of the runs.  No atomics: the same tokens give the same bits.
+enum { kRun = 64, kRankMost = 16384, kTile = 4096, kDigit = 8 };
+#define FTP_NO_ID 0xffffffffu
+
+template <typename I>
+__global__ __launch_bounds__(256) void embed_keys_k(const I* __restrict__ ids, int n, int vocab, int64_t pad_id, uint32_t* __restrict__ keys,
+                                                    uint32_t* __restrict__ pos) {
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
+    const int64_t id = (int64_t)ids[i];
+    keys[i] = id >= 0 && id < vocab && id != pad_id ? (uint32_t)id : FTP_NO_ID;
+    if (pos) pos[i] = (uint32_t)i;
+  }
+}
+// Few tokens: a token's place is how many come before it, counted outright: n^2 comparisons, two instructions for 64 of them, no passes
+// that wait for one another.  A block places 64 tokens, its wavefronts share the ones compared with.
+__global__ __launch_bounds__(256) void embed_rank_k(const uint32_t* __restrict__ keys, int n, uint32_t* __restrict__ skeys,
+                                                    uint32_t* __restrict__ spos) {
+  __shared__ uint32_t cnt[4][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int first = blockIdx.x * 64, i = first + lane;
+  const uint32_t k = i < n ? keys[i] : 0;
+  uint32_t c = 0;
+  // tokens in front of this block's count where their id is not larger, those behind it where it is smaller
+  const int per = ((n + 3) / 4 + 15) & ~15, j0 = wave * per, j1 = j0 + per < n ? j0 + per : n;
+  const int a1 = j1 < first ? j1 : first;
+  int j = j0;
+  for (; j + 16 <= a1; j += 16) {
+#pragma unroll
+    for (int u = 0; u < 16; ++u) c += keys[j + u] <= k;
+  }
+  for (; j < a1; ++j) c += keys[j] <= k;
+  for (; j < j1 && j < first + 64; ++j) c += (keys[j] < k) || (keys[j] == k && j < i);
+  for (; j < j1 && (j & 15); ++j) c += keys[j] < k;
+  for (; j + 16 <= j1; j += 16) {
+#pragma unroll
+    for (int u = 0; u < 16; ++u) c += keys[j + u] < k;
+  }
+  for (; j < j1; ++j) c += keys[j] < k;
+  cnt[wave][lane] = c;
+  __syncthreads();
+  if (wave == 0 && i < n) {
+    const uint32_t at = cnt[0][lane] + cnt[1][lane] + cnt[2][lane] + cnt[3][lane];
+    skeys[at] = k;
+    spos[at] = (uint32_t)i;
+  }
+}
+// Many tokens: 8 bits of the id at a time, from the lowest.  A block has kTile tokens; counts per block and digit, their running sum over
+// (digit, block), then every token goes to its digit's place in its order.
+__global__ __launch_bounds__(256) void embed_count_k(const uint32_t* __restrict__ keys, int n, int shift, uint32_t* __restrict__ hist, int blocks) {
+  __shared__ uint32_t h[256];
+  h[threadIdx.x] = 0;
+  __syncthreads();
+  for (int u = 0; u < kTile / 256; ++u) {
+    const int i = blockIdx.x * kTile + u * 256 + threadIdx.x;
+    if (i < n) atomicAdd(&h[(keys[i] >> shift) & 255], 1u);      // counts: their order does not matter
+  }
+  __syncthreads();
+  hist[threadIdx.x * blocks + blockIdx.x] = h[threadIdx.x];
+}
+__global__ __launch_bounds__(1024) void embed_scan_k(uint32_t* __restrict__ hist, int m) {       // exclusive running sum, one block
+  __shared__ uint32_t part[1024];
+  const int per = (m + 1023) / 1024, a = threadIdx.x * per, b = a + per < m ? a + per : m;
+  uint32_t s = 0;
+  for (int i = a; i < b; ++i) s += hist[i];
+  part[threadIdx.x] = s;
+  __syncthreads();
+  for (int d = 1; d < 1024; d <<= 1) {
+    const uint32_t t = threadIdx.x >= (unsigned)d ? part[threadIdx.x - d] : 0;
+    __syncthreads();
+    part[threadIdx.x] += t;
+    __syncthreads();
+  }
+  s = part[threadIdx.x] - s;
+  for (int i = a; i < b; ++i) {
+    const uint32_t t = hist[i];
+    hist[i] = s;
+    s += t;
+  }
+}
+__global__ __launch_bounds__(256) void embed_place_k(const uint32_t* __restrict__ keys, const uint32_t* __restrict__ pos, int n, int shift,
+                                                     const uint32_t* __restrict__ hist, int blocks, uint32_t* __restrict__ okeys,
+                                                     uint32_t* __restrict__ opos) {
+  __shared__ uint32_t next[256], have[4][256];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  next[tid] = hist[tid * blocks + blockIdx.x];
+  for (int u = 0; u < kTile / 256; ++u) {
+    const int i = blockIdx.x * kTile + u * 256 + tid;
+    const bool in = i < n;
+    const uint32_t k = in ? keys[i] : 0, p = in ? pos[i] : 0, d = (k >> shift) & 255;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) have[w][tid] = 0;
+    __syncthreads();
+    uint64_t same = __ballot(in);                                // lanes of this wavefront with the same digit
+#pragma unroll
+    for (int b = 0; b < kDigit; ++b) {
+      const uint64_t m = __ballot((d >> b) & 1);
+      same &= (d >> b) & 1 ? m : ~m;
+    }
+    const uint32_t before = __popcll(same & ((1ull << lane) - 1));
+    if (in && before == 0) have[wave][d] = (uint32_t)__popcll(same);
+    __syncthreads();
+    if (in) {
+      uint32_t at = next[d] + before;
+      for (int w = 0; w < wave; ++w) at += have[w][d];
+      okeys[at] = k;
+      opos[at] = p;
+    }
+    __syncthreads();
+    next[tid] += have[0][tid] + have[1][tid] + have[2][tid] + have[3][tid];
+    __syncthreads();
+  }
+}
+
+template <typename E>
+__global__ __launch_bounds__(256) void embed_sum_k(const uint32_t* __restrict__ skeys, const uint32_t* __restrict__ spos, int n, int width,
+                                                   float scale, const E* __restrict__ dy, int64_t lddy, float* __restrict__ dtable,
+                                                   int64_t lddt, int accumulate, float* __restrict__ part) {
+  constexpr int U = 8;
+  __shared__ uint32_t key[kRun + 2], pos[kRun];
+  const int tid = threadIdx.x, r0 = blockIdx.x * kRun, cnt = n - r0 < kRun ? n - r0 : kRun;
+  if (tid < kRun + 2) {
+    const int j = r0 + tid - 1;
+    key[tid] = j >= 0 && j < n && tid <= cnt + 1 ? skeys[j] : FTP_NO_ID;
+  }
+  if (tid < kRun) pos[tid] = tid < cnt ? spos[r0 + tid] : 0;
+  __syncthreads();
+  const int c = (blockIdx.y * 256 + tid) * 8;
+  const int left = width - c;
+  if (left <= 0) return;
+  float s[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s[e] = 0.f;
+  int start = 0;
+  for (int q = 0; q < cnt; q += U) {
+    if (key[q + 1] == FTP_NO_ID) return;                         // ids of no row come last
+    float v[U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool in = q + u < cnt && key[q + u + 1] != FTP_NO_ID;
+      tk_load8<E>(dy + (int64_t)(in ? pos[q + u] : pos[q]) * lddy + c, left, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (q + u >= cnt) break;
+      const uint32_t k = key[q + u + 1];
+      if (k == FTP_NO_ID) break;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[e] += v[u][e];
+      if (q + u + 1 < cnt && key[q + u + 2] == k) continue;
+      // the id's last token in this run
+      const bool before = start == 0 && key[0] == k, behind = q + u + 1 == cnt && key[q + u + 2] == k;
+      if (before || behind) {
+        // [run][0]: of an id that began in an earlier run; [run][1]: of one that begins here and goes on
+        tk_store8<float>(part + ((int64_t)blockIdx.x * 2 + (before ? 0 : 1)) * width + c, left, s);
+      } else {
+        float* const d = dtable + (int64_t)k * lddt + c;
+        float o[8];
+        if (accumulate) tk_load8<float>(d, left, o);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = accumulate ? fmaf(s[e], scale, o[e]) : s[e] * scale;
+        tk_store8<float>(d, left, o);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[e] = 0.f;
+      start = q + u + 1;
+    }
+  }
+}
+// ids with tokens in several runs: the run in which one begins adds up its parts
+__global__ __launch_bounds__(256) void embed_join_k(const uint32_t* __restrict__ skeys, int n, int width, float scale, float* __restrict__ dtable,
+                                                    int64_t lddt, int accumulate, const float* __restrict__ part) {
+  const int run = blockIdx.x, last = (run + 1) * kRun - 1;
+  if (last + 1 >= n) return;
+  const uint32_t k = skeys[last];
+  if (k == FTP_NO_ID || skeys[last + 1] != k || (run > 0 && skeys[run * kRun] == k && skeys[run * kRun - 1] == k)) return;
+  const int c = (blockIdx.y * 256 + threadIdx.x) * 8, left = width - c;
+  if (left <= 0) return;
+  float s[8], v[8];
+  tk_load8<float>(part + ((int64_t)run * 2 + 1) * width + c, left, s);
+  for (int r = run + 1;; ++r) {
+    tk_load8<float>(part + (int64_t)r * 2 * width + c, left, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] += v[e];
+    const int end = (r + 1) * kRun;
+    if (end >= n || skeys[end] != k) break;
+  }
+  float* const d = dtable + (int64_t)k * lddt + c;
+  if (accumulate) tk_load8<float>(d, left, v);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = accumulate ? fmaf(s[e], scale, v[e]) : s[e] * scale;
+  tk_store8<float>(d, left, v);
+}
+__global__ __launch_bounds__(256) void tk_fill_k(char* __restrict__ p, uint32_t rows, int64_t row_bytes, int64_t ld_bytes) {   // zeros
+  const uint32_t per = (uint32_t)((row_bytes + 15) / 16), all = rows * per;
+  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += gridDim.x * 256) {
+    const uint32_t r = i / per, c = i - r * per;
+    char* const q = p + (int64_t)r * ld_bytes + (int64_t)c * 16;
+    const int64_t left = row_bytes - (int64_t)c * 16;
+    if (left >= 16) tk_st16<float>(reinterpret_cast<float*>(q), u4v_t{0, 0, 0, 0});
+    else
+      for (int64_t b = 0; b < left; b += 4) *reinterpret_cast<float*>(q + b) = 0.f;
+  }
+}
+void tk_fill(hipStream_t st, void* p, int64_t rows, int64_t row_bytes, int64_t ld_bytes) {
+  if (ld_bytes == row_bytes && row_bytes < 65536) {              // rows one behind the other: longer ones
+    int64_t f = std::min<int64_t>(64, rows);
+    while (f > 1 && rows % f) --f;
+    rows /= f; row_bytes *= f; ld_bytes *= f;
+  }
+  by_rows(rows, (row_bytes + 15) / 16, [&](int64_t r, int m) {
+    hipLaunchKernelGGL(tk_fill_k, dim3(blocks_of((int64_t)m * ((row_bytes + 15) / 16), 8192)), dim3(256), 0, st, (char*)p + r * ld_bytes,
+                       (uint32_t)m, row_bytes, ld_bytes);
+  });
+}
+
+static inline size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
+size_t tk_embed_bwd_bytes(int64_t n, int vocab, int width) {
+  const size_t runs = (n + kRun - 1) / kRun, tiles = (n + kTile - 1) / kTile;
+  (void)vocab;
+  return 4 * up256((size_t)n * 4) + up256(tiles * 256 * 4) + up256(runs * 2 * width * 4);
+}
+void tk_embed_bwd(int dt, hipStream_t st, const void* ids, int ids64, int64_t n64, int vocab, int width, float scale, int64_t pad_id,
+                  const void* dy, int64_t lddy, float* dtable, int64_t lddt, int accumulate, void* ws) {
+  const int es = dt == 1 ? 2 : 4, n = (int)n64;
+  KScope ks(st, "tok_embed_bwd", (double)n * width * es + (accumulate ? 0.0 : (double)vocab * width * 4) + 4.0 * n, 2.0 * n * width, n, vocab, width);
+  if (!accumulate) tk_fill(st, dtable, vocab, (int64_t)width * 4, lddt * 4);
+  if (n == 0) return;
+  char* w = (char*)ws;
+  uint32_t* buf[4];
+  for (auto& b : buf) { b = (uint32_t*)w; w += up256((size_t)n * 4); }
+  const int tiles = (n + kTile - 1) / kTile, runs = (n + kRun - 1) / kRun;
+  uint32_t* hist = (uint32_t*)w;
+  w += up256((size_t)tiles * 256 * 4);
+  float* part = (float*)w;
+  const bool rank = n <= kRankMost;
+  uint32_t *k0 = buf[0], *p0 = buf[1], *k1 = buf[2], *p1 = buf[3];
+  if (ids64) hipLaunchKernelGGL(embed_keys_k<int64_t>, dim3(blocks_of(n, 4096)), dim3(256), 0, st, (const int64_t*)ids, n, vocab, pad_id, k0, rank ? nullptr : p0);
+  else hipLaunchKernelGGL(embed_keys_k<int32_t>, dim3(blocks_of(n, 4096)), dim3(256), 0, st, (const int32_t*)ids, n, vocab, pad_id, k0, rank ? nullptr : p0);
+  if (rank) {
+    hipLaunchKernelGGL(embed_rank_k, dim3((n + 63) / 64), dim3(256), 0, st, k0, n, k1, p1);
+    k0 = k1; p0 = p1;
+  } else {
+    // the digits of ids below vocab; no id (all ones) stays behind them because its digits are the largest, where one more bit than the largest id's counts
+    int bits = 1;
+    while (bits < 32 && ((uint64_t)vocab >> bits)) ++bits;
+    for (int shift = 0; shift < bits; shift += kDigit) {
+      hipLaunchKernelGGL(embed_count_k, dim3(tiles), dim3(256), 0, st, k0, n, shift, hist, tiles);
+      hipLaunchKernelGGL(embed_scan_k, dim3(1), dim3(1024), 0, st, hist, tiles * 256);
+      hipLaunchKernelGGL(embed_place_k, dim3(tiles), dim3(256), 0, st, k0, p0, n, shift, hist, tiles, k1, p1);
+      std::swap(k0, k1);
+      std::swap(p0, p1);
+    }
+  }
+  const dim3 g(runs, (width + 2047) / 2048);
+  if (dt == 1) hipLaunchKernelGGL(embed_sum_k<bf16_t>, g, dim3(256), 0, st, k0, p0, n, width, scale, (const bf16_t*)dy, lddy, dtable, lddt, accumulate, part);
+  else hipLaunchKernelGGL(embed_sum_k<float>, g, dim3(256), 0, st, k0, p0, n, width, scale, (const float*)dy, lddy, dtable, lddt, accumulate, part);
+  if (runs > 1) hipLaunchKernelGGL(embed_join_k, g, dim3(256), 0, st, k0, n, width, scale, dtable, lddt, accumulate, part);
+}
+
+// ---------------------------------------------------------------- activations in 8 bits
+// Four threads have a group of 32 columns, eight each: the group's largest magnitude goes between them without LDS.
+template <typename E>
+__global__ __launch_bounds__(256) void act8_pack_k(const E* __restrict__ x, int64_t ldx, int rows, int N, uint8_t* __restrict__ q, int64_t ldq,
+                                                   uint8_t* __restrict__ s, int64_t lds) {
+  const uint32_t per = (uint32_t)(N + 31) / 32 * 4, all = (uint32_t)rows * per;
+  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += gridDim.x * 256) {     // all is a multiple of 4: a group's threads stay together
+    const uint32_t r = i / per, c = (i - r * per) * 8;
+    const int left = N - (int)c;
+    float v[8];
+    tk_load8<E>(x + (int64_t)r * ldx + c, left, v);
+    float top = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = fmaxf(top, act8_mag(v[e]));
+    top = fmaxf(top, dpp_move<0xB1>(top));
+    top = fmaxf(top, dpp_move<0x4E>(top));
+    const uint32_t b = act8_scale(top);
+    const float inv = act8_inv(b);
+    const uint32_t lo = act8_pack4(v, inv), hi = act8_pack4(v + 4, inv);
+    uint8_t* const p = q + (int64_t)r * ldq + c;
+    if (left >= 8) {
+      *reinterpret_cast<TkAt<1>::v8*>(p) = u2v_t{lo, hi};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < left) p[e] = (uint8_t)((e < 4 ? lo : hi) >> (8 * (e & 3)));
+    }
+    if ((c & 31) == 0) s[(int64_t)r * lds + c / 32] = (uint8_t)b;
+  }
+}
+// pad_to >= N: columns from N to there become zero
+template <typename E>
+__global__ __launch_bounds__(256) void act8_unpack_k(const uint8_t* __restrict__ q, int64_t ldq, const uint8_t* __restrict__ s, int64_t lds,
+                                                     int rows, int N, int pad_to, E* __restrict__ y, int64_t ldy) {
+  const uint32_t per = (uint32_t)(pad_to + 7) / 8, all = (uint32_t)rows * per;
+  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += gridDim.x * 256) {
+    const uint32_t r = i / per, c = (i - r * per) * 8;
+    const int left = N - (int)c;
+    const uint8_t* const p = q + (int64_t)r * ldq + c;
+    uint32_t lo = 0, hi = 0;
+    if (left >= 8) {
+      const u2v_t t = *reinterpret_cast<const TkAt<1>::v8*>(p);
+      lo = t[0]; hi = t[1];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < left) (e < 4 ? lo : hi) |= (uint32_t)p[e] << (8 * (e & 3));
+    }
+    const float mul = left > 0 ? act8_mul(s[(int64_t)r * lds + c / 32]) : 0.f;
+    float v[8];
+    act8_unpack4(lo, mul, v);
+    act8_unpack4(hi, mul, v + 4);
+    tk_store8<E>(y + (int64_t)r * ldy + c, pad_to - (int)c, v);
+  }
+}
+void tk_act8_pack(int dt, hipStream_t st, const void* x, int64_t ldx, int64_t M, int N, uint8_t* q, int64_t ldq, uint8_t* s, int64_t lds) {
+  KScope ks(st, "tok_act8_pack", (double)M * N * ((dt == 1 ? 2 : 4) + 1 + 1.0 / 32), 2.0 * M * N, M, N);
+  const int64_t per = (int64_t)act8_groups(N) * 4;
+  by_rows(M, per, [&](int64_t r, int m) {
+    const unsigned b = blocks_of(m * per, 1 << 20);
+    if (dt == 1) hipLaunchKernelGGL(act8_pack_k<bf16_t>, dim3(b), dim3(256), 0, st, (const bf16_t*)x + r * ldx, ldx, m, N, q + r * ldq, ldq, s + r * lds, lds);
+    else hipLaunchKernelGGL(act8_pack_k<float>, dim3(b), dim3(256), 0, st, (const float*)x + r * ldx, ldx, m, N, q + r * ldq, ldq, s + r * lds, lds);
+  });
+}
+void tk_act8_unpack(int dt, hipStream_t st, const uint8_t* q, int64_t ldq, const uint8_t* s, int64_t lds, int64_t M, int N, int pad_to,
+                    void* y, int64_t ldy) {
+  KScope ks(st, "tok_act8_unpack", (double)M * N * ((dt == 1 ? 2 : 4) + 1 + 1.0 / 32), 1.0 * M * N, M, N);
+  const int64_t per = (pad_to + 7) / 8;
+  by_rows(M, per, [&](int64_t r, int m) {
+    const unsigned b = blocks_of(m * per, 1 << 20);
+    if (dt == 1) hipLaunchKernelGGL(act8_unpack_k<bf16_t>, dim3(b), dim3(256), 0, st, q + r * ldq, ldq, s + r * lds, lds, m, N, pad_to, (bf16_t*)y + r * ldy, ldy);
+    else hipLaunchKernelGGL(act8_unpack_k<float>, dim3(b), dim3(256), 0, st, q + r * ldq, ldq, s + r * lds, lds, m, N, pad_to, (float*)y + r * ldy, ldy);
+  });
+}
+
+// ---------------------------------------------------------------- linear layers
+template <typename E>
+__global__ __launch_bounds__(256) void tk_align_k(const E* __restrict__ x, int64_t ldx, int rows, int N, E* __restrict__ y, int64_t ldy) {
+  constexpr int V = 16 / sizeof(E);
+  const uint32_t per = (uint32_t)(ldy / V), all = (uint32_t)rows * per;
+  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += gridDim.x * 256) {
+    const uint32_t r = i / per, c = (i - r * per) * V;
+    const E* const p = x + (int64_t)r * ldx + c;
+    const int left = N - (int)c;
+    u4v_t t = {0, 0, 0, 0};
+    if (left >= V) {
+      t = tk_ld16<E>(p);
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        uint32_t b = 0;
+        if (e < left) b = sizeof(E) == 2 ? (uint32_t)*reinterpret_cast<const uint16_t*>(p + e) : *reinterpret_cast<const uint32_t*>(p + e);
+        if (sizeof(E) == 4) t[e & 3] = b;
+        else t[e / 2] |= b << (16 * (e & 1));
+      }
+    }
+    *reinterpret_cast<u4v_t*>(y + (int64_t)r * ldy + c) = t;
+  }
+}
+void tk_align(int dt, hipStream_t st, const void* x, int64_t ldx, int M, int N, void* y, int64_t ldy) {
+  KScope ks(st, "tok_align", 2.0 * M * N * (dt == 1 ? 2 : 4), 0, M, N);
+  const int64_t per = ldy / (dt == 1 ? 8 : 4);
+  by_rows(M, per, [&](int64_t r, int m) {
+    const unsigned b = blocks_of(m * per, 1 << 20);
+    if (dt == 1) hipLaunchKernelGGL(tk_align_k<bf16_t>, dim3(b), dim3(256), 0, st, (const bf16_t*)x + r * ldx, ldx, m, N, (bf16_t*)y + r * ldy, ldy);
+    else hipLaunchKernelGGL(tk_align_k<float>, dim3(b), dim3(256), 0, st, (const float*)x + r * ldx, ldx, m, N, (float*)y + r * ldy, ldy);
+  });
+}
+
+// dz = dy * act'(z) and its column sums.  A block has 256 columns (64 threads of four) of a chunk of rows, four threads to a column;
+// the sums are of dz before it is rounded.
+static int dz_rows(int M) { return std::max(32, (M + 255) / 256); }
+int tk_dz_chunks(int M) { return M > 0 ? (M + dz_rows(M) - 1) / dz_rows(M) : 0; }
+template <typename E>
+__global__ __launch_bounds__(256) void tk_dz_k(const E* __restrict__ dy, int64_t lddy, const E* __restrict__ z, int64_t ldz, int act, int M, int N,
+                                               int per, E* __restrict__ dz, int64_t ldd, float* __restrict__ part, int vec) {
+  __shared__ float4 sum[4][64];
+  const int lane = threadIdx.x & 63, ty = threadIdx.x >> 6, n = (blockIdx.x * 64 + lane) * 4;
+  const int r0 = blockIdx.y * per, r1 = r0 + per < M ? r0 + per : M;
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  const int wide = dz ? (int)ldd : N;
+  if (n < wide)
+    for (int r = r0 + ty; r < r1; r += 4) {
+      float v[4];
+      get4<E>(dy, lddy, r, n, N, vec & 1, v);
+      if (act != TACT_NONE) {
+        float t[4], a[4], d[4];
+        get4<E>(z, ldz, r, n, N, vec & 2, t);
+        tact_grad4(t, a, d, act);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] *= d[e];
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += n + e < N ? v[e] : 0.f;
+      if (dz) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = n + e < N ? v[e] : 0.f;
+        put4<E>(dz, ldd, r, n, (int)ldd, true, v);
+      }
+    }
+  if (!part) return;
+  sum[ty][lane] = make_float4(s[0], s[1], s[2], s[3]);
+  __syncthreads();
+  if (ty == 0) {
+    const float4 a = sum[0][lane], b = sum[1][lane], c = sum[2][lane], d = sum[3][lane];
+    const float t[4] = {(a.x + b.x) + (c.x + d.x), (a.y + b.y) + (c.y + d.y), (a.z + b.z) + (c.z + d.z), (a.w + b.w) + (c.w + d.w)};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (n + e < N) part[(int64_t)blockIdx.y * N + n + e] = t[e];
+  }
+}
+void tk_dz(int dt, hipStream_t st, const void* dy, int64_t lddy, const void* z, int64_t ldz, int act, int M, int N, void* dz,
+           int64_t ldd, float* part) {
+  const int es = dt == 1 ? 2 : 4;
+  KScope ks(st, "tok_dz", (double)M * N * es * ((act != TACT_NONE) + 1 + (dz != nullptr)), 4.0 * M * N, M, N);
+  const auto fits = [&](const void* p, int64_t ld) { return ((uintptr_t)p % (4 * es)) == 0 && ld % 4 == 0; };
+  const int vec = (fits(dy, lddy) ? 1 : 0) | (act != TACT_NONE && fits(z, ldz) ? 2 : 0);
+  const dim3 g((std::max<int64_t>(N, dz ? ldd : 0) + 255) / 256, tk_dz_chunks(M));
+  if (dt == 1) hipLaunchKernelGGL(tk_dz_k<bf16_t>, g, dim3(256), 0, st, (const bf16_t*)dy, lddy, (const bf16_t*)z, ldz, act, M, N, dz_rows(M), (bf16_t*)dz, ldd, part, vec);
+  else hipLaunchKernelGGL(tk_dz_k<float>, g, dim3(256), 0, st, (const float*)dy, lddy, (const float*)z, ldz, act, M, N, dz_rows(M), (float*)dz, ldd, part, vec);
+}
+// 64 columns a block, four threads to a column
+__global__ __launch_bounds__(256) void tk_colsum_join_k(const float* __restrict__ part, int chunks, int N, void* __restrict__ db, int bf16, int accumulate) {
+  __shared__ float sum[4][64];
+  const int lane = threadIdx.x & 63, ty = threadIdx.x >> 6, n = blockIdx.x * 64 + lane;
+  float s = 0.f;
+  if (n < N) {
+#pragma unroll 8
+    for (int c = ty; c < chunks; c += 4) s += part[(int64_t)c * N + n];
+  }
+  sum[ty][lane] = s;
+  __syncthreads();
+  if (ty || n >= N) return;
+  s = (sum[0][lane] + sum[1][lane]) + (sum[2][lane] + sum[3][lane]);
+  if (bf16) ((bf16_t*)db)[n] = f32_to_bf16(s);
+  else ((float*)db)[n] = accumulate ? ((float*)db)[n] + s : s;
+}
+void tk_colsum_join(hipStream_t st, const float* part, int chunks, int N, void* db, int out_dt, int accumulate) {
+  KScope ks(st, "tok_bias_grad", 4.0 * chunks * N, (double)chunks * N, chunks, N);
+  hipLaunchKernelGGL(tk_colsum_join_k, dim3((N + 63) / 64), dim3(256), 0, st, part, chunks, N, db, out_dt, accumulate);
+}
+
+}  // namespace ftp

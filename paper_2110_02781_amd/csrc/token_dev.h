@@ -1,0 +1,213 @@
+// Device functions the token kernels share: activations and their derivatives, the 8-bit form of activations, accesses to
+// four consecutive columns of a row of any alignment.
+#pragma once
+#include "dev_common.h"
+#include "token.h"
+
+namespace ftp {
+
+// 1 / (1 + e^-t): the exponential is the hardware's, 2^x; t = -inf .. inf give 0 .. 1
+__device__ __forceinline__ float sigmoid_f(float t) { return __builtin_amdgcn_rcpf(1.f + __expf(-t)); }
+// GELU in its tanh form: (1 + tanh(s)) / 2 = sigmoid(2 s), s = sqrt(2/pi) (z + 0.044715 z^3).  The square is capped so that
+// 0 * inf cannot come up: beyond |z| = 1000 the sigmoid is 0 or 1 exactly.
+#define FTP_GELU_2K 1.5957691216057308f
+#define FTP_GELU_C 0.044715f
+
+__device__ __forceinline__ void tact4(float v[4], int act) {
+  if (act == TACT_SILU) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] *= sigmoid_f(v[e]);
+  } else if (act == TACT_GELU) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float z = v[e], z2 = fminf(z * z, 1e6f);
+      v[e] = z * sigmoid_f(FTP_GELU_2K * z * fmaf(FTP_GELU_C, z2, 1.f));
+    }
+  } else if (act != TACT_NONE) {                 // comparisons, so that NaN stays NaN
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = v[e] < 0.f ? 0.f : v[e];
+      if (act == TACT_RELU6) v[e] = v[e] > 6.f ? 6.f : v[e];
+    }
+  }
+}
+// a <- act(z), d <- act'(z)
+__device__ __forceinline__ void tact_grad4(const float z[4], float a[4], float d[4], int act) {
+  if (act == TACT_SILU) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float p = sigmoid_f(z[e]);
+      a[e] = z[e] * p;
+      d[e] = fmaf(a[e], 1.f - p, p);
+    }
+  } else if (act == TACT_GELU) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float z2 = fminf(z[e] * z[e], 1e6f);
+      const float p = sigmoid_f(FTP_GELU_2K * z[e] * fmaf(FTP_GELU_C, z2, 1.f));
+      a[e] = z[e] * p;
+      d[e] = fmaf(a[e] * (1.f - p), FTP_GELU_2K * fmaf(3.f * FTP_GELU_C, z2, 1.f), p);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      a[e] = z[e];
+      d[e] = 1.f;
+      if (act != TACT_NONE) {
+        const bool over = act == TACT_RELU6 && z[e] >= 6.f;
+        a[e] = z[e] < 0.f ? 0.f : over ? 6.f : z[e];
+        d[e] = z[e] > 0.f && !over ? 1.f : 0.f;
+      }
+    }
+  }
+}
+
+// ---- four consecutive columns n .. n+3 of a row of N; `vec`: the row's fours are aligned ----
+template <typename E>
+__device__ __forceinline__ void get4(const void* base, int64_t ld, int64_t m, int n, int N, bool vec, float v[4]) {
+  const E* p = (const E*)base + m * ld + n;
+  if (vec && n + 3 < N) {
+    const float4 t = load4(p);
+    v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = n + e < N ? to_f32(p[e]) : 0.f;
+  }
+}
+template <typename E>
+__device__ __forceinline__ void put4(void* base, int64_t ld, int64_t m, int n, int N, bool vec, const float v[4]) {
+  E* p = (E*)base + m * ld + n;
+  if (vec && n + 3 < N) {
+    store4(p, make_float4(v[0], v[1], v[2], v[3]));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (n + e < N) p[e] = from_f32<E>(v[e]);
+  }
+}
+
+// ---- the 8-bit form: groups of 32 columns share 2^(byte - 127); values are e4m3 (largest finite 448 = 1.75 * 2^8) ----
+// largest finite magnitude of a group -> the byte.  The exponent field says top = m * 2^E, m in [1, 2): 2^(E-8) holds m <= 1.75.
+__device__ __forceinline__ uint32_t act8_scale(float top) {
+  const uint32_t b = __float_as_uint(top), E = b >> 23, over = (b & 0x7fffffu) > 0x600000u ? 1u : 0u;
+  const int s = (int)E - 8 + (int)over;
+  return s < 0 ? 0u : (uint32_t)s;
+}
+__device__ __forceinline__ float act8_mul(uint32_t s) { return __uint_as_float(s ? s << 23 : 0x00400000u); }         // 2^(s-127)
+__device__ __forceinline__ float act8_inv(uint32_t s) { return __uint_as_float(s < 254 ? (254u - s) << 23 : 0x00400000u); }
+__device__ __forceinline__ float act8_mag(float v) {                        // magnitude that counts for the scale
+  const float a = fabsf(v);
+  return a <= 3.402823466e38f ? a : 0.f;                                    // an infinity or NaN does not
+}
+__device__ __forceinline__ uint32_t act8_pack4(const float v[4], float inv) {
+  float t[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) t[e] = fabsf(v[e]) <= 3.402823466e38f ? v[e] * inv : __uint_as_float(0x7fc00000u);
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(t[0], t[1], 0, false);
+  r = __builtin_amdgcn_cvt_pk_fp8_f32(t[2], t[3], r, true);
+  return (uint32_t)r;
+}
+__device__ __forceinline__ void act8_unpack4(uint32_t q, float mul, float v[4]) {
+  const f32x2_t lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)q, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)q, true);
+  v[0] = lo.x * mul; v[1] = lo.y * mul; v[2] = hi.x * mul; v[3] = hi.y * mul;
+}
+__device__ __forceinline__ uint32_t get_q4(const void* base, int64_t ld, int64_t m, int n, int N, bool vec) {
+  const uint8_t* p = (const uint8_t*)base + m * ld + n;
+  if (vec && n + 3 < N) return *reinterpret_cast<const uint32_t*>(p);
+  uint32_t r = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (n + e < N) r |= (uint32_t)p[e] << (8 * e);
+  return r;
+}
+__device__ __forceinline__ void put_q4(void* base, int64_t ld, int64_t m, int n, int N, bool vec, uint32_t q) {
+  uint8_t* p = (uint8_t*)base + m * ld + n;
+  if (vec && n + 3 < N) {
+    *reinterpret_cast<uint32_t*>(p) = q;
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (n + e < N) p[e] = (uint8_t)(q >> (8 * e));
+}
+
+// ---- results of four columns, the same code behind a tile and behind the joining of split reductions ----
+template <typename E>
+__device__ __forceinline__ void tg_linear4(const TgJob& p, int64_t m, int n, float v[4]) {
+  if (p.bias) {
+    float b[4];
+    get4<float>(p.bias, 0, 0, n, p.N, p.flags & TG_VEC_BIAS, b);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += b[e];
+  }
+  if (p.z) put4<E>(p.z, p.ldz, m, n, p.N, p.flags & TG_VEC_Z, v);
+  tact4(v, p.act);                               // of the sum itself, not of the z that is kept: one rounding less
+  if (p.res) {
+    float r[4];
+    get4<E>(p.res, p.ldr, m, n, p.N, p.flags & TG_VEC_RES, r);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += r[e];
+  }
+  put4<E>(p.out, p.ldo, m, n, p.N, p.flags & TG_VEC_OUT, v);
+}
+// act(g) * u into the hidden rows, whose pad columns (up to a multiple of 16 bytes) become zero: g and u are zero there
+template <typename E>
+__device__ __forceinline__ void tg_glu4(const TgJob& p, int64_t m, int n, const float g[4], const float u[4]) {
+  if (p.save == 1) {
+    put4<E>(p.z, p.ldz, m, n, p.N, p.flags & TG_VEC_Z, g);
+    put4<E>(p.up, p.ldu, m, n, p.N, p.flags & TG_VEC_Z, u);
+  }
+  float h[4] = {g[0], g[1], g[2], g[3]};
+  tact4(h, p.act);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) h[e] *= u[e];
+  put4<E>(p.out, p.ldo, m, n, (int)p.ldo, true, h);
+}
+__device__ __forceinline__ void tg_keep8(void* q, int64_t ldq, uint8_t* s, int64_t lds, int64_t m, int n, int N, bool vec, bool lead,
+                                         float top, const float v[4]) {
+  const uint32_t b = act8_scale(top);
+  if (n < N) put_q4(q, ldq, m, n, N, vec, act8_pack4(v, act8_inv(b)));
+  if (lead && n < N) s[m * lds + n / kAct8Group] = (uint8_t)b;
+}
+template <typename E>
+__device__ __forceinline__ void tg_glubwd4(const TgJob& p, int64_t m, int n, const float dh[4]) {
+  float g[4], u[4];
+  const bool vec = p.flags & TG_VEC_Z;
+  if (p.save == 2) {
+    const bool in = n < p.N;
+    const float sg = in ? act8_mul(p.zs[m * p.lds + n / kAct8Group]) : 0.f, su = in ? act8_mul(p.us[m * p.lds + n / kAct8Group]) : 0.f;
+    act8_unpack4(get_q4(p.z, p.ldz, m, n, p.N, vec), sg, g);
+    act8_unpack4(get_q4(p.up, p.ldu, m, n, p.N, vec), su, u);
+  } else {
+    get4<E>(p.z, p.ldz, m, n, p.N, vec, g);
+    get4<E>(p.up, p.ldu, m, n, p.N, vec, u);
+  }
+  float a[4], d[4], dg[4], du[4];
+  tact_grad4(g, a, d, p.act);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    dg[e] = dh[e] * u[e] * d[e];
+    du[e] = dh[e] * a[e];
+    a[e] *= u[e];
+  }
+  // rounded to the type of the products that follow, as their operands
+  put4<E>(p.dgate, p.ldd, m, n, (int)p.ldd, true, dg);
+  put4<E>(p.dup, p.ldd, m, n, (int)p.ldd, true, du);
+  put4<E>(p.out, p.ldo, m, n, (int)p.ldo, true, a);
+}
+template <typename E>
+__device__ __forceinline__ void tg_grad4(const TgJob& p, int64_t m, int n, float v[4]) {
+  if (p.out_f32) {
+    if (p.accumulate) {
+      float o[4];
+      get4<float>(p.out, p.ldo, m, n, p.N, p.flags & TG_VEC_OUT, o);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += o[e];
+    }
+    put4<float>(p.out, p.ldo, m, n, p.N, p.flags & TG_VEC_OUT, v);
+  } else {
+    put4<E>(p.out, p.ldo, m, n, p.N, p.flags & TG_VEC_OUT, v);
+  }
+}
+
+}  // namespace ftp
