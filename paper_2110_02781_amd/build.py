@@ -10,9 +10,9 @@ LIB = os.path.join(HERE, "libftp_hip.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 
 COMMON = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",
-          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-          # MFMA accumulators in ordinary VGPRs: the epilogues read them without accvgpr moves
-          "-mllvm", "-amdgpu-mfma-vgpr-form"]
+          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
+# MFMA accumulators in ordinary VGPRs: the epilogues read them without accvgpr moves
+VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
 SOURCES = [
     ("k_elem.hip", ["-x", "hip"]),
     ("k_conv.hip", ["-x", "hip"]),
@@ -20,7 +20,7 @@ SOURCES = [
     ("k_gemm.hip", ["-x", "hip"]),
     ("k_fused.hip", ["-x", "hip"]),
     ("k_gemm_deep.hip", ["-x", "hip"]),
-    ("k_token_gemm.hip", ["-x", "hip"]),
+    ("k_token_gemm.hip", ["-x", "hip", "no-vgpr-form"]),   # its large tile's sums fill the accumulation registers
     ("k_token.hip", ["-x", "hip"]),
     ("token.cpp", ["-x", "hip"]),
     ("stage.cpp", ["-x", "hip"]),
@@ -35,7 +35,9 @@ def _compile(item):
     if extra[:2] == ["-x", "c++"]:
         cmd = ["hipcc", "-O2", "-fPIC", "-std=c++17", "-Wall"] + extra + ["-c", os.path.join(CSRC, src), "-o", obj]
     else:
-        cmd = ["hipcc"] + COMMON + extra + ["-c", os.path.join(CSRC, src), "-o", obj]
+        form = [] if "no-vgpr-form" in extra else VGPR_FORM
+        extra = [e for e in extra if e != "no-vgpr-form"]
+        cmd = ["hipcc"] + COMMON + form + extra + ["-c", os.path.join(CSRC, src), "-o", obj]
     r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     out = "\n".join(l for l in r.stdout.splitlines() if "packed-fp32-ops" not in l)
     if r.returncode != 0:

@@ -62,11 +62,11 @@ __device__ __forceinline__ void tact_grad4(const float z[4], float a[4], float d
   }
 }
 
-// ---- four consecutive columns n .. n+3 of a row of N; `vec`: the row's fours are aligned ----
-template <typename E>
+// ---- four consecutive columns n .. n+3 of a row of N; `vec`: the row's fours are aligned; F: known to be, and inside ----
+template <typename E, bool F = false>
 __device__ __forceinline__ void get4(const void* base, int64_t ld, int64_t m, int n, int N, bool vec, float v[4]) {
   const E* p = (const E*)base + m * ld + n;
-  if (vec && n + 3 < N) {
+  if (F || (vec && n + 3 < N)) {
     const float4 t = load4(p);
     v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
   } else {
@@ -74,10 +74,10 @@ __device__ __forceinline__ void get4(const void* base, int64_t ld, int64_t m, in
     for (int e = 0; e < 4; ++e) v[e] = n + e < N ? to_f32(p[e]) : 0.f;
   }
 }
-template <typename E>
+template <typename E, bool F = false>
 __device__ __forceinline__ void put4(void* base, int64_t ld, int64_t m, int n, int N, bool vec, const float v[4]) {
   E* p = (E*)base + m * ld + n;
-  if (vec && n + 3 < N) {
+  if (F || (vec && n + 3 < N)) {
     store4(p, make_float4(v[0], v[1], v[2], v[3]));
   } else {
 #pragma unroll
@@ -111,18 +111,20 @@ __device__ __forceinline__ void act8_unpack4(uint32_t q, float mul, float v[4]) 
   const f32x2_t lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)q, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)q, true);
   v[0] = lo.x * mul; v[1] = lo.y * mul; v[2] = hi.x * mul; v[3] = hi.y * mul;
 }
+template <bool F = false>
 __device__ __forceinline__ uint32_t get_q4(const void* base, int64_t ld, int64_t m, int n, int N, bool vec) {
   const uint8_t* p = (const uint8_t*)base + m * ld + n;
-  if (vec && n + 3 < N) return *reinterpret_cast<const uint32_t*>(p);
+  if (F || (vec && n + 3 < N)) return *reinterpret_cast<const uint32_t*>(p);
   uint32_t r = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
     if (n + e < N) r |= (uint32_t)p[e] << (8 * e);
   return r;
 }
+template <bool F = false>
 __device__ __forceinline__ void put_q4(void* base, int64_t ld, int64_t m, int n, int N, bool vec, uint32_t q) {
   uint8_t* p = (uint8_t*)base + m * ld + n;
-  if (vec && n + 3 < N) {
+  if (F || (vec && n + 3 < N)) {
     *reinterpret_cast<uint32_t*>(p) = q;
     return;
   }
@@ -131,83 +133,147 @@ __device__ __forceinline__ void put_q4(void* base, int64_t ld, int64_t m, int n,
     if (n + e < N) p[e] = (uint8_t)(q >> (8 * e));
 }
 
-// ---- results of four columns, the same code behind a tile and behind the joining of split reductions ----
-template <typename E>
-__device__ __forceinline__ void tg_linear4(const TgJob& p, int64_t m, int n, float v[4]) {
-  if (p.bias) {
-    float b[4];
-    get4<float>(p.bias, 0, 0, n, p.N, p.flags & TG_VEC_BIAS, b);
+// ---- results of four columns, the same code behind a tile and behind the joining of split reductions.  In two parts: `request` loads what the
+// results need from memory (rows past the last: the last one's), `finish` computes and stores. ----
+template <typename E> struct Tg4;
+template <> struct Tg4<bf16_t> { typedef uint2 raw; };
+template <> struct Tg4<float> { typedef float4 raw; };
+// four columns as stored; where they do not go as one, element by element
+template <typename E, bool F = false>
+__device__ __forceinline__ typename Tg4<E>::raw get_raw4(const void* base, int64_t ld, int64_t m, int n, int N, bool vec) {
+  const E* p = (const E*)base + m * ld + n;
+  if (F || (vec && n + 3 < N)) return *reinterpret_cast<const typename Tg4<E>::raw*>(p);
+  E t[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] += b[e];
-  }
-  if (p.z) put4<E>(p.z, p.ldz, m, n, p.N, p.flags & TG_VEC_Z, v);
-  tact4(v, p.act);                               // of the sum itself, not of the z that is kept: one rounding less
-  if (p.res) {
-    float r[4];
-    get4<E>(p.res, p.ldr, m, n, p.N, p.flags & TG_VEC_RES, r);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] += r[e];
-  }
-  put4<E>(p.out, p.ldo, m, n, p.N, p.flags & TG_VEC_OUT, v);
+  for (int e = 0; e < 4; ++e) t[e] = n + e < N ? p[e] : (E)0;
+  typename Tg4<E>::raw r;
+  __builtin_memcpy(&r, t, sizeof(r));
+  return r;
 }
-// act(g) * u into the hidden rows, whose pad columns (up to a multiple of 16 bytes) become zero: g and u are zero there
 template <typename E>
+__device__ __forceinline__ void open4(const typename Tg4<E>::raw& r, float v[4]) {
+  const float4 t = load4(reinterpret_cast<const E*>(&r));
+  v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
+}
+
+template <typename E, int EPI, bool F = false> struct TgSide;
+
+template <typename E, bool F> struct TgSide<E, TG_LINEAR, F> {
+  typename Tg4<E>::raw res;
+  __device__ __forceinline__ void request(const TgJob& p, int64_t m, int n) {
+    if (p.res) res = get_raw4<E, F>(p.res, p.ldr, m < p.M ? m : p.M - 1, n, p.N, p.flags & TG_VEC_RES);
+  }
+  __device__ __forceinline__ void finish(const TgJob& p, int64_t m, int n, float v[4]) const {
+    if (p.bias) {
+      float b[4];
+      get4<float, F>(p.bias, 0, 0, n, p.N, p.flags & TG_VEC_BIAS, b);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += b[e];
+    }
+    if (p.z) put4<E, F>(p.z, p.ldz, m, n, p.N, p.flags & TG_VEC_Z, v);
+    tact4(v, p.act);                             // of the sum itself, not of the z that is kept: one rounding less
+    if (p.res) {
+      float r[4];
+      open4<E>(res, r);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += r[e];
+    }
+    put4<E, F>(p.out, p.ldo, m, n, p.N, p.flags & TG_VEC_OUT, v);
+  }
+};
+
+template <typename E, bool F> struct TgSide<E, TG_GLUBWD, F> {
+  typename Tg4<E>::raw g, u;                     // in 8 bits: x the values, y the scale
+  __device__ __forceinline__ void request(const TgJob& p, int64_t m, int n) {
+    const bool vec = p.flags & TG_VEC_Z;
+    const int64_t r = m < p.M ? m : p.M - 1;
+    if (p.save == 2) {
+      const bool in = F || n < p.N;
+      const int64_t s = r * p.lds + (in ? n : 0) / kAct8Group;
+      uint32_t q[4] = {get_q4<F>(p.z, p.ldz, r, n, p.N, vec), in ? p.zs[s] : 0u, get_q4<F>(p.up, p.ldu, r, n, p.N, vec), in ? p.us[s] : 0u};
+      __builtin_memcpy(&g, q, 8);
+      __builtin_memcpy(&u, q + 2, 8);
+    } else {
+      g = get_raw4<E, F>(p.z, p.ldz, r, n, p.N, vec);
+      u = get_raw4<E, F>(p.up, p.ldu, r, n, p.N, vec);
+    }
+  }
+  __device__ __forceinline__ void finish(const TgJob& p, int64_t m, int n, const float dh[4]) const {
+    float gv[4], uv[4];
+    if (p.save == 2) {
+      uint32_t q[4];
+      __builtin_memcpy(q, &g, 8);
+      __builtin_memcpy(q + 2, &u, 8);
+      act8_unpack4(q[0], act8_mul(q[1]), gv);
+      act8_unpack4(q[2], act8_mul(q[3]), uv);
+    } else {
+      open4<E>(g, gv);
+      open4<E>(u, uv);
+    }
+    float a[4], d[4], dg[4], du[4];
+    tact_grad4(gv, a, d, p.act);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      dg[e] = dh[e] * uv[e] * d[e];
+      du[e] = dh[e] * a[e];
+      a[e] *= uv[e];
+    }
+    // rounded to the type of the products that follow, as their operands
+    put4<E, F>(p.dgate, p.ldd, m, n, (int)p.ldd, true, dg);
+    put4<E, F>(p.dup, p.ldd, m, n, (int)p.ldd, true, du);
+    put4<E, F>(p.out, p.ldo, m, n, (int)p.ldo, true, a);
+  }
+};
+
+template <typename E, bool F> struct TgSide<E, TG_GRAD, F> {
+  __device__ __forceinline__ void request(const TgJob&, int64_t, int) {}
+  __device__ __forceinline__ void finish(const TgJob& p, int64_t m, int n, float v[4]) const {
+    if (p.out_f32) {
+      if (p.accumulate) {
+        float o[4];
+        get4<float, F>(p.out, p.ldo, m, n, p.N, p.flags & TG_VEC_OUT, o);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += o[e];
+      }
+      put4<float, F>(p.out, p.ldo, m, n, p.N, p.flags & TG_VEC_OUT, v);
+    } else {
+      put4<E, F>(p.out, p.ldo, m, n, p.N, p.flags & TG_VEC_OUT, v);
+    }
+  }
+};
+template <typename E, int EPI>
+__device__ __forceinline__ void tg_finish4(const TgJob& p, int64_t m, int n, float v[4]) {
+  TgSide<E, EPI> s;
+  s.request(p, m, n);
+  s.finish(p, m, n, v);
+}
+
+// largest of the eight lanes that share 32 columns of a row (lanes 8 i .. 8 i + 7): inside fours, then a half row mirrored
+__device__ __forceinline__ float tg_max8(float x) {
+  x = fmaxf(x, dpp_move<0xB1>(x));
+  x = fmaxf(x, dpp_move<0x4E>(x));
+  return fmaxf(x, dpp_move<0x141>(x));
+}
+
+// act(g) * u into the hidden rows, whose pad columns (up to a multiple of 16 bytes) become zero: g and u are zero there
+template <typename E, bool F = false>
 __device__ __forceinline__ void tg_glu4(const TgJob& p, int64_t m, int n, const float g[4], const float u[4]) {
   if (p.save == 1) {
-    put4<E>(p.z, p.ldz, m, n, p.N, p.flags & TG_VEC_Z, g);
-    put4<E>(p.up, p.ldu, m, n, p.N, p.flags & TG_VEC_Z, u);
+    put4<E, F>(p.z, p.ldz, m, n, p.N, p.flags & TG_VEC_Z, g);
+    put4<E, F>(p.up, p.ldu, m, n, p.N, p.flags & TG_VEC_Z, u);
   }
   float h[4] = {g[0], g[1], g[2], g[3]};
   tact4(h, p.act);
 #pragma unroll
   for (int e = 0; e < 4; ++e) h[e] *= u[e];
-  put4<E>(p.out, p.ldo, m, n, (int)p.ldo, true, h);
+  put4<E, F>(p.out, p.ldo, m, n, (int)p.ldo, true, h);
 }
+template <bool F = false>
 __device__ __forceinline__ void tg_keep8(void* q, int64_t ldq, uint8_t* s, int64_t lds, int64_t m, int n, int N, bool vec, bool lead,
                                          float top, const float v[4]) {
   const uint32_t b = act8_scale(top);
-  if (n < N) put_q4(q, ldq, m, n, N, vec, act8_pack4(v, act8_inv(b)));
-  if (lead && n < N) s[m * lds + n / kAct8Group] = (uint8_t)b;
-}
-template <typename E>
-__device__ __forceinline__ void tg_glubwd4(const TgJob& p, int64_t m, int n, const float dh[4]) {
-  float g[4], u[4];
-  const bool vec = p.flags & TG_VEC_Z;
-  if (p.save == 2) {
-    const bool in = n < p.N;
-    const float sg = in ? act8_mul(p.zs[m * p.lds + n / kAct8Group]) : 0.f, su = in ? act8_mul(p.us[m * p.lds + n / kAct8Group]) : 0.f;
-    act8_unpack4(get_q4(p.z, p.ldz, m, n, p.N, vec), sg, g);
-    act8_unpack4(get_q4(p.up, p.ldu, m, n, p.N, vec), su, u);
-  } else {
-    get4<E>(p.z, p.ldz, m, n, p.N, vec, g);
-    get4<E>(p.up, p.ldu, m, n, p.N, vec, u);
-  }
-  float a[4], d[4], dg[4], du[4];
-  tact_grad4(g, a, d, p.act);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    dg[e] = dh[e] * u[e] * d[e];
-    du[e] = dh[e] * a[e];
-    a[e] *= u[e];
-  }
-  // rounded to the type of the products that follow, as their operands
-  put4<E>(p.dgate, p.ldd, m, n, (int)p.ldd, true, dg);
-  put4<E>(p.dup, p.ldd, m, n, (int)p.ldd, true, du);
-  put4<E>(p.out, p.ldo, m, n, (int)p.ldo, true, a);
-}
-template <typename E>
-__device__ __forceinline__ void tg_grad4(const TgJob& p, int64_t m, int n, float v[4]) {
-  if (p.out_f32) {
-    if (p.accumulate) {
-      float o[4];
-      get4<float>(p.out, p.ldo, m, n, p.N, p.flags & TG_VEC_OUT, o);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] += o[e];
-    }
-    put4<float>(p.out, p.ldo, m, n, p.N, p.flags & TG_VEC_OUT, v);
-  } else {
-    put4<E>(p.out, p.ldo, m, n, p.N, p.flags & TG_VEC_OUT, v);
-  }
+  if (F || n < N) put_q4<F>(q, ldq, m, n, N, vec, act8_pack4(v, act8_inv(b)));
+  if (lead && (F || n < N)) s[m * lds + n / kAct8Group] = (uint8_t)b;
 }
 
 }  // namespace ftp

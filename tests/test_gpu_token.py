@@ -54,7 +54,7 @@ def given(a, torch, n):
 # reductions, the large tile
 LINEAR = [(1, 1, 1, 0, 0), (1, 64, 16, 0, 0), (2, 7, 3, 1, 1), (16, 129, 33, 0, 0), (17, 129, 33, 0, 3), (5, 4104, 40, 8, 0), (33, 4097, 21, 0, 0),
           (130, 64, 128, 0, 0), (129, 200, 130, 5, 0), (300, 331, 203, 0, 1), (64, 72, 520, 8, 8)]
-BIG = [(1030, 520, 1032, 0, 0), (2050, 136, 2056, 8, 0)]
+BIG = [(4090, 4088, 4072, 0, 0), (4095, 4089, 4001, 8, 1)]
 
 
 def linear_case(env, dtype, act, rows, k, n, slack, skip, bias=True, res=True, grad=None, accumulate=0, x8=False, seed=1):
@@ -135,9 +135,28 @@ def test_linear_activations(env, dtype, act):
         linear_case(env, dtype, act, rows, 96, 77, 0, 0, bias=act != "none", res=act != "relu")
 
 
+class routes:
+    """the tiles that the products inside took, by family: {"tok_linear": {"256", ...}, ...}"""
+
+    def __init__(self, P):
+        self.P, self.took = P, {}
+
+    def __enter__(self):
+        self.P.ktrace_begin(-512)
+        return self.took
+
+    def __exit__(self, *_):
+        for r in self.P.ktrace_end():
+            if r["name"].startswith("__route "):
+                tile, rest = r["name"][8:].split(" tok_")
+                self.took.setdefault("tok_" + rest.split()[0], set()).add(tile)
+
+
 @pytest.mark.parametrize("rows,k,n,slack,skip", BIG)
 def test_linear_large_tile(env, rows, k, n, slack, skip):
-    linear_case(env, "bf16", "silu", rows, k, n, slack, skip)
+    with routes(env[1]) as took:
+        linear_case(env, "bf16", "silu", rows, k, n, slack, skip)
+    assert took == {"tok_linear": {"256"}, "tok_wgrad": {"256"}}, took
 
 
 @pytest.mark.parametrize("accumulate", [0, 1])
@@ -267,9 +286,11 @@ def test_ffn_activations(env, act):
         ffn_case(env, dtype, act, 0, 7, 64, 72, 0, 0)
 
 
-def test_ffn_large_tile(env):
-    for save in (1, 2):
-        ffn_case(env, "bf16", "silu", save, 1040, 520, 1100, 0, 0)
+@pytest.mark.parametrize("save,rows,d,f", [(1, 4090, 4088, 4090), (2, 4095, 4089, 4064)])
+def test_ffn_large_tile(env, save, rows, d, f):
+    with routes(env[1]) as took:
+        ffn_case(env, "bf16", "silu", save, rows, d, f, 0, 0)
+    assert took == {k: {"256"} for k in ("tok_glu", "tok_glu_bwd", "tok_linear", "tok_wgrad")}, took
 
 
 def test_ffn_split_reduction(env):
