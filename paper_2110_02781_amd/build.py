@@ -20,7 +20,8 @@ SOURCES = [
     ("k_gemm.hip", ["-x", "hip"]),
     ("k_fused.hip", ["-x", "hip"]),
     ("k_gemm_deep.hip", ["-x", "hip"]),
-    ("k_token_gemm.hip", ["-x", "hip", "no-vgpr-form"]),   # its large tile's sums fill the accumulation registers
+    ("k_token_big.hip", ["-x", "hip", "no-vgpr-form"]),    # its sums fill the accumulation registers
+    ("k_token_gemm.hip", ["-x", "hip"]),
     ("k_token.hip", ["-x", "hip"]),
     ("token.cpp", ["-x", "hip"]),
     ("stage.cpp", ["-x", "hip"]),

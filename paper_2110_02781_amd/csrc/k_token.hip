@@ -100,11 +100,35 @@ void tk_embed(int dt, hipStream_t st, const void* ids, int ids64, int64_t n, int
   });
 }
 
+// zeros: block b of nb, blocks of T threads
+template <int T>
+__device__ __forceinline__ void tk_fill_rows(char* __restrict__ p, uint32_t rows, int64_t row_bytes, int64_t ld_bytes, uint32_t b, uint32_t nb) {
+  const uint32_t per = (uint32_t)((row_bytes + 15) / 16), all = rows * per;
+  for (uint32_t i = b * T + threadIdx.x; i < all; i += nb * T) {
+    const uint32_t r = i / per, c = i - r * per;
+    char* const q = p + (int64_t)r * ld_bytes + (int64_t)c * 16;
+    const int64_t left = row_bytes - (int64_t)c * 16;
+    if (left >= 16) tk_st16<float>(reinterpret_cast<float*>(q), u4v_t{0, 0, 0, 0});
+    else
+      for (int64_t o = 0; o < left; o += 4) *reinterpret_cast<float*>(q + o) = 0.f;
+  }
+}
+__global__ __launch_bounds__(256) void tk_fill_k(char* __restrict__ p, uint32_t rows, int64_t row_bytes, int64_t ld_bytes) {
+  tk_fill_rows<256>(p, rows, row_bytes, ld_bytes, blockIdx.x, gridDim.x);
+}
+// rows one behind the other count as longer ones
+static void long_rows(int64_t& rows, int64_t& row_bytes, int64_t& ld_bytes) {
+  if (ld_bytes != row_bytes || row_bytes >= 65536) return;
+  int64_t f = std::min<int64_t>(64, rows);
+  while (f > 1 && rows % f) --f;
+  rows /= f; row_bytes *= f; ld_bytes *= f;
+}
+
 // ---------------------------------------------------------------- its gradient
 // Tokens are sorted by id, equal ids in the order of the tokens; then every kRun of them are one block's: it walks them with a running
 // sum per column and writes a row of the gradient where the id changes.  What an id has in other runs as well goes to memory as partial
 // sums, which embed_join_k adds in the order of the runs.  No atomics: the same tokens give the same bits.
-enum { kRun = 64, kRankMost = 16384, kTile = 4096, kDigit = 8 };
+enum { kRun = 16, kRankMost = 16384, kTile = 4096, kDigit = 8 };
 #define FTP_NO_ID 0xffffffffu
 
 template <typename I>
@@ -117,16 +141,24 @@ __global__ __launch_bounds__(256) void embed_keys_k(const I* __restrict__ ids, i
   }
 }
 // Few tokens: a token's place is how many come before it, counted outright: n^2 comparisons, two instructions for 64 of them, no passes
-// that wait for one another.  A block places 64 tokens, its wavefronts share the ones compared with.
-__global__ __launch_bounds__(256) void embed_rank_k(const uint32_t* __restrict__ keys, int n, uint32_t* __restrict__ skeys,
-                                                    uint32_t* __restrict__ spos) {
-  __shared__ uint32_t cnt[4][64];
+// that wait for one another.  A block places 64 tokens, its sixteen wavefronts share the ones compared with (they come by scalar loads, whose
+// latency four wavefronts to a SIMD hide: with one 16384 tokens took 85 us).  The blocks from `rank` on write the zeros that a gradient written
+// whole starts from, beside the counting, which leaves the memory alone.
+__global__ __launch_bounds__(1024) void embed_rank_k(const uint32_t* __restrict__ keys, int n, uint32_t* __restrict__ skeys,
+                                                     uint32_t* __restrict__ spos, int rank, char* __restrict__ zero, uint32_t rows, int64_t row_bytes,
+                                                     int64_t ld_bytes) {
+  constexpr int W = 16;
+  __shared__ uint32_t cnt[W][64];
+  if ((int)blockIdx.x >= rank) {
+    tk_fill_rows<1024>(zero, rows, row_bytes, ld_bytes, blockIdx.x - rank, gridDim.x - rank);
+    return;
+  }
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int first = blockIdx.x * 64, i = first + lane;
   const uint32_t k = i < n ? keys[i] : 0;
   uint32_t c = 0;
   // tokens in front of this block's count where their id is not larger, those behind it where it is smaller
-  const int per = ((n + 3) / 4 + 15) & ~15, j0 = wave * per, j1 = j0 + per < n ? j0 + per : n;
+  const int per = ((n + W - 1) / W + 15) & ~15, j0 = wave * per, j1 = j0 + per < n ? j0 + per : n;
   const int a1 = j1 < first ? j1 : first;
   int j = j0;
   for (; j + 16 <= a1; j += 16) {
@@ -144,7 +176,9 @@ __global__ __launch_bounds__(256) void embed_rank_k(const uint32_t* __restrict__
   cnt[wave][lane] = c;
   __syncthreads();
   if (wave == 0 && i < n) {
-    const uint32_t at = cnt[0][lane] + cnt[1][lane] + cnt[2][lane] + cnt[3][lane];
+    uint32_t at = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) at += cnt[w][lane];
     skeys[at] = k;
     spos[at] = (uint32_t)i;
   }
@@ -278,16 +312,33 @@ __global__ __launch_bounds__(256) void embed_join_k(const uint32_t* __restrict__
   if (last + 1 >= n) return;
   const uint32_t k = skeys[last];
   if (k == FTP_NO_ID || skeys[last + 1] != k || (run > 0 && skeys[run * kRun] == k && skeys[run * kRun - 1] == k)) return;
+  // the runs that it goes on in: those that begin with it, one behind the other (all lanes are here)
+  int cnt = 0;
+  for (;;) {
+    const int64_t at = (int64_t)(run + 1 + cnt + (int)(threadIdx.x & 63)) * kRun;
+    const uint64_t same = __ballot(at < n && skeys[at < n ? at : 0] == k);
+    cnt += ~same ? __builtin_ctzll(~same) : 64;
+    if (~same) break;
+  }
   const int c = (blockIdx.y * 256 + threadIdx.x) * 8, left = width - c;
   if (left <= 0) return;
   float s[8], v[8];
   tk_load8<float>(part + ((int64_t)run * 2 + 1) * width + c, left, s);
-  for (int r = run + 1;; ++r) {
-    tk_load8<float>(part + (int64_t)r * 2 * width + c, left, v);
+  const float* q = part + (int64_t)(run + 1) * 2 * width + c;
+  int r = 0;
+  for (; r + 8 <= cnt; r += 8, q += 16 * (int64_t)width) {
+    float t[8][8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) tk_load8<float>(q + u * 2 * (int64_t)width, left, t[u]);
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[e] += t[u][e];
+  }
+  for (; r < cnt; ++r, q += 2 * (int64_t)width) {
+    tk_load8<float>(q, left, v);
 #pragma unroll
     for (int e = 0; e < 8; ++e) s[e] += v[e];
-    const int end = (r + 1) * kRun;
-    if (end >= n || skeys[end] != k) break;
   }
   float* const d = dtable + (int64_t)k * lddt + c;
   if (accumulate) tk_load8<float>(d, left, v);
@@ -295,23 +346,8 @@ __global__ __launch_bounds__(256) void embed_join_k(const uint32_t* __restrict__
   for (int e = 0; e < 8; ++e) v[e] = accumulate ? fmaf(s[e], scale, v[e]) : s[e] * scale;
   tk_store8<float>(d, left, v);
 }
-__global__ __launch_bounds__(256) void tk_fill_k(char* __restrict__ p, uint32_t rows, int64_t row_bytes, int64_t ld_bytes) {   // zeros
-  const uint32_t per = (uint32_t)((row_bytes + 15) / 16), all = rows * per;
-  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += gridDim.x * 256) {
-    const uint32_t r = i / per, c = i - r * per;
-    char* const q = p + (int64_t)r * ld_bytes + (int64_t)c * 16;
-    const int64_t left = row_bytes - (int64_t)c * 16;
-    if (left >= 16) tk_st16<float>(reinterpret_cast<float*>(q), u4v_t{0, 0, 0, 0});
-    else
-      for (int64_t b = 0; b < left; b += 4) *reinterpret_cast<float*>(q + b) = 0.f;
-  }
-}
 void tk_fill(hipStream_t st, void* p, int64_t rows, int64_t row_bytes, int64_t ld_bytes) {
-  if (ld_bytes == row_bytes && row_bytes < 65536) {              // rows one behind the other: longer ones
-    int64_t f = std::min<int64_t>(64, rows);
-    while (f > 1 && rows % f) --f;
-    rows /= f; row_bytes *= f; ld_bytes *= f;
-  }
+  long_rows(rows, row_bytes, ld_bytes);
   by_rows(rows, (row_bytes + 15) / 16, [&](int64_t r, int m) {
     hipLaunchKernelGGL(tk_fill_k, dim3(blocks_of((int64_t)m * ((row_bytes + 15) / 16), 8192)), dim3(256), 0, st, (char*)p + r * ld_bytes,
                        (uint32_t)m, row_bytes, ld_bytes);
@@ -328,7 +364,11 @@ void tk_embed_bwd(int dt, hipStream_t st, const void* ids, int ids64, int64_t n6
                   const void* dy, int64_t lddy, float* dtable, int64_t lddt, int accumulate, void* ws) {
   const int es = dt == 1 ? 2 : 4, n = (int)n64;
   KScope ks(st, "tok_embed_bwd", (double)n * width * es + (accumulate ? 0.0 : (double)vocab * width * 4) + 4.0 * n, 2.0 * n * width, n, vocab, width);
-  if (!accumulate) tk_fill(st, dtable, vocab, (int64_t)width * 4, lddt * 4);
+  const bool rank = n > 0 && n <= kRankMost;
+  int64_t zr = vocab, zb = (int64_t)width * 4, zl = lddt * 4;
+  long_rows(zr, zb, zl);
+  const bool beside = rank && zr * ((zb + 15) / 16) < ((int64_t)1 << 31);       // the zeros are written beside the counting
+  if (!accumulate && !beside) tk_fill(st, dtable, vocab, (int64_t)width * 4, lddt * 4);
   if (n == 0) return;
   char* w = (char*)ws;
   uint32_t* buf[4];
@@ -337,12 +377,14 @@ void tk_embed_bwd(int dt, hipStream_t st, const void* ids, int ids64, int64_t n6
   uint32_t* hist = (uint32_t*)w;
   w += up256((size_t)tiles * 256 * 4);
   float* part = (float*)w;
-  const bool rank = n <= kRankMost;
   uint32_t *k0 = buf[0], *p0 = buf[1], *k1 = buf[2], *p1 = buf[3];
   if (ids64) hipLaunchKernelGGL(embed_keys_k<int64_t>, dim3(blocks_of(n, 4096)), dim3(256), 0, st, (const int64_t*)ids, n, vocab, pad_id, k0, rank ? nullptr : p0);
   else hipLaunchKernelGGL(embed_keys_k<int32_t>, dim3(blocks_of(n, 4096)), dim3(256), 0, st, (const int32_t*)ids, n, vocab, pad_id, k0, rank ? nullptr : p0);
   if (rank) {
-    hipLaunchKernelGGL(embed_rank_k, dim3((n + 63) / 64), dim3(256), 0, st, k0, n, k1, p1);
+    const int blocks = (n + 63) / 64;
+    const int64_t vecs = accumulate || !beside ? 0 : zr * ((zb + 15) / 16);
+    const int fill = (int)std::min<int64_t>((vecs + 1023) / 1024, 2048);
+    hipLaunchKernelGGL(embed_rank_k, dim3(blocks + fill), dim3(1024), 0, st, k0, n, k1, p1, blocks, (char*)dtable, (uint32_t)zr, zb, zl);
     k0 = k1; p0 = p1;
   } else {
     // the digits of ids below vocab; no id (all ones) stays behind them because its digits are the largest, where one more bit than the largest id's counts
@@ -473,7 +515,7 @@ void tk_align(int dt, hipStream_t st, const void* x, int64_t ldx, int M, int N, 
 
 // dz = dy * act'(z) and its column sums.  A block has 256 columns (64 threads of four) of a chunk of rows, four threads to a column;
 // the sums are of dz before it is rounded.
-static int dz_rows(int M) { return std::max(32, (M + 255) / 256); }
+static int dz_rows(int M) { return std::max(16, (M + 255) / 256); }
 int tk_dz_chunks(int M) { return M > 0 ? (M + dz_rows(M) - 1) / dz_rows(M) : 0; }
 template <typename E>
 __global__ __launch_bounds__(256) void tk_dz_k(const E* __restrict__ dy, int64_t lddy, const E* __restrict__ z, int64_t ldz, int act, int M, int N,

@@ -68,7 +68,7 @@ struct Call {
   void* part = nullptr;
   size_t part_most = 0;
   void product(int lay, int epi, TgJob* jobs, int n) {
-    TgPlan plan{0, 1};
+    TgPlan plan{128, 1};
     size_t room = 0;
     // the plan of the largest job; all of them have to fit the room with it
     int big = 0;
