@@ -128,62 +128,103 @@ static void long_rows(int64_t& rows, int64_t& row_bytes, int64_t& ld_bytes) {
 // Tokens are sorted by id, equal ids in the order of the tokens; then every kRun of them are one block's: it walks them with a running
 // sum per column and writes a row of the gradient where the id changes.  What an id has in other runs as well goes to memory as partial
 // sums, which embed_join_k adds in the order of the runs.  No atomics: the same tokens give the same bits.
-enum { kRun = 16, kRankMost = 16384, kTile = 4096, kDigit = 8 };
+enum { kRun = 16, kChunk = 8192, kChunksMost = 65536, kTile = 4096, kDigit = 8 };
 #define FTP_NO_ID 0xffffffffu
 
+// an id as the sort sees it: one that is no row's, or whose gradient is left out, behind all others
+__device__ __forceinline__ uint32_t embed_key(int64_t id, int vocab, int64_t pad_id) {
+  return id >= 0 && id < vocab && id != pad_id ? (uint32_t)id : FTP_NO_ID;
+}
 template <typename I>
 __global__ __launch_bounds__(256) void embed_keys_k(const I* __restrict__ ids, int n, int vocab, int64_t pad_id, uint32_t* __restrict__ keys,
                                                     uint32_t* __restrict__ pos) {
   for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
-    const int64_t id = (int64_t)ids[i];
-    keys[i] = id >= 0 && id < vocab && id != pad_id ? (uint32_t)id : FTP_NO_ID;
-    if (pos) pos[i] = (uint32_t)i;
+    keys[i] = embed_key((int64_t)ids[i], vocab, pad_id);
+    pos[i] = (uint32_t)i;
   }
 }
-// Few tokens: a token's place is how many come before it, counted outright: n^2 comparisons, two instructions for 64 of them, no passes
-// that wait for one another.  A block places 64 tokens, its sixteen wavefronts share the ones compared with (they come by scalar loads, whose
-// latency four wavefronts to a SIMD hide: with one 16384 tokens took 85 us).  The blocks from `rank` on write the zeros that a gradient written
-// whole starts from, beside the counting, which leaves the memory alone.
-__global__ __launch_bounds__(1024) void embed_rank_k(const uint32_t* __restrict__ keys, int n, uint32_t* __restrict__ skeys,
-                                                     uint32_t* __restrict__ spos, int rank, char* __restrict__ zero, uint32_t rows, int64_t row_bytes,
-                                                     int64_t ld_bytes) {
+// A token's place among kChunk tokens is how many come before it, counted outright: n^2 comparisons, two instructions for 64 of them, no passes
+// that wait for one another.  A block has the chunk's keys in LDS and places 64 tokens, its sixteen wavefronts share the ones compared with, four to a
+// read that all lanes make together.  The blocks from `rank` on write the zeros that a gradient written whole starts from, beside the counting,
+// which leaves the memory alone.  (Keys by scalar loads, four wavefronts: 16384 tokens at once 85 us; that many beside 262 MB of zeros now 43, the zeros' time.)
+template <typename I>
+__global__ __launch_bounds__(1024) void embed_rank_k(const I* __restrict__ ids, int n, int vocab, int64_t pad_id, uint32_t* __restrict__ skeys,
+                                                     uint32_t* __restrict__ spos, int rank, char* __restrict__ zero, uint32_t rows,
+                                                     int64_t row_bytes, int64_t ld_bytes) {
   constexpr int W = 16;
+  __shared__ __attribute__((aligned(16))) uint32_t key[kChunk];
   __shared__ uint32_t cnt[W][64];
   if ((int)blockIdx.x >= rank) {
     tk_fill_rows<1024>(zero, rows, row_bytes, ld_bytes, blockIdx.x - rank, gridDim.x - rank);
     return;
   }
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int first = blockIdx.x * 64, i = first + lane;
-  const uint32_t k = i < n ? keys[i] : 0;
+  const int first = blockIdx.x * 64, c0 = first / kChunk * kChunk, m = n - c0 < kChunk ? n - c0 : kChunk, at0 = first - c0;   // first: a multiple of 64
+  const int m4 = (m + 3) & ~3;
+  for (int j = threadIdx.x; j < m4; j += 1024) key[j] = j < m ? embed_key((int64_t)ids[c0 + j], vocab, pad_id) : 0xffffffffu;
+  __syncthreads();
+  const int i = at0 + lane;
+  const uint32_t k = i < m ? key[i] : 0;
   uint32_t c = 0;
-  // tokens in front of this block's count where their id is not larger, those behind it where it is smaller
-  const int per = ((n + W - 1) / W + 15) & ~15, j0 = wave * per, j1 = j0 + per < n ? j0 + per : n;
-  const int a1 = j1 < first ? j1 : first;
-  int j = j0;
-  for (; j + 16 <= a1; j += 16) {
-#pragma unroll
-    for (int u = 0; u < 16; ++u) c += keys[j + u] <= k;
+  // tokens in front of this block's count where their id is not larger, those behind it where it is smaller (what pads the last four never is)
+  const int per = (((m4 + W - 1) / W) + 3) & ~3, j0 = wave * per, j1 = j0 + per < m4 ? j0 + per : m4;
+  const int f1 = j1 < at0 ? j1 : at0, b0 = j0 > at0 + 64 ? j0 : at0 + 64;
+#pragma unroll 4
+  for (int j = j0; j < f1; j += 4) {
+    const uint4 q = *reinterpret_cast<const uint4*>(key + j);
+    c += q.x <= k; c += q.y <= k; c += q.z <= k; c += q.w <= k;
   }
-  for (; j < a1; ++j) c += keys[j] <= k;
-  for (; j < j1 && j < first + 64; ++j) c += (keys[j] < k) || (keys[j] == k && j < i);
-  for (; j < j1 && (j & 15); ++j) c += keys[j] < k;
-  for (; j + 16 <= j1; j += 16) {
-#pragma unroll
-    for (int u = 0; u < 16; ++u) c += keys[j + u] < k;
+  for (int j = j0 > at0 ? j0 : at0; j < j1 && j < at0 + 64; ++j) c += key[j] < k || (key[j] == k && j < i);
+#pragma unroll 4
+  for (int j = b0; j < j1; j += 4) {
+    const uint4 q = *reinterpret_cast<const uint4*>(key + j);
+    c += q.x < k; c += q.y < k; c += q.z < k; c += q.w < k;
   }
-  for (; j < j1; ++j) c += keys[j] < k;
   cnt[wave][lane] = c;
   __syncthreads();
-  if (wave == 0 && i < n) {
-    uint32_t at = 0;
+  if (wave == 0 && i < m) {
+    uint32_t at = c0;
 #pragma unroll
     for (int w = 0; w < W; ++w) at += cnt[w][lane];
     skeys[at] = k;
-    spos[at] = (uint32_t)i;
+    spos[at] = (uint32_t)(first + lane);
   }
 }
-// Many tokens: 8 bits of the id at a time, from the lowest.  A block has kTile tokens; counts per block and digit, their running sum over
+// From sorted chunks to one order: a token's place is its own in its chunk and, for every other chunk, how many there come before it (ids not larger in
+// the chunks in front, smaller ones in those behind), by halving, four chunks at a time.
+__global__ __launch_bounds__(256) void embed_merge_k(const uint32_t* __restrict__ keys, const uint32_t* __restrict__ pos, int n,
+                                                     uint32_t* __restrict__ okeys, uint32_t* __restrict__ opos) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  const int own = i / kChunk, chunks = (n + kChunk - 1) / kChunk;
+  const uint32_t k = keys[i];
+  uint32_t at = (uint32_t)(i - own * kChunk);
+  for (int c = 0; c < chunks; c += 4) {
+    int lo[4], size[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int s = (c + u) * kChunk;
+      lo[u] = 0;
+      size[u] = c + u >= chunks || c + u == own ? 0 : n - s < kChunk ? n - s : kChunk;
+    }
+    // how many of the chunk's first `size` count: halves of [lo, lo + size]
+#pragma unroll 1
+    for (int h = kChunk; h > 0; h >>= 1) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int m = lo[u] + h;                                 // do the first m count?  (the m-th decides)
+        const bool in = m <= size[u];
+        const uint32_t x = in ? keys[(c + u) * kChunk + m - 1] : 0;
+        if (in && (c + u < own ? x <= k : x < k)) lo[u] = m;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) at += lo[u];
+  }
+  okeys[at] = k;
+  opos[at] = pos[i];
+}
+// Many tokens (more than 65536: 131072 of width 256 took 215 us in chunks, 188 this way; 32768 72 in chunks, more than 110 this way): 8 bits of the id at a time, from the lowest.  A block has kTile tokens; counts per block and digit, their running sum over
 // (digit, block), then every token goes to its digit's place in its order.
 __global__ __launch_bounds__(256) void embed_count_k(const uint32_t* __restrict__ keys, int n, int shift, uint32_t* __restrict__ hist, int blocks) {
   __shared__ uint32_t h[256];
@@ -250,47 +291,73 @@ __global__ __launch_bounds__(256) void embed_place_k(const uint32_t* __restrict_
   }
 }
 
+// A block has 256 >> shift runs, of 1 << shift threads with eight columns each (wide rows: blockIdx.y).
 template <typename E>
-__global__ __launch_bounds__(256) void embed_sum_k(const uint32_t* __restrict__ skeys, const uint32_t* __restrict__ spos, int n, int width,
+__global__ __launch_bounds__(256) void embed_sum_k(const uint32_t* __restrict__ skeys, const uint32_t* __restrict__ spos, int n, int width, int shift,
                                                    float scale, const E* __restrict__ dy, int64_t lddy, float* __restrict__ dtable,
                                                    int64_t lddt, int accumulate, float* __restrict__ part) {
-  constexpr int U = 8;
-  __shared__ uint32_t key[kRun + 2], pos[kRun];
-  const int tid = threadIdx.x, r0 = blockIdx.x * kRun, cnt = n - r0 < kRun ? n - r0 : kRun;
-  if (tid < kRun + 2) {
-    const int j = r0 + tid - 1;
-    key[tid] = j >= 0 && j < n && tid <= cnt + 1 ? skeys[j] : FTP_NO_ID;
+  constexpr int U = sizeof(E) == 2 ? 16 : 8, K = kRun + 2;
+  extern __shared__ uint32_t held[];                             // per run: the id in front of it, its own, the one behind; then its tokens
+  const int tid = threadIdx.x, R = 256 >> shift, run0 = blockIdx.x * R;
+  uint32_t* const where = held + R * K;
+  for (int t = tid; t < R * K; t += 256) {
+    const int j = (run0 + t / K) * kRun + t % K - 1;
+    held[t] = j >= 0 && j < n ? skeys[j] : FTP_NO_ID;
   }
-  if (tid < kRun) pos[tid] = tid < cnt ? spos[r0 + tid] : 0;
+  for (int t = tid; t < R * kRun; t += 256) {
+    const int j = run0 * kRun + t;
+    where[t] = j < n ? spos[j] : 0;
+  }
   __syncthreads();
-  const int c = (blockIdx.y * 256 + tid) * 8;
-  const int left = width - c;
+  const int sub = tid >> shift, run = run0 + sub, cnt = n - run * kRun < kRun ? n - run * kRun : kRun;
+  const uint32_t *key = held + sub * K, *pos = where + sub * kRun;
+  const int c = (blockIdx.y * 256 + (tid & ((1 << shift) - 1))) * 8, left = width - c;
   if (left <= 0) return;
+  const bool whole = left >= 8;
   float s[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) s[e] = 0.f;
   int start = 0;
   for (int q = 0; q < cnt; q += U) {
     if (key[q + 1] == FTP_NO_ID) return;                         // ids of no row come last
-    float v[U][8];
+    u4v_t raw[U][sizeof(E) == 2 ? 1 : 2];
+    if (whole) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const bool in = q + u < cnt && key[q + u + 1] != FTP_NO_ID;
-      tk_load8<E>(dy + (int64_t)(in ? pos[q + u] : pos[q]) * lddy + c, left, v[u]);
+      for (int u = 0; u < U; ++u) {
+        const bool in = q + u < cnt && key[q + u + 1] != FTP_NO_ID;
+        const E* const p = dy + (int64_t)(in ? pos[q + u] : pos[q]) * lddy + c;
+        raw[u][0] = tk_ld16<E>(p);
+        if (sizeof(E) == 4) raw[u][sizeof(E) == 4] = tk_ld16<E>(p + 4);
+      }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (q + u >= cnt) break;
       const uint32_t k = key[q + u + 1];
       if (k == FTP_NO_ID) break;
+      float v[8];
+      if (whole) {
+        if constexpr (sizeof(E) == 2) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[e] += v[u][e];
+          for (int i = 0; i < 4; ++i) {
+            v[2 * i] = __uint_as_float(raw[u][0][i] << 16);
+            v[2 * i + 1] = __uint_as_float(raw[u][0][i] & 0xffff0000u);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) { v[i] = __uint_as_float(raw[u][0][i]); v[i + 4] = __uint_as_float(raw[u][1][i]); }
+        }
+      } else {
+        tk_load8<E>(dy + (int64_t)pos[q + u] * lddy + c, left, v);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[e] += v[e];
       if (q + u + 1 < cnt && key[q + u + 2] == k) continue;
       // the id's last token in this run
       const bool before = start == 0 && key[0] == k, behind = q + u + 1 == cnt && key[q + u + 2] == k;
       if (before || behind) {
         // [run][0]: of an id that began in an earlier run; [run][1]: of one that begins here and goes on
-        tk_store8<float>(part + ((int64_t)blockIdx.x * 2 + (before ? 0 : 1)) * width + c, left, s);
+        tk_store8<float>(part + ((int64_t)run * 2 + (before ? 0 : 1)) * width + c, left, s);
       } else {
         float* const d = dtable + (int64_t)k * lddt + c;
         float o[8];
@@ -320,18 +387,18 @@ __global__ __launch_bounds__(256) void embed_join_k(const uint32_t* __restrict__
     cnt += ~same ? __builtin_ctzll(~same) : 64;
     if (~same) break;
   }
-  const int c = (blockIdx.y * 256 + threadIdx.x) * 8, left = width - c;
+  const int c = (blockIdx.y * blockDim.x + threadIdx.x) * 8, left = width - c;
   if (left <= 0) return;
   float s[8], v[8];
   tk_load8<float>(part + ((int64_t)run * 2 + 1) * width + c, left, s);
   const float* q = part + (int64_t)(run + 1) * 2 * width + c;
   int r = 0;
-  for (; r + 8 <= cnt; r += 8, q += 16 * (int64_t)width) {
-    float t[8][8];
+  for (; r + 16 <= cnt; r += 16, q += 32 * (int64_t)width) {
+    float t[16][8];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) tk_load8<float>(q + u * 2 * (int64_t)width, left, t[u]);
+    for (int u = 0; u < 16; ++u) tk_load8<float>(q + u * 2 * (int64_t)width, left, t[u]);
 #pragma unroll
-    for (int u = 0; u < 8; ++u)
+    for (int u = 0; u < 16; ++u)
 #pragma unroll
       for (int e = 0; e < 8; ++e) s[e] += t[u][e];
   }
@@ -364,7 +431,8 @@ void tk_embed_bwd(int dt, hipStream_t st, const void* ids, int ids64, int64_t n6
                   const void* dy, int64_t lddy, float* dtable, int64_t lddt, int accumulate, void* ws) {
   const int es = dt == 1 ? 2 : 4, n = (int)n64;
   KScope ks(st, "tok_embed_bwd", (double)n * width * es + (accumulate ? 0.0 : (double)vocab * width * 4) + 4.0 * n, 2.0 * n * width, n, vocab, width);
-  const bool rank = n > 0 && n <= kRankMost;
+  // counting among chunks of the tokens, and merging these, or passes over the ids' digits
+  const bool rank = n > 0 && n <= kChunksMost;
   int64_t zr = vocab, zb = (int64_t)width * 4, zl = lddt * 4;
   long_rows(zr, zb, zl);
   const bool beside = rank && zr * ((zb + 15) / 16) < ((int64_t)1 << 31);       // the zeros are written beside the counting
@@ -378,15 +446,24 @@ void tk_embed_bwd(int dt, hipStream_t st, const void* ids, int ids64, int64_t n6
   w += up256((size_t)tiles * 256 * 4);
   float* part = (float*)w;
   uint32_t *k0 = buf[0], *p0 = buf[1], *k1 = buf[2], *p1 = buf[3];
-  if (ids64) hipLaunchKernelGGL(embed_keys_k<int64_t>, dim3(blocks_of(n, 4096)), dim3(256), 0, st, (const int64_t*)ids, n, vocab, pad_id, k0, rank ? nullptr : p0);
-  else hipLaunchKernelGGL(embed_keys_k<int32_t>, dim3(blocks_of(n, 4096)), dim3(256), 0, st, (const int32_t*)ids, n, vocab, pad_id, k0, rank ? nullptr : p0);
   if (rank) {
     const int blocks = (n + 63) / 64;
     const int64_t vecs = accumulate || !beside ? 0 : zr * ((zb + 15) / 16);
     const int fill = (int)std::min<int64_t>((vecs + 1023) / 1024, 2048);
-    hipLaunchKernelGGL(embed_rank_k, dim3(blocks + fill), dim3(1024), 0, st, k0, n, k1, p1, blocks, (char*)dtable, (uint32_t)zr, zb, zl);
+    auto go = [&](auto k, auto* id) {
+      hipLaunchKernelGGL(k, dim3(blocks + fill), dim3(1024), 0, st, id, n, vocab, pad_id, k1, p1, blocks, (char*)dtable, (uint32_t)zr, zb, zl);
+    };
+    if (ids64) go(embed_rank_k<int64_t>, (const int64_t*)ids);
+    else go(embed_rank_k<int32_t>, (const int32_t*)ids);
+    if (n > kChunk) {
+      hipLaunchKernelGGL(embed_merge_k, dim3((n + 255) / 256), dim3(256), 0, st, k1, p1, n, k0, p0);
+      std::swap(k0, k1);
+      std::swap(p0, p1);
+    }
     k0 = k1; p0 = p1;
   } else {
+    if (ids64) hipLaunchKernelGGL(embed_keys_k<int64_t>, dim3(blocks_of(n, 4096)), dim3(256), 0, st, (const int64_t*)ids, n, vocab, pad_id, k0, p0);
+    else hipLaunchKernelGGL(embed_keys_k<int32_t>, dim3(blocks_of(n, 4096)), dim3(256), 0, st, (const int32_t*)ids, n, vocab, pad_id, k0, p0);
     // the digits of ids below vocab; no id (all ones) stays behind them because its digits are the largest, where one more bit than the largest id's counts
     int bits = 1;
     while (bits < 32 && ((uint64_t)vocab >> bits)) ++bits;
@@ -398,10 +475,13 @@ void tk_embed_bwd(int dt, hipStream_t st, const void* ids, int ids64, int64_t n6
       std::swap(p0, p1);
     }
   }
-  const dim3 g(runs, (width + 2047) / 2048);
-  if (dt == 1) hipLaunchKernelGGL(embed_sum_k<bf16_t>, g, dim3(256), 0, st, k0, p0, n, width, scale, (const bf16_t*)dy, lddy, dtable, lddt, accumulate, part);
-  else hipLaunchKernelGGL(embed_sum_k<float>, g, dim3(256), 0, st, k0, p0, n, width, scale, (const float*)dy, lddy, dtable, lddt, accumulate, part);
-  if (runs > 1) hipLaunchKernelGGL(embed_join_k, g, dim3(256), 0, st, k0, n, width, scale, dtable, lddt, accumulate, part);
+  int shift = 0;
+  while (shift < 8 && (8 << shift) < width) ++shift;
+  const int per = 256 >> shift, slabs = (width + 2047) / 2048, lds = per * (2 * kRun + 2) * 4;
+  const dim3 g((runs + per - 1) / per, slabs);
+  if (dt == 1) hipLaunchKernelGGL(embed_sum_k<bf16_t>, g, dim3(256), lds, st, k0, p0, n, width, shift, scale, (const bf16_t*)dy, lddy, dtable, lddt, accumulate, part);
+  else hipLaunchKernelGGL(embed_sum_k<float>, g, dim3(256), lds, st, k0, p0, n, width, shift, scale, (const float*)dy, lddy, dtable, lddt, accumulate, part);
+  if (runs > 1) hipLaunchKernelGGL(embed_join_k, dim3(runs, slabs), dim3(std::max(64, 1 << shift)), 0, st, k0, n, width, scale, dtable, lddt, accumulate, part);
 }
 
 // ---------------------------------------------------------------- activations in 8 bits

@@ -355,12 +355,13 @@ def test_embed_forward(env, dtype, ids64):
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("accumulate", [0, 1])
 def test_embed_backward(env, dtype, accumulate):
-    """Counting, the passes of the sort, runs of one id over several blocks, ids of no row, an id left out."""
+    """Counting in chunks, merging them, the passes of the sort, runs of one id over several blocks, ids of no row, an id left out; ids of either width."""
     torch, P, R = env
     tdt, code = types(P, torch, dtype)
     sp = torch.cuda.current_stream().cuda_stream
     for rows, vocab, width, kind in ((1, 3, 1, "any"), (63, 7, 9, "any"), (64, 500, 8, "any"), (65, 1, 16, "any"), (1000, 40, 101, "bad"), (700, 9, 2057, "one"),
-                                     (16384, 5000, 8, "any"), (16385, 255, 8, "bad"), (20000, 256, 9, "any"), (30000, 70000, 8, "bad"), (20000, 3, 8, "one")):
+                                     (8192, 5000, 8, "any"), (8193, 255, 8, "bad"), (16384, 5000, 8, "any"), (16385, 255, 8, "bad"), (20000, 256, 9, "any"), (30000, 70000, 8, "bad"), (20000, 3, 8, "one"), (73737, 70000, 8, "bad"),
+                                     (65536, 300, 8, "any"), (65537, 255, 8, "bad"), (140000, 70000, 9, "any"), (150000, 256, 8, "one")):
         print(f"embed backward {dtype} {rows} {vocab} {width} {kind}", flush=True)
         gen = torch.Generator(device="cuda").manual_seed(rows)
         ids = torch.randint(0, vocab, (rows,), generator=gen, device="cuda")
@@ -371,12 +372,14 @@ def test_embed_backward(env, dtype, accumulate):
             ids[::5] = vocab + 3
             ids[3::7] = -4
             ids[2::11] = pad
-        ids = ids.to(torch.int32)
+        ids64 = rows % 2
+        if not ids64:
+            ids = ids.to(torch.int32)
         dy = matrix(torch, gen, rows, width, tdt, 1.0, 3, 1)
         g, ok = out(torch, vocab, width, torch.float32, 2, 1)
         if accumulate:
             g.fill_(0.5)
-        a = P.embed_args(rows=rows, vocab=vocab, width=width, dtype=code, scale=0.75, pad_id=pad, accumulate=accumulate, ids=ids, dy=dy, lddy=dy.stride(0),
+        a = P.embed_args(rows=rows, vocab=vocab, width=width, dtype=code, ids64=ids64, scale=0.75, pad_id=pad, accumulate=accumulate, ids=ids, dy=dy, lddy=dy.stride(0),
                          dtable=g, lddt=g.stride(0))
         ws, ws_ok = given(a, torch, P.embed_backward_workspace(a))
         P.embed_backward(a, sp)
@@ -384,9 +387,11 @@ def test_embed_backward(env, dtype, accumulate):
         ok()
         ws_ok()
         use = (ids >= 0) & (ids < vocab) & (ids != pad)
-        want = torch.zeros(vocab, width, dtype=torch.float64, device="cuda").index_add_(0, ids[use].long(), R.f64(dy)[use])
-        mag = torch.zeros_like(want).index_add_(0, ids[use].long(), R.f64(dy)[use].abs())
-        many = torch.zeros(vocab, dtype=torch.float64, device="cuda").index_add_(0, ids[use].long(), torch.ones(int(use.sum()), dtype=torch.float64, device="cuda"))
+        # on the host: thousands of 64-bit additions to one row take the GPU's atomics seconds
+        at, rows_of = ids[use].long().cpu(), R.f64(dy)[use].cpu()
+        want = torch.zeros(vocab, width, dtype=torch.float64).index_add_(0, at, rows_of).cuda()
+        mag = torch.zeros(vocab, width, dtype=torch.float64).index_add_(0, at, rows_of.abs()).cuda()
+        many = torch.bincount(at, minlength=vocab).double().cuda()
         want, bound = want * 0.75 + 0.5 * accumulate, ((many[:, None] + 2) * mag * 0.75 + 0.5 * accumulate) * R.U + R.U * want.abs()
         R.close(g, want, bound, "dtable")
         if not accumulate:
