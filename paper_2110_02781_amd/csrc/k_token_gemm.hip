@@ -374,24 +374,48 @@ __global__ __launch_bounds__(64 * NW) void tg_skinny_k(const TgJob p) {
       return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, w), __builtin_bit_cast(bf16x8_t, xv), c, 0, 0, 0);
     }
   };
+  // a vector at any element; the row's last may end inside it, and what follows is not the row's
+  auto whole = [&](const char* row, int k) __attribute__((always_inline)) {
+    const u4v_t t = tk_ld16<E>(reinterpret_cast<const E*>(row) + k);
+    return make_uint4(t[0], t[1], t[2], t[3]);
+  };
+  auto ragged = [&](const char* row, int k) __attribute__((always_inline)) {
+    if (k + V <= K) return whole(row, k);
+    uint32_t t[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (k + e < K) {
+        const E* q = reinterpret_cast<const E*>(row) + k + e;
+        if constexpr (F32) t[e & 3] = *reinterpret_cast<const uint32_t*>(q);
+        else t[(e / 2) & 3] |= (uint32_t)*reinterpret_cast<const uint16_t*>(q) << (16 * (e & 1));
+      }
+    return make_uint4(t[0], t[1], t[2], t[3]);
+  };
   const int turn = 4 * U * V;                                   // reduction elements a wavefront takes per turn
-  for (int k0 = wave * turn; k0 < K; k0 += NW * turn) {
+  int k0 = wave * turn;
+  for (; k0 + turn <= K; k0 += NW * turn) {
     uint4 a[U], b[U], c[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int k = k0 + (u * 4 + G) * V;
-      const bool in = k < K;                                    // K is a multiple of V: a vector is inside or outside
-      const int64_t o = (int64_t)(in ? k : 0) * (int64_t)sizeof(E);
-      a[u] = *reinterpret_cast<const uint4*>(w0 + o);
-      if (GLU) b[u] = *reinterpret_cast<const uint4*>(w1 + o);
+      a[u] = whole(w0, k);
+      if (GLU) b[u] = whole(w1, k);
       c[u] = make_uint4(0, 0, 0, 0);
-      if (xin && in) c[u] = *reinterpret_cast<const uint4*>(x + o);
-      if (!in) { a[u] = make_uint4(0, 0, 0, 0); b[u] = a[u]; }
+      if (xin) c[u] = whole(x, k);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       acc[0] = mul(acc[0], a[u], c[u]);
       if (GLU) acc[1] = mul(acc[1], b[u], c[u]);
+    }
+  }
+  if (k0 < K) {
+#pragma unroll 1
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + (u * 4 + G) * V;
+      const uint4 a = ragged(w0, k), c = xin ? ragged(x, k) : make_uint4(0, 0, 0, 0);
+      acc[0] = mul(acc[0], a, c);
+      if (GLU) acc[1] = mul(acc[1], ragged(w1, k), c);
     }
   }
   meet[0][wave][lane] = make_float4(acc[0][0], acc[0][1], acc[0][2], acc[0][3]);

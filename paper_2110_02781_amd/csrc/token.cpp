@@ -53,16 +53,26 @@ struct Call {
   bool dry() const { return !ws.base; }
   int64_t wide(int64_t cols) const { return up_to(cols, dt == FTP_BF16 ? 8 : 4); }
   // The products load 16 bytes at a time: an operand whose rows do not start and end on 16 bytes is copied into rows that do (a
-  // pass over it; a product reads it several times), one in 8 bits is read back into such rows.
-  Mat operand(const void* p, int64_t ld, const uint8_t* scales, int64_t lds, int rows, int cols) {
+  // pass over it; a product reads it several times), one in 8 bits is read back into such rows.  `any`: for the kernel of few rows, which reads
+  // rows as they are.
+  bool as_is(const void* p, int64_t ld, int cols) const { return wide(cols) == cols && (uintptr_t)p % 16 == 0 && wide(ld) == ld; }
+  Mat operand(const void* p, int64_t ld, const uint8_t* scales, int64_t lds, int rows, int cols, bool any = false) {
     const int64_t w = wide(cols);
-    if (!scales && cols == w && (uintptr_t)p % 16 == 0 && wide(ld) == ld) return Mat{p, ld};
+    if (!scales && (any || as_is(p, ld, cols))) return Mat{p, ld};
     void* q = ws.take((size_t)rows * w * esize(dt));
     if (!dry()) {
       if (scales) tk_act8_unpack(dt, st, (const uint8_t*)p, ld, scales, lds, rows, cols, (int)w, q, w);
       else tk_align(dt, st, p, ld, rows, cols, q, w);
     }
     return Mat{q, w};
+  }
+  // Whether the kernel of few rows takes a product of `mats` weight matrices [n][k] (aligned: a tile could read them as they are).  Up to eight rows always.
+  // Beyond them its reads of x, 16 rows for every 16 weight rows, cost more than the empty rows of a tile where the weights are bfloat16 and many: 16 rows, 4096 x 4096
+  // 11.4 us, a tile split by four 14.3; 14336 x 4096 33.4 and 28.0; gate and up of 2048 x 5632 and down 25.3, 21.9; fp32 64 and 69, 20 and 28.  Weights that
+  // a tile needs copied first are streamed: 4096 x 4100 with one row 11 us, with copies 24.
+  bool few(int rows, int n, int k, int mats, bool aligned) const {
+    if (rows > kSkinnyRows) return false;
+    return rows <= 8 || dt == FTP_F32 || !aligned || (double)n * k * mats * 2 <= 40e6;
   }
   // the partial sums' room is the same for all products of a call, which follow one another
   void* part = nullptr;
@@ -166,12 +176,13 @@ int check_linear(const char* who, const ftp_linear_args* a, bool backward) {
 void linear_forward(Call& c, const ftp_linear_args& a) {
   const int rows = (int)a.rows;
   if (rows == 0) return;
-  const Mat x = c.operand(a.x, a.ldx, a.x_scales, a.ldxs, rows, a.n_in), w = c.operand(a.w, a.ldw, nullptr, 0, a.n_out, a.n_in);
+  const bool few = c.few(rows, a.n_out, a.n_in, 1, c.as_is(a.w, a.ldw, a.n_in));
+  const Mat x = c.operand(a.x, a.ldx, a.x_scales, a.ldxs, rows, a.n_in, few), w = c.operand(a.w, a.ldw, nullptr, 0, a.n_out, a.n_in, few);
   const size_t es = esize(a.dtype);
   TgJob j{};
   j.a[0] = x.p; j.lda = x.ld;
   j.b[0] = w.p; j.ldb[0] = w.ld;
-  j.M = rows; j.N = a.n_out; j.K = (int)c.wide(a.n_in); j.nseg = 1;
+  j.M = rows; j.N = a.n_out; j.K = few ? a.n_in : (int)c.wide(a.n_in); j.nseg = 1;
   j.act = a.act;
   j.bias = a.bias;
   j.res = a.residual; j.ldr = a.ldr;
@@ -179,7 +190,7 @@ void linear_forward(Call& c, const ftp_linear_args& a) {
   j.z = a.z; j.ldz = a.ldz;
   j.flags = (fours(a.y, a.ldy, es) ? TG_VEC_OUT : 0) | (fours(a.residual, a.ldr, es) ? TG_VEC_RES : 0) | (fours(a.z, a.ldz, es) ? TG_VEC_Z : 0) |
             ((uintptr_t)a.bias % 16 == 0 ? TG_VEC_BIAS : 0);
-  if (rows <= kSkinnyRows) {
+  if (few) {
     if (!c.dry()) tg_skinny(a.dtype, c.st, TG_LINEAR, j);
   } else {
     c.product(TG_NT, TG_LINEAR, &j, 1);
@@ -285,24 +296,26 @@ void ffn_forward(Call& c, const ftp_ffn_args& a) {
   const size_t es = esize(a.dtype);
   const int64_t fw = c.wide(f);
   void* h = c.ws.take((size_t)rows * fw * es);
-  const Mat x = c.operand(a.x, a.ldx, a.x_scales, a.ldxs, rows, d);
-  const Mat wg = c.operand(a.w_gate, a.ldwg, nullptr, 0, f, d), wu = c.operand(a.w_up, a.ldwu, nullptr, 0, f, d);
-  const Mat wd = c.operand(a.w_down, a.ldwd, nullptr, 0, d, f);
+  // few rows: the weights are streamed as they lie (gate and up kept in 8 bits need a tile, which has whole groups of a row)
+  const bool few = c.few(rows, d, f, 1, c.as_is(a.w_down, a.ldwd, f));
+  const bool few_up = a.save != FTP_SAVE_ACT8 && c.few(rows, f, d, 2, c.as_is(a.w_gate, a.ldwg, d) && c.as_is(a.w_up, a.ldwu, d));
+  const Mat x = c.operand(a.x, a.ldx, a.x_scales, a.ldxs, rows, d, few_up);
+  const Mat wg = c.operand(a.w_gate, a.ldwg, nullptr, 0, f, d, few_up), wu = c.operand(a.w_up, a.ldwu, nullptr, 0, f, d, few_up);
+  const Mat wd = c.operand(a.w_down, a.ldwd, nullptr, 0, d, f, few);
   TgJob j{};
   j.a[0] = x.p; j.lda = x.ld;
   j.b[0] = wg.p; j.ldb[0] = wg.ld;
   j.b[1] = wu.p; j.ldb[1] = wu.ld;
-  j.M = rows; j.N = f; j.K = (int)c.wide(d); j.nseg = 1;
+  j.M = rows; j.N = f; j.K = few_up ? d : (int)c.wide(d); j.nseg = 1;
   j.act = a.act;
   j.out = h; j.ldo = fw;
   kept(j, a);
-  const bool few = rows <= kSkinnyRows;
-  if (!few || a.save == FTP_SAVE_ACT8) c.product(TG_NT, TG_GLU, &j, 1);
+  if (!few_up) c.product(TG_NT, TG_GLU, &j, 1);
   else if (!c.dry()) tg_skinny(a.dtype, c.st, TG_GLU, j);
   TgJob k{};
   k.a[0] = h; k.lda = fw;
   k.b[0] = wd.p; k.ldb[0] = wd.ld;
-  k.M = rows; k.N = d; k.K = (int)fw; k.nseg = 1;
+  k.M = rows; k.N = d; k.K = few ? f : (int)fw; k.nseg = 1;
   k.res = a.residual; k.ldr = a.ldr;
   k.out = a.y; k.ldo = a.ldy;
   k.flags = (fours(a.y, a.ldy, es) ? TG_VEC_OUT : 0) | (fours(a.residual, a.ldr, es) ? TG_VEC_RES : 0);

@@ -6,6 +6,16 @@
 
 namespace ftp {
 
+// 16 or 8 bytes at any element-aligned address as one access
+typedef uint32_t u4v_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u2v_t __attribute__((ext_vector_type(2)));
+template <int A> struct TkAt;
+template <> struct TkAt<1> { typedef u2v_t v8 __attribute__((aligned(1))); };
+template <> struct TkAt<2> { typedef u4v_t v16 __attribute__((aligned(2))); };
+template <> struct TkAt<4> { typedef u4v_t v16 __attribute__((aligned(4))); };
+template <typename E> __device__ __forceinline__ u4v_t tk_ld16(const E* p) { return *reinterpret_cast<const typename TkAt<sizeof(E)>::v16*>(p); }
+template <typename E> __device__ __forceinline__ void tk_st16(E* p, u4v_t v) { *reinterpret_cast<typename TkAt<sizeof(E)>::v16*>(p) = v; }
+
 // 1 / (1 + e^-t): the exponential is the hardware's, 2^x; t = -inf .. inf give 0 .. 1
 __device__ __forceinline__ float sigmoid_f(float t) { return __builtin_amdgcn_rcpf(1.f + __expf(-t)); }
 // GELU in its tanh form: (1 + tanh(s)) / 2 = sigmoid(2 s), s = sqrt(2/pi) (z + 0.044715 z^3).  The square is capped so that

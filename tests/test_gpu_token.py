@@ -299,6 +299,15 @@ def test_ffn_split_reduction(env):
     ffn_case(env, "bf16", "silu", 2, 5, 2048, 64, 0, 0)
 
 
+def test_few_rows_and_many_weights(env):
+    """From nine rows on, aligned weights of 40 MB and more go through a tile; fewer, and those of odd rows, are streamed."""
+    torch, P, R = env
+    for rows, k, n in ((8, 4608, 4608), (9, 4608, 4608), (16, 4608, 4608), (16, 4608, 4000), (16, 4607, 4608)):
+        linear_case(env, "bf16", "none", rows, k, n, 0, 0)
+    ffn_case(env, "bf16", "silu", 1, 12, 2048, 5632, 0, 0)
+    ffn_case(env, "bf16", "silu", 1, 12, 2047, 5631, 0, 0)
+
+
 def test_ffn_options(env):
     ffn_case(env, "bf16", "silu", 2, 90, 64, 100, 0, 0, grad="f32", accumulate=1, dx_residual=0)
     ffn_case(env, "f32", "silu", 1, 90, 64, 100, 0, 0, accumulate=1)

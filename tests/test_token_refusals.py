@@ -120,14 +120,15 @@ def test_null_records(P):
 
 
 def test_workspaces(P):
-    """Aligned operands need none for their copies; what a call names is what it asks for."""
-    assert P.linear_workspace(linear(P, rows=4, n_in=64, n_out=64, ldx=64, ldw=64, ldy=64, ldz=64)) == 0
-    odd = linear(P, rows=4, n_in=15, n_out=8, ldx=16, ldw=16)
+    """Aligned operands need none for their copies, nor do those of few rows; what a call names is what it asks for."""
+    assert P.linear_workspace(linear(P, rows=40, n_in=64, n_out=64, ldx=64, ldw=64, ldy=64, ldz=64)) == 0
+    assert P.linear_workspace(linear(P, rows=4, n_in=15, n_out=8, x=AT + 2, ldx=17, ldw=15)) == 0
+    odd = linear(P, rows=40, n_in=15, n_out=8, ldx=16, ldw=16)
     n = P.linear_workspace(odd)
-    assert n >= (4 + 8) * 16 * 2
+    assert n >= (40 + 8) * 16 * 2
     refused(P, P.linear_forward, odd)
     for off in (dict(x=AT + 2), dict(ldx=17, n_in=16)):                             # an offset, rows of an odd distance
-        assert P.linear_workspace(linear(P, **off)) >= 4 * 16 * 2
+        assert P.linear_workspace(linear(P, rows=40, **off)) >= 40 * 16 * 2
     f = ffn(P)
     n = P.ffn_workspace(f, True)
     assert n >= 3 * 4 * 40 * 2
