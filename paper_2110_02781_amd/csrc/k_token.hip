@@ -550,14 +550,17 @@ void tk_act8_unpack(int dt, hipStream_t st, const uint8_t* q, int64_t ldq, const
 }
 
 // ---------------------------------------------------------------- linear layers
+// All copies of a call go as one launch, blockIdx.y a matrix: 1000 x 1001, fp32, takes 5 us, of which the bytes are 2.
+struct AlignGroup { TkCopy j[kCopies]; };
 template <typename E>
-__global__ __launch_bounds__(256) void tk_align_k(const E* __restrict__ x, int64_t ldx, int rows, int N, E* __restrict__ y, int64_t ldy) {
+__global__ __launch_bounds__(256) void tk_align_k(AlignGroup g) {
   constexpr int V = 16 / sizeof(E);
-  const uint32_t per = (uint32_t)(ldy / V), all = (uint32_t)rows * per;
+  const TkCopy& j = g.j[blockIdx.y];
+  const uint32_t per = (uint32_t)(j.ldy / V), all = (uint32_t)j.rows * per;
   for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += gridDim.x * 256) {
     const uint32_t r = i / per, c = (i - r * per) * V;
-    const E* const p = x + (int64_t)r * ldx + c;
-    const int left = N - (int)c;
+    const E* const p = (const E*)j.x + (int64_t)r * j.ldx + c;
+    const int left = j.cols - (int)c;
     u4v_t t = {0, 0, 0, 0};
     if (left >= V) {
       t = tk_ld16<E>(p);
@@ -570,17 +573,39 @@ __global__ __launch_bounds__(256) void tk_align_k(const E* __restrict__ x, int64
         else t[e / 2] |= b << (16 * (e & 1));
       }
     }
-    *reinterpret_cast<u4v_t*>(y + (int64_t)r * ldy + c) = t;
+    *reinterpret_cast<u4v_t*>((E*)j.y + (int64_t)r * j.ldy + c) = t;
   }
 }
-void tk_align(int dt, hipStream_t st, const void* x, int64_t ldx, int M, int N, void* y, int64_t ldy) {
-  KScope ks(st, "tok_align", 2.0 * M * N * (dt == 1 ? 2 : 4), 0, M, N);
-  const int64_t per = ldy / (dt == 1 ? 8 : 4);
-  by_rows(M, per, [&](int64_t r, int m) {
-    const unsigned b = blocks_of(m * per, 1 << 20);
-    if (dt == 1) hipLaunchKernelGGL(tk_align_k<bf16_t>, dim3(b), dim3(256), 0, st, (const bf16_t*)x + r * ldx, ldx, m, N, (bf16_t*)y + r * ldy, ldy);
-    else hipLaunchKernelGGL(tk_align_k<float>, dim3(b), dim3(256), 0, st, (const float*)x + r * ldx, ldx, m, N, (float*)y + r * ldy, ldy);
-  });
+void tk_align(int dt, hipStream_t st, const TkCopy* jobs, int n) {
+  const int es = dt == 1 ? 2 : 4;
+  double elements = 0;
+  for (int i = 0; i < n; ++i) elements += (double)jobs[i].rows * jobs[i].cols;
+  KScope ks(st, "tok_align", 2.0 * elements * es, 0, n, jobs[0].rows, jobs[0].cols);
+  auto go = [&](const AlignGroup& g, int m, int64_t most) {
+    const dim3 b(blocks_of(most, 1 << 20), m);
+    if (dt == 1) hipLaunchKernelGGL(tk_align_k<bf16_t>, b, dim3(256), 0, st, g);
+    else hipLaunchKernelGGL(tk_align_k<float>, b, dim3(256), 0, st, g);
+  };
+  AlignGroup g{};
+  int m = 0;
+  int64_t most = 0;
+  for (int i = 0; i < n; ++i) {
+    const int64_t per = jobs[i].ldy * es / 16, all = jobs[i].rows * per;
+    if (all <= (int64_t)1 << 30) {
+      g.j[m++] = jobs[i];
+      most = std::max(most, all);
+      continue;
+    }
+    by_rows(jobs[i].rows, per, [&](int64_t r, int rows) {
+      AlignGroup one{};
+      one.j[0] = jobs[i];
+      one.j[0].x = (const char*)jobs[i].x + r * jobs[i].ldx * es;
+      one.j[0].y = (char*)jobs[i].y + r * jobs[i].ldy * es;
+      one.j[0].rows = rows;
+      go(one, 1, rows * per);
+    });
+  }
+  if (m) go(g, m, most);
 }
 
 // dz = dy * act'(z) and its column sums.  A block has 256 columns (64 threads of four) of a chunk of rows, four threads to a column;

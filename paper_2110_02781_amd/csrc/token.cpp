@@ -52,19 +52,27 @@ struct Call {
   Space ws;
   bool dry() const { return !ws.base; }
   int64_t wide(int64_t cols) const { return up_to(cols, dt == FTP_BF16 ? 8 : 4); }
-  // The products load 16 bytes at a time: an operand whose rows do not start and end on 16 bytes is copied into rows that do (a
-  // pass over it; a product reads it several times), one in 8 bits is read back into such rows.  `any`: for the kernel of few rows, which reads
-  // rows as they are.
-  bool as_is(const void* p, int64_t ld, int cols) const { return wide(cols) == cols && (uintptr_t)p % 16 == 0 && wide(ld) == ld; }
+  // The products load 16 bytes at a time, from any multiple of 4: an operand whose rows have another length, or start elsewhere, is copied into rows
+  // that do (a pass over it; a product reads it several times), one in 8 bits is read back into such rows.  Rows off the 16 bytes are better read where
+  // they lie, also by large products: x [8192][4096 of 4098], bfloat16, against 4096 weight rows 268 us, copied 276, on 16 bytes 251; against 512
+  // weight rows 62 and 98.  `any`: for the kernel of few rows, which reads rows as they are.  copied() launches the copies that the operands so far need, all at once.
+  bool as_is(const void* p, int64_t ld, int cols) const { return wide(cols) == cols && (uintptr_t)p % 4 == 0 && ld * (int64_t)esize(dt) % 4 == 0; }
+  TkCopy copies[kCopies];
+  int ncopies = 0;
   Mat operand(const void* p, int64_t ld, const uint8_t* scales, int64_t lds, int rows, int cols, bool any = false) {
     const int64_t w = wide(cols);
     if (!scales && (any || as_is(p, ld, cols))) return Mat{p, ld};
     void* q = ws.take((size_t)rows * w * esize(dt));
-    if (!dry()) {
-      if (scales) tk_act8_unpack(dt, st, (const uint8_t*)p, ld, scales, lds, rows, cols, (int)w, q, w);
-      else tk_align(dt, st, p, ld, rows, cols, q, w);
+    if (scales) {
+      if (!dry()) tk_act8_unpack(dt, st, (const uint8_t*)p, ld, scales, lds, rows, cols, (int)w, q, w);
+    } else {
+      copies[ncopies++] = TkCopy{p, ld, q, w, rows, cols};
     }
     return Mat{q, w};
+  }
+  void copied() {
+    if (ncopies && !dry()) tk_align(dt, st, copies, ncopies);
+    ncopies = 0;
   }
   // Whether the kernel of few rows takes a product of `mats` weight matrices [n][k] (aligned: a tile could read them as they are).  Up to eight rows always.
   // Beyond them its reads of x, 16 rows for every 16 weight rows, cost more than the empty rows of a tile where the weights are bfloat16 and many: 16 rows, 4096 x 4096
@@ -178,6 +186,7 @@ void linear_forward(Call& c, const ftp_linear_args& a) {
   if (rows == 0) return;
   const bool few = c.few(rows, a.n_out, a.n_in, 1, c.as_is(a.w, a.ldw, a.n_in));
   const Mat x = c.operand(a.x, a.ldx, a.x_scales, a.ldxs, rows, a.n_in, few), w = c.operand(a.w, a.ldw, nullptr, 0, a.n_out, a.n_in, few);
+  c.copied();
   const size_t es = esize(a.dtype);
   TgJob j{};
   j.a[0] = x.p; j.lda = x.ld;
@@ -221,9 +230,12 @@ void linear_backward(Call& c, const ftp_linear_args& a) {
     if (a.dbias && !c.dry()) tk_dz(a.dtype, c.st, a.dy, a.lddy, a.z, a.ldz, a.act, rows, n, nullptr, 0, sums);
     if (a.dx || a.dw) dz = c.operand(a.dy, a.lddy, nullptr, 0, rows, n);
   }
+  Mat w{}, x{};
+  if (a.dx) w = c.operand(a.w, a.ldw, nullptr, 0, n, k);
+  if (a.dw) x = c.operand(a.x, a.ldx, a.x_scales, a.ldxs, rows, k);
+  c.copied();
   if (a.dbias && !c.dry()) tk_colsum_join(c.st, sums, chunks, n, a.dbias, a.grad_dtype, a.accumulate);
   if (a.dx) {
-    const Mat w = c.operand(a.w, a.ldw, nullptr, 0, n, k);
     TgJob j{};
     j.a[0] = dz.p; j.lda = dz.ld;
     j.b[0] = w.p; j.ldb[0] = w.ld;
@@ -233,7 +245,6 @@ void linear_backward(Call& c, const ftp_linear_args& a) {
     c.product(TG_NN, TG_LINEAR, &j, 1);
   }
   if (a.dw) {
-    const Mat x = c.operand(a.x, a.ldx, a.x_scales, a.ldxs, rows, k);
     TgJob j{};
     j.a[0] = dz.p; j.lda = dz.ld;
     j.b[0] = x.p; j.ldb[0] = x.ld;
@@ -302,6 +313,7 @@ void ffn_forward(Call& c, const ftp_ffn_args& a) {
   const Mat x = c.operand(a.x, a.ldx, a.x_scales, a.ldxs, rows, d, few_up);
   const Mat wg = c.operand(a.w_gate, a.ldwg, nullptr, 0, f, d, few_up), wu = c.operand(a.w_up, a.ldwu, nullptr, 0, f, d, few_up);
   const Mat wd = c.operand(a.w_down, a.ldwd, nullptr, 0, d, f, few);
+  c.copied();
   TgJob j{};
   j.a[0] = x.p; j.lda = x.ld;
   j.b[0] = wg.p; j.ldb[0] = wg.ld;
@@ -335,6 +347,13 @@ void ffn_backward(Call& c, const ftp_ffn_args& a) {
   const int64_t fw = c.wide(f);
   void *dg = c.ws.take((size_t)rows * fw * es), *du = c.ws.take((size_t)rows * fw * es), *h = c.ws.take((size_t)rows * fw * es);
   const Mat dy = c.operand(a.dy, a.lddy, nullptr, 0, rows, d), wd = c.operand(a.w_down, a.ldwd, nullptr, 0, d, f);
+  Mat wg{}, wu{}, x{};
+  if (a.dx) {
+    wg = c.operand(a.w_gate, a.ldwg, nullptr, 0, f, d);
+    wu = c.operand(a.w_up, a.ldwu, nullptr, 0, f, d);
+  }
+  if (a.dw_gate) x = c.operand(a.x, a.ldx, a.x_scales, a.ldxs, rows, d);
+  c.copied();
   TgJob j{};
   j.a[0] = dy.p; j.lda = dy.ld;
   j.b[0] = wd.p; j.ldb[0] = wd.ld;
@@ -345,7 +364,6 @@ void ffn_backward(Call& c, const ftp_ffn_args& a) {
   j.dgate = dg; j.dup = du; j.ldd = fw;
   c.product(TG_NN, TG_GLUBWD, &j, 1);
   if (a.dx) {
-    const Mat wg = c.operand(a.w_gate, a.ldwg, nullptr, 0, f, d), wu = c.operand(a.w_up, a.ldwu, nullptr, 0, f, d);
     TgJob k{};
     k.a[0] = dg; k.a[1] = du; k.lda = fw;
     k.b[0] = wg.p; k.ldb[0] = wg.ld;
@@ -357,7 +375,6 @@ void ffn_backward(Call& c, const ftp_ffn_args& a) {
     c.product(TG_NN, TG_LINEAR, &k, 1);
   }
   if (a.dw_gate) {
-    const Mat x = c.operand(a.x, a.ldx, a.x_scales, a.ldxs, rows, d);
     TgJob k[3] = {};
     const void* left[3] = {dg, du, dy.p};
     const Mat right[3] = {x, x, Mat{h, fw}};

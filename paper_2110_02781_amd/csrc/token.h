@@ -56,8 +56,10 @@ int tk_dz_chunks(int M);
 void tk_dz(int dt, hipStream_t st, const void* dy, int64_t lddy, const void* z, int64_t ldz, int act, int M, int N, void* dz,
            int64_t ldd, float* part);
 void tk_colsum_join(hipStream_t st, const float* part, int chunks, int N, void* db, int out_dt, int accumulate);
-// copy into rows of a length that is a multiple of 16 bytes, the rest of a row zero
-void tk_align(int dt, hipStream_t st, const void* x, int64_t ldx, int M, int N, void* y, int64_t ldy);
+// copies of rows into rows (16-byte aligned) of ldy elements, a multiple of 16 bytes, the rest of a row zero; up to kCopies of them
+enum { kCopies = 5 };
+struct TkCopy { const void* x; int64_t ldx; void* y; int64_t ldy; int rows, cols; };
+void tk_align(int dt, hipStream_t st, const TkCopy* jobs, int n);
 void tk_act8_pack(int dt, hipStream_t st, const void* x, int64_t ldx, int64_t M, int N, uint8_t* q, int64_t ldq, uint8_t* s, int64_t lds);
 void tk_act8_unpack(int dt, hipStream_t st, const uint8_t* q, int64_t ldq, const uint8_t* s, int64_t lds, int64_t M, int N, int pad_to,
                     void* y, int64_t ldy);

@@ -3,8 +3,8 @@
 // out[m][n] = sum_k A(m,k) B(n,k).  A and B lie in memory with the reduction along their rows (x, the forward's weights) or across
 // them (the weights in a data gradient, both operands of a weight gradient); neither is repacked:
 //   * a block owns BM x BN of the result and walks the reduction in steps of 128 bytes of a row (64 bfloat16, 32 fp32).  Both
-//     operands' parts of a step go from memory straight into one of two LDS buffers (buffer loads that write LDS: no registers,
-//     no LDS-write instructions), while the other buffer is multiplied;
+//     operands' parts of a step go from memory straight into LDS (buffer loads that write it: no registers, no LDS-write
+//     instructions), while an earlier step's is multiplied: two buffers, three for tiles of 64, five half ones for the large tile;
 //   * such a load puts its 64 lanes' vectors one behind the other, so the order that keeps LDS reads free of bank conflicts is made
 //     by which vector each lane asks for: 16-byte vector c of row r lies at place c ^ (r & 7) (reduction along the row), or 32-byte
 //     unit p of reduction row r at p ^ g(r) (across; g: the low two bits of r and its bit 3, as many as there are units), where it is read by the LDS transpose read (fp32: word by word);
@@ -87,10 +87,7 @@ __device__ __forceinline__ void tg_tile(int t, int tm, int tn, int& it, int& jt)
 }
 
 // LDS buffers of the small tiles: with a CU to itself a block of 64 x 64 multiplies for half the time that its operands take to come
-#ifndef NB64
-#define NB64 3
-#endif
-constexpr int tg_buffers(int bm) { return bm == 64 ? NB64 : 2; }
+constexpr int tg_buffers(int bm) { return bm == 64 ? 3 : 2; }
 
 // what a block does: its job, tile and steps of the reduction, and the loading of a step
 template <typename E, int LAY, int EPI, int BM, int BN, int NW>

@@ -159,6 +159,25 @@ def test_linear_large_tile(env, rows, k, n, slack, skip):
     assert took == {"tok_linear": {"256"}, "tok_wgrad": {"256"}}, took
 
 
+# rows of whole vectors that start on 4 bytes but not on 16: read as they lie, in every product and tile
+FOUR = [("bf16", 130, 136, 264, 2, 2), ("bf16", 300, 328, 200, 6, 4), ("bf16", 70, 4096, 40, 2, 6), ("f32", 130, 132, 260, 1, 1), ("f32", 301, 332, 204, 3, 2),
+        ("f32", 70, 2048, 40, 5, 3), ("bf16", 33, 64, 8, 2, 2)]
+
+
+@pytest.mark.parametrize("dtype,rows,k,n,slack,skip", FOUR)
+def test_rows_on_four_bytes(env, dtype, rows, k, n, slack, skip):
+    linear_case(env, dtype, "silu", rows, k, n, slack, skip)
+    ffn_case(env, dtype, "silu", 1, rows, k, n, slack, skip)
+
+
+@pytest.mark.parametrize("slack,skip", [(2, 2), (6, 4)])
+def test_rows_on_four_bytes_large_tile(env, slack, skip):
+    with routes(env[1]) as took:
+        linear_case(env, "bf16", "silu", 4090, 4088, 4072, slack, skip)
+        ffn_case(env, "bf16", "silu", 2, 4090, 4088, 4096, slack, skip)
+    assert took == {k: {"256"} for k in ("tok_glu", "tok_glu_bwd", "tok_linear", "tok_wgrad")}, took
+
+
 @pytest.mark.parametrize("accumulate", [0, 1])
 def test_linear_fp32_gradients(env, accumulate):
     linear_case(env, "bf16", "none", 200, 120, 90, 0, 0, grad="f32", accumulate=accumulate)
