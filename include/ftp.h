@@ -321,7 +321,7 @@ int ftp_stage_copy_units(ftp_stage* dst, const ftp_stage* src, int unit_lo, int 
  * and options (zero it first: a NULL pointer or 0 is "not wanted"); the caller keeps it for as long as its buffers live.
  *   - Matrices are row-major; ld... is the distance between rows in elements (bytes for 8-bit forms), at least the
  *     row's length, at most 2^20.  Pointers are aligned to their elements; sizes, strides and offsets are otherwise
- *     free, but an operand whose rows do not start on 4 bytes, or are no multiple of 16 long, is first copied into the workspace.
+ *     free, but an operand whose rows do not start on 4 bytes, or are not a multiple of 16 bytes long, is first copied into ws.
  *   - `rows` counts tokens, 0 .. 2^30; with 0 a forward does nothing and a backward writes zero gradients
  *     (accumulate: leaves them).
  *   - `dtype` is the type of activations, their gradients and the weights.  Sums, activations and scales are fp32;

@@ -281,7 +281,9 @@ __global__ __launch_bounds__(256) void embed_place_k(const uint32_t* __restrict_
   }
 }
 
-// A block has 256 >> shift runs, of 1 << shift threads with eight columns each (wide rows: blockIdx.y).
+// A block has 256 >> shift runs, of 1 << shift threads with eight columns each (wide rows: blockIdx.y).  16384 tokens of 2048 columns, 32000 rows:
+// 36 us for 172 MB, a copy's rate.  Zeros only for the rows that no token has, written beside the sums, move 105 MB less, but counting has nothing
+// beside it then: 18 and 65 us instead of 45 (with the zeros) and 36.
 template <typename E>
 __global__ __launch_bounds__(256) void embed_sum_k(const uint32_t* __restrict__ skeys, const uint32_t* __restrict__ spos, int n, int width, int shift,
                                                    float scale, const E* __restrict__ dy, int64_t lddy, float* __restrict__ dtable,

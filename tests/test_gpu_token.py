@@ -430,6 +430,35 @@ def test_embed_backward(env, dtype, accumulate):
             assert torch.equal(again, g)
 
 
+@pytest.mark.parametrize("rows,vocab,width", [(1, 5000, 1), (40, 5000, 1), (300, 200, 2100), (3, 40, 70000), (9000, 3000, 7), (70000, 3000, 3), (64, 64, 1024),
+                                              (500, 1025, 64), (4097, 4096, 33)])
+def test_embed_backward_rows_without_tokens(env, rows, vocab, width):
+    """Whole numbers, so that sums are exact: rows with tokens hold their sum, all others zeros, whatever the gradient held."""
+    torch, P, R = env
+    sp = torch.cuda.current_stream().cuda_stream
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    for kind in range(4):
+        print(f"rows without tokens {rows} {vocab} {width} {kind}", flush=True)
+        ids = torch.randint(0, vocab, (rows,), generator=gen, device="cuda")
+        if kind == 1:
+            ids = ids // 2                                       # none in the upper half
+        elif kind == 2:
+            ids = ids * 0 + (vocab - 1)
+        elif kind == 3:
+            ids = ids * 0 + vocab                                # none at all
+        dy = torch.randint(-4, 5, (rows, width), generator=gen, device="cuda").to(torch.bfloat16)
+        g, ok = out(torch, vocab, width, torch.float32, 3, 1)
+        a = P.embed_args(rows=rows, vocab=vocab, width=width, dtype=P.BF16, ids64=1, scale=1.0, pad_id=-1, ids=ids, dy=dy, lddy=width, dtable=g, lddt=g.stride(0))
+        ws, ws_ok = given(a, torch, P.embed_backward_workspace(a))
+        P.embed_backward(a, sp)
+        torch.cuda.synchronize()
+        ok()
+        ws_ok()
+        use = ids < vocab
+        want = torch.zeros(vocab, width).index_add_(0, ids[use].cpu(), dy[use].cpu().float())
+        assert torch.equal(g.cpu(), want)
+
+
 # ---- 8 bits ----------------------------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_act8(env, dtype):
