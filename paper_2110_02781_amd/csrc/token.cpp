@@ -92,7 +92,7 @@ struct Call {
     int big = 0;
     for (int i = 1; i < n; ++i)
       if ((double)jobs[i].M * jobs[i].N > (double)jobs[big].M * jobs[big].N) big = i;
-    plan = tg_plan(dt, lay, epi, jobs[big].M, jobs[big].N * n, jobs[big].K * jobs[big].nseg, kPartBytes);
+    plan = tg_plan(dt, epi, jobs[big].M, jobs[big].N * n, jobs[big].K * jobs[big].nseg, kPartBytes);
     for (int i = 0; i < n; ++i) room += (size_t)up_to((int64_t)tg_part_bytes(epi, jobs[i].M, jobs[i].N, plan.splits), 256);
     part_most = std::max(part_most, room);
     if (dry()) return;

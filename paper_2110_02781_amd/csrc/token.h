@@ -42,7 +42,7 @@ enum { TG_VEC_OUT = 1, TG_VEC_RES = 2, TG_VEC_Z = 4, TG_VEC_BIAS = 8 };   // fou
 
 struct TgPlan { int tile, splits; };     // tile: 256, 128 or 64 rows and columns
 // tile and split of one job's reduction; max_bytes: workspace that its partial sums may take
-TgPlan tg_plan(int dt, int lay, int epi, int M, int N, int K, size_t max_bytes);
+TgPlan tg_plan(int dt, int epi, int M, int N, int K, size_t max_bytes);
 size_t tg_part_bytes(int epi, int M, int N, int splits);
 // jobs [0, n): n up to 3, all with the same plan (TG_GRAD), otherwise 1
 void tg_launch(int dt, hipStream_t st, int lay, int epi, TgJob* jobs, int n, TgPlan plan);
