@@ -23,36 +23,41 @@ __device__ __forceinline__ float sigmoid_f(float t) { return __builtin_amdgcn_rc
 #define FTP_GELU_2K 1.5957691216057308f
 #define FTP_GELU_C 0.044715f
 
-__device__ __forceinline__ void tact4(float v[4], int act) {
+// K values at a time: which activation it is costs a chain of branches, 20 cycles a value if asked for every four
+template <int K>
+__device__ __forceinline__ void tactn(float* v, int act) {
   if (act == TACT_SILU) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] *= sigmoid_f(v[e]);
+    for (int e = 0; e < K; ++e) v[e] *= sigmoid_f(v[e]);
   } else if (act == TACT_GELU) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < K; ++e) {
       const float z = v[e], z2 = fminf(z * z, 1e6f);
       v[e] = z * sigmoid_f(FTP_GELU_2K * z * fmaf(FTP_GELU_C, z2, 1.f));
     }
   } else if (act != TACT_NONE) {                 // comparisons, so that NaN stays NaN
+    const float top = act == TACT_RELU6 ? 6.f : __uint_as_float(0x7f800000u);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < K; ++e) {
       v[e] = v[e] < 0.f ? 0.f : v[e];
-      if (act == TACT_RELU6) v[e] = v[e] > 6.f ? 6.f : v[e];
+      v[e] = v[e] > top ? top : v[e];
     }
   }
 }
+__device__ __forceinline__ void tact4(float v[4], int act) { tactn<4>(v, act); }
 // a <- act(z), d <- act'(z)
-__device__ __forceinline__ void tact_grad4(const float z[4], float a[4], float d[4], int act) {
+template <int K>
+__device__ __forceinline__ void tact_gradn(const float* z, float* a, float* d, int act) {
   if (act == TACT_SILU) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < K; ++e) {
       const float p = sigmoid_f(z[e]);
       a[e] = z[e] * p;
       d[e] = fmaf(a[e], 1.f - p, p);
     }
   } else if (act == TACT_GELU) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < K; ++e) {
       const float z2 = fminf(z[e] * z[e], 1e6f);
       const float p = sigmoid_f(FTP_GELU_2K * z[e] * fmaf(FTP_GELU_C, z2, 1.f));
       a[e] = z[e] * p;
@@ -60,7 +65,7 @@ __device__ __forceinline__ void tact_grad4(const float z[4], float a[4], float d
     }
   } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < K; ++e) {
       a[e] = z[e];
       d[e] = 1.f;
       if (act != TACT_NONE) {
@@ -71,6 +76,7 @@ __device__ __forceinline__ void tact_grad4(const float z[4], float a[4], float d
     }
   }
 }
+__device__ __forceinline__ void tact_grad4(const float z[4], float a[4], float d[4], int act) { tact_gradn<4>(z, a, d, act); }
 
 // ---- four consecutive columns n .. n+3 of a row of N; `vec`: the row's fours are aligned; F: known to be, and inside ----
 template <typename E, bool F = false>
@@ -208,30 +214,42 @@ template <typename E, bool F> struct TgSide<E, TG_GLUBWD, F> {
       u = get_raw4<E, F>(p.up, p.ldu, r, n, p.N, vec);
     }
   }
-  __device__ __forceinline__ void finish(const TgJob& p, int64_t m, int n, const float dh[4]) const {
-    float gv[4], uv[4];
+  __device__ __forceinline__ void finish(const TgJob& p, int64_t m, int n, const float dh[4]) const { finish_rows<1>(this, p, m, n, dh); }
+  // K rows, two apart
+  template <int K>
+  static __device__ __forceinline__ void finish_rows(const TgSide* side, const TgJob& p, int64_t m, int n, const float* dh) {
+    float gv[4 * K], uv[4 * K];
     if (p.save == 2) {
-      uint32_t q[4];
-      __builtin_memcpy(q, &g, 8);
-      __builtin_memcpy(q + 2, &u, 8);
-      act8_unpack4(q[0], act8_mul(q[1]), gv);
-      act8_unpack4(q[2], act8_mul(q[3]), uv);
-    } else {
-      open4<E>(g, gv);
-      open4<E>(u, uv);
-    }
-    float a[4], d[4], dg[4], du[4];
-    tact_grad4(gv, a, d, p.act);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+      for (int k = 0; k < K; ++k) {
+        uint32_t q[4];
+        __builtin_memcpy(q, &side[k].g, 8);
+        __builtin_memcpy(q + 2, &side[k].u, 8);
+        act8_unpack4(q[0], act8_mul(q[1]), gv + 4 * k);
+        act8_unpack4(q[2], act8_mul(q[3]), uv + 4 * k);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        open4<E>(side[k].g, gv + 4 * k);
+        open4<E>(side[k].u, uv + 4 * k);
+      }
+    }
+    float a[4 * K], d[4 * K], dg[4 * K], du[4 * K];
+    tact_gradn<4 * K>(gv, a, d, p.act);
+#pragma unroll
+    for (int e = 0; e < 4 * K; ++e) {
       dg[e] = dh[e] * uv[e] * d[e];
       du[e] = dh[e] * a[e];
       a[e] *= uv[e];
     }
     // rounded to the type of the products that follow, as their operands
-    put4<E, F>(p.dgate, p.ldd, m, n, (int)p.ldd, true, dg);
-    put4<E, F>(p.dup, p.ldd, m, n, (int)p.ldd, true, du);
-    put4<E, F>(p.out, p.ldo, m, n, (int)p.ldo, true, a);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      put4<E, F>(p.dgate, p.ldd, m + 2 * k, n, (int)p.ldd, true, dg + 4 * k);
+      put4<E, F>(p.dup, p.ldd, m + 2 * k, n, (int)p.ldd, true, du + 4 * k);
+      put4<E, F>(p.out, p.ldo, m + 2 * k, n, (int)p.ldo, true, a + 4 * k);
+    }
   }
 };
 

@@ -178,6 +178,19 @@ def test_rows_on_four_bytes_large_tile(env, slack, skip):
     assert took == {k: {"256"} for k in ("tok_glu", "tok_glu_bwd", "tok_linear", "tok_wgrad")}, took
 
 
+@pytest.mark.parametrize("act", ["none", "relu", "relu6", "silu", "gelu"])
+def test_large_tile_epilogues(env, act):
+    """Every activation behind whole large tiles, with and without bias and residual, both stashes; the last tiles are partly outside."""
+    for bias, res in ((True, True), (True, False), (False, True), (False, False)):
+        with routes(env[1]) as took:
+            linear_case(env, "bf16", act, 4360, 72, 4104, 0, 0, bias=bias, res=res)
+        assert "256" in took["tok_linear"], took
+    for save in (0, 1, 2):
+        with routes(env[1]) as took:
+            ffn_case(env, "bf16", act, save, 4360, 72, 4104, 0, 0)
+        assert "256" in took["tok_glu"] and (save == 0 or "256" in took["tok_glu_bwd"]), took
+
+
 @pytest.mark.parametrize("accumulate", [0, 1])
 def test_linear_fp32_gradients(env, accumulate):
     linear_case(env, "bf16", "none", 200, 120, 90, 0, 0, grad="f32", accumulate=accumulate)
