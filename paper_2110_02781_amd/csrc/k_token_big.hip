@@ -34,17 +34,18 @@ __device__ __forceinline__ void tg_glu_row(const TgJob& p, int split, int64_t m,
   }
 }
 
-// 64 rows of 128 columns that are all inside, from LDS (rows LD apart), eight rows of a lane at a time and each question (which activation, whether there
-// is a residual) asked once for the eight: nobody else is on the SIMD, so what is not in flight, or not next to other rows' instructions, is waited
-// for.  Asked row by row, 32768 x 512 by 2048 weight rows took 133 us with a bias for 108 without, 134 with GELU.  What comes from memory is requested eight rows ahead.
+// `rows` (16, 32, 48 or 64) whole rows of 128 columns from LDS (rows LD apart); a lane's four columns are inside or outside.  Eight rows of a lane at a time,
+// and each question (which activation, whether there is a residual) asked once for the eight: nobody else is on the SIMD, so what is not in flight, or
+// not next to other rows' instructions, is waited for.  32768 x 512 by 2048 weight rows with bias and GELU: 103 us, 158 asked row by row; without either
+// 87 and 108.  What comes from memory is requested eight rows ahead.
 template <int EPI, int LD>
-__device__ __forceinline__ void tg_rows_inside(const TgJob& p, const float* mine, int row0, int jw, int lane) {
+__device__ __forceinline__ void tg_rows_inside(const TgJob& p, const float* mine, int row0, int jw, int lane, int rows) {
   if constexpr (EPI == TG_GLU) {
     const int c = (lane & 15) * 4, n = jw + c, first = lane >> 4;
-    const bool lead = (n & 31) == 0;
+    const bool lead = (n & 31) == 0, in = n < p.N;
     bf16_t* const out = (bf16_t*)p.out + (int64_t)(row0 + first) * p.ldo + n;
 #pragma unroll 1
-    for (int i = 0; i < 64; i += 16) {
+    for (int i = 0; i < rows; i += 16) {
       float g[16], u[16];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -65,11 +66,14 @@ __device__ __forceinline__ void tg_rows_inside(const TgJob& p, const float* mine
         for (int k = 0; k < 4; ++k) { tg[k] = tg_max8(tg[k]); tu[k] = tg_max8(tu[k]); }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
+          if (!in) break;                                        // outside only now: the maximum goes across lanes
           const int64_t m = row0 + i + 4 * k + first;
           tg_keep8<true>(p.z, p.ldz, p.zs, p.lds, m, n, p.N, true, lead, tg[k], g + 4 * k);
           tg_keep8<true>(p.up, p.ldu, p.us, p.lds, m, n, p.N, true, lead, tu[k], u + 4 * k);
         }
-      } else if (p.save == 1) {
+      }
+      if (!in) continue;
+      if (p.save == 1) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const int64_t m = row0 + i + 4 * k + first;
@@ -87,6 +91,7 @@ __device__ __forceinline__ void tg_rows_inside(const TgJob& p, const float* mine
     }
   } else {
     const int c = (lane & 31) * 4, n = jw + c, r0 = lane >> 5, m0 = row0 + r0;
+    if (n >= p.N) return;
     typedef TgSide<bf16_t, EPI, true> Side;
     Side now[8], next[8];
     const bool asks = EPI == TG_GLUBWD || (EPI == TG_LINEAR && p.res);
@@ -100,10 +105,10 @@ __device__ __forceinline__ void tg_rows_inside(const TgJob& p, const float* mine
     float bias[4] = {0.f, 0.f, 0.f, 0.f};
     if (EPI == TG_LINEAR && p.bias) get4<float, true>(p.bias, 0, 0, n, p.N, true, bias);
 #pragma unroll 1
-    for (int i = 0; i < 64; i += 16) {
+    for (int i = 0; i < rows; i += 16) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) now[k] = next[k];
-      if (i < 48) request(i + 16);
+      if (i + 16 < rows) request(i + 16);
       float v[32];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
@@ -143,11 +148,12 @@ __device__ __forceinline__ void tg_rows_inside(const TgJob& p, const float* mine
 // The same at the matrix's edges and for partial sums: 64 rows of 128 columns from LDS, eight rows of a lane at a time.  What the epilogue reads from memory is
 // requested for the next eight before these are finished.
 template <int EPI, bool PART, int LD>
-__device__ __forceinline__ void tg_rows(const TgJob& p, int split, const float* mine, int row0, int jw, int lane) {
+__device__ __forceinline__ void tg_rows(const TgJob& p, int split, const float* mine, int row0, int jw, int lane, int from) {
+  const int left = p.M - row0, to = left < 64 ? left : 64;
   if constexpr (EPI == TG_GLU) {
     const int c = (lane & 15) * 4;
 #pragma unroll 1
-    for (int i = 0; i < 64; i += 16) {
+    for (int i = from; i < to; i += 16) {
       float4 g[4], u[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -165,12 +171,12 @@ __device__ __forceinline__ void tg_rows(const TgJob& p, int split, const float* 
     typedef TgSide<bf16_t, PART ? TG_GRAD : EPI> Side;
     Side now[8], next[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) next[k].request(p, row0 + 2 * k + r0, n);
+    for (int k = 0; k < 8; ++k) next[k].request(p, row0 + from + 2 * k + r0, n);
 #pragma unroll 1
-    for (int i = 0; i < 64; i += 16) {
+    for (int i = from; i < to; i += 16) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) now[k] = next[k];
-      if (i < 48) {
+      if (i + 16 < to) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) next[k].request(p, row0 + i + 16 + 2 * k + r0, n);
       }
@@ -309,7 +315,8 @@ __global__ __launch_bounds__(256, 1) void tg_big_k(const TgGroup grp) {
   const int jw = blk.j0 + (GLU ? bsub / 2 : bsub) * 16;
   const int need = (EPI == TG_GRAD || EPI == TG_LINEAR ? TG_VEC_OUT : 0) | (EPI == TG_LINEAR && p.res ? TG_VEC_RES : 0) |
                    ((EPI == TG_LINEAR && p.z) || EPI == TG_GLUBWD || (GLU && p.save) ? TG_VEC_Z : 0) | (EPI == TG_LINEAR && p.bias ? TG_VEC_BIAS : 0);
-  const bool inside = blk.j0 + (GLU ? 128 : 256) <= p.N && blk.m0 + 256 <= p.M && (p.flags & need) == need;
+  // fours of columns that are accessed as one, and no columns that only pad the rows: whole rows are quick
+  const bool quick = (p.flags & need) == need && p.N % 4 == 0 && (EPI == TG_LINEAR || EPI == TG_GRAD || p.ldo == p.N);
   auto write = [&](auto half) __attribute__((always_inline)) {
 #pragma unroll
     for (int a = 0; a < 4; ++a)
@@ -318,12 +325,13 @@ __global__ __launch_bounds__(256, 1) void tg_big_k(const TgGroup grp) {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // the other lanes' columns too: a wavefront's LDS accesses are in order
   };
   auto rows = [&](int row0) __attribute__((always_inline)) {
+    int done = 0;
     if constexpr (!PART) {
-      if (inside) tg_rows_inside<EPI, LD>(p, mine, row0, jw, blk.lane);
-      else tg_rows<EPI, PART, LD>(p, blk.split, mine, row0, jw, blk.lane);
-    } else {
-      tg_rows<EPI, PART, LD>(p, blk.split, mine, row0, jw, blk.lane);
+      const int left = p.M - row0;
+      done = !quick || left < 0 ? 0 : left < 64 ? left & ~15 : 64;
+      if (done) tg_rows_inside<EPI, LD>(p, mine, row0, jw, blk.lane, done);
     }
+    if (done < 64) tg_rows<EPI, PART, LD>(p, blk.split, mine, row0, jw, blk.lane, done);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   };
   const int row0 = blk.m0 + arow;
