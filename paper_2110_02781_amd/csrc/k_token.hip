@@ -2,6 +2,7 @@
 // linear layer's activation, rows copied into the alignment that the matrix products need.
 // Rows may start at any element: vectors of 16 bytes are accessed at the element's alignment (global memory takes them unaligned).
 #include <algorithm>
+#include <type_traits>
 
 #include "token_dev.h"
 
@@ -614,37 +615,62 @@ void tk_align(int dt, hipStream_t st, const TkCopy* jobs, int n) {
   if (m) go(g, m, most);
 }
 
-// dz = dy * act'(z) and its column sums.  A block has 256 columns (64 threads of four) of a chunk of rows, four threads to a column;
-// the sums are of dz before it is rounded.  1000 x 777 fp32 6.5 us and its join below 4.6, of which the bytes are 2: latency.
+// dz = dy * act'(z) and its column sums.  A block has 256 columns (64 threads of four) of a chunk of rows, four threads to a column, each with four
+// rows in flight; the sums are of dz before it is rounded.  Memory where there are enough rows and columns (8192 x 4096 bfloat16 36 us, 5.6 TB/s), latency
+// where not: 22715 x 64 9.3 us (two rows in flight 12.1, one 23), 1000 x 777 fp32 4.2 and its join below 4.6, of which the bytes are 2.  32768 x 2048 84, two rows 80.
 static int dz_rows(int M) { return std::max(16, (M + 255) / 256); }
 int tk_dz_chunks(int M) { return M > 0 ? (M + dz_rows(M) - 1) / dz_rows(M) : 0; }
+// four columns at any alignment, or (not whole) the `left` that there are; as stored, so that a row's wait is not the next one's
+template <typename E, bool WHOLE>
+__device__ __forceinline__ typename Tg4<E>::raw at4(const E* p, int left) {
+  typename Tg4<E>::raw r;
+  if constexpr (!WHOLE) return get_raw4<E>(p, 0, 0, 0, left, false);
+  else if constexpr (sizeof(E) == 2) { const u2v_t t = *reinterpret_cast<const TkAt<2>::v8*>(p); __builtin_memcpy(&r, &t, 8); }
+  else { const u4v_t t = tk_ld16<E>(p); __builtin_memcpy(&r, &t, 16); }
+  return r;
+}
 template <typename E>
 __global__ __launch_bounds__(256) void tk_dz_k(const E* __restrict__ dy, int64_t lddy, const E* __restrict__ z, int64_t ldz, int act, int M, int N,
-                                               int per, E* __restrict__ dz, int64_t ldd, float* __restrict__ part, int vec) {
+                                               int per, E* __restrict__ dz, int64_t ldd, float* __restrict__ part) {
+  constexpr int U = 4;
   __shared__ float4 sum[4][64];
   const int lane = threadIdx.x & 63, ty = threadIdx.x >> 6, n = (blockIdx.x * 64 + lane) * 4;
   const int r0 = blockIdx.y * per, r1 = r0 + per < M ? r0 + per : M;
   float s[4] = {0.f, 0.f, 0.f, 0.f};
   const int wide = dz ? (int)ldd : N;
-  if (n < wide)
-    for (int r = r0 + ty; r < r1; r += 4) {
-      float v[4];
-      get4<E>(dy, lddy, r, n, N, vec & 1, v);
-      if (act != TACT_NONE) {
-        float t[4], a[4], d[4];
-        get4<E>(z, ldz, r, n, N, vec & 2, t);
-        tact_grad4(t, a, d, act);
+  const auto walk = [&](auto whole) __attribute__((always_inline)) {
+    for (int r = r0 + ty; r < r1; r += 4 * U) {
+      typename Tg4<E>::raw y[U], x[U];
+      float v[4 * U], t[4 * U], a[4 * U], d[4 * U];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] *= d[e];
+      for (int u = 0; u < U; ++u) {
+        const int64_t m = r + 4 * u < r1 ? r + 4 * u : r;
+        y[u] = at4<E, whole.value>(dy + m * lddy + n, N - n);
+        if (act != TACT_NONE) x[u] = at4<E, whole.value>(z + m * ldz + n, N - n);
       }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] += n + e < N ? v[e] : 0.f;
-      if (dz) {
+      for (int u = 0; u < U; ++u) open4<E>(y[u], v + 4 * u);
+      if (act != TACT_NONE) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = n + e < N ? v[e] : 0.f;
-        put4<E>(dz, ldd, r, n, (int)ldd, true, v);
+        for (int u = 0; u < U; ++u) open4<E>(x[u], t + 4 * u);
+        tact_gradn<4 * U>(t, a, d, act);
+#pragma unroll
+        for (int e = 0; e < 4 * U; ++e) v[e] *= d[e];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (r + 4 * u >= r1) break;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (!whole.value && n + e >= N) v[4 * u + e] = 0.f;    // pad columns
+          s[e] += v[4 * u + e];
+        }
+        if (dz) put4<E>(dz, ldd, r + 4 * u, n, (int)ldd, true, v + 4 * u);
       }
     }
+  };
+  if (N - n >= 4) walk(std::true_type());
+  else if (n < wide) walk(std::false_type());
   if (!part) return;
   sum[ty][lane] = make_float4(s[0], s[1], s[2], s[3]);
   __syncthreads();
@@ -660,11 +686,9 @@ void tk_dz(int dt, hipStream_t st, const void* dy, int64_t lddy, const void* z, 
            int64_t ldd, float* part) {
   const int es = dt == 1 ? 2 : 4;
   KScope ks(st, "tok_dz", (double)M * N * es * ((act != TACT_NONE) + 1 + (dz != nullptr)), 4.0 * M * N, M, N);
-  const auto fits = [&](const void* p, int64_t ld) { return ((uintptr_t)p % (4 * es)) == 0 && ld % 4 == 0; };
-  const int vec = (fits(dy, lddy) ? 1 : 0) | (act != TACT_NONE && fits(z, ldz) ? 2 : 0);
   const dim3 g((std::max<int64_t>(N, dz ? ldd : 0) + 255) / 256, tk_dz_chunks(M));
-  if (dt == 1) hipLaunchKernelGGL(tk_dz_k<bf16_t>, g, dim3(256), 0, st, (const bf16_t*)dy, lddy, (const bf16_t*)z, ldz, act, M, N, dz_rows(M), (bf16_t*)dz, ldd, part, vec);
-  else hipLaunchKernelGGL(tk_dz_k<float>, g, dim3(256), 0, st, (const float*)dy, lddy, (const float*)z, ldz, act, M, N, dz_rows(M), (float*)dz, ldd, part, vec);
+  if (dt == 1) hipLaunchKernelGGL(tk_dz_k<bf16_t>, g, dim3(256), 0, st, (const bf16_t*)dy, lddy, (const bf16_t*)z, ldz, act, M, N, dz_rows(M), (bf16_t*)dz, ldd, part);
+  else hipLaunchKernelGGL(tk_dz_k<float>, g, dim3(256), 0, st, (const float*)dy, lddy, (const float*)z, ldz, act, M, N, dz_rows(M), (float*)dz, ldd, part);
 }
 // 64 columns a block, four threads to a column
 __global__ __launch_bounds__(256) void tk_colsum_join_k(const float* __restrict__ part, int chunks, int N, void* __restrict__ db, int bf16, int accumulate) {

@@ -11,7 +11,7 @@ typedef uint32_t u4v_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u2v_t __attribute__((ext_vector_type(2)));
 template <int A> struct TkAt;
 template <> struct TkAt<1> { typedef u2v_t v8 __attribute__((aligned(1))); };
-template <> struct TkAt<2> { typedef u4v_t v16 __attribute__((aligned(2))); };
+template <> struct TkAt<2> { typedef u4v_t v16 __attribute__((aligned(2))); typedef u2v_t v8 __attribute__((aligned(2))); };
 template <> struct TkAt<4> { typedef u4v_t v16 __attribute__((aligned(4))); };
 template <typename E> __device__ __forceinline__ u4v_t tk_ld16(const E* p) { return *reinterpret_cast<const typename TkAt<sizeof(E)>::v16*>(p); }
 template <typename E> __device__ __forceinline__ void tk_st16(E* p, u4v_t v) { *reinterpret_cast<typename TkAt<sizeof(E)>::v16*>(p) = v; }
