@@ -62,6 +62,48 @@ __device__ __forceinline__ void tg_results(const TgJob& p, f4v_t (&acc)[S][T], i
         if (m < M && n < p.ldo) tg_glu4<E>(p, m, n, g, u);
       }
     }
+  } else if constexpr (EPI == TG_LINEAR) {
+    // what comes from memory is under way for all of the results before any is waited for, and which activation it is asked once
+    typename Tg4<E>::raw res[S][T];
+    float v[S * T * 4];
+    if (p.res) {
+#pragma unroll
+      for (int a = 0; a < S; ++a)
+#pragma unroll
+        for (int b = 0; b < T; ++b)
+          res[a][b] = get_raw4<E>(p.res, p.ldr, row + a * 16 < M ? row + a * 16 : M - 1, jb + b * 16, N, p.flags & TG_VEC_RES);
+    }
+#pragma unroll
+    for (int b = 0; b < T; ++b) {
+      float t[4] = {0.f, 0.f, 0.f, 0.f};
+      if (p.bias) get4<float>(p.bias, 0, 0, jb + b * 16, N, p.flags & TG_VEC_BIAS, t);
+#pragma unroll
+      for (int a = 0; a < S; ++a)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[(a * T + b) * 4 + e] = acc[a][b][e] + t[e];
+    }
+    if (p.z) {
+#pragma unroll
+      for (int a = 0; a < S; ++a)
+#pragma unroll
+        for (int b = 0; b < T; ++b)
+          if (row + a * 16 < M && jb + b * 16 < N) put4<E>(p.z, p.ldz, row + a * 16, jb + b * 16, N, p.flags & TG_VEC_Z, v + (a * T + b) * 4);
+    }
+    tactn<S * T * 4>(v, p.act);
+    if (p.res) {
+#pragma unroll
+      for (int i = 0; i < S * T; ++i) {
+        float r[4];
+        open4<E>(res[i / T][i % T], r);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[i * 4 + e] += r[e];
+      }
+    }
+#pragma unroll
+    for (int a = 0; a < S; ++a)
+#pragma unroll
+      for (int b = 0; b < T; ++b)
+        if (row + a * 16 < M && jb + b * 16 < N) put4<E>(p.out, p.ldo, row + a * 16, jb + b * 16, N, p.flags & TG_VEC_OUT, v + (a * T + b) * 4);
   } else {
 #pragma unroll
     for (int a = 0; a < S; ++a)
