@@ -417,13 +417,12 @@ __global__ __launch_bounds__(64 * NW) void tg_skinny_k(const TgJob p) {
       return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, w), __builtin_bit_cast(bf16x8_t, xv), c, 0, 0, 0);
     }
   };
-  // a vector at any element; the row's last may end inside it, and what follows is not the row's
+  // a vector at any element; what follows a row that ends inside one is not the row's
   auto whole = [&](const char* row, int k) __attribute__((always_inline)) {
     const u4v_t t = tk_ld16<E>(reinterpret_cast<const E*>(row) + k);
     return make_uint4(t[0], t[1], t[2], t[3]);
   };
   auto ragged = [&](const char* row, int k) __attribute__((always_inline)) {
-    if (k + V <= K) return whole(row, k);
     uint32_t t[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int e = 0; e < V; ++e)
@@ -452,13 +451,28 @@ __global__ __launch_bounds__(64 * NW) void tg_skinny_k(const TgJob p) {
       if (GLU) acc[1] = mul(acc[1], b[u], c[u]);
     }
   }
-  if (k0 < K) {
-#pragma unroll 1
+  if (k0 < K) {                                                 // the last turn: its whole vectors together, then the one that the row ends in
+    uint4 a[U], b[U], c[U];
+#pragma unroll
     for (int u = 0; u < U; ++u) {
       const int k = k0 + (u * 4 + G) * V;
-      const uint4 a = ragged(w0, k), c = xin ? ragged(x, k) : make_uint4(0, 0, 0, 0);
-      acc[0] = mul(acc[0], a, c);
-      if (GLU) acc[1] = mul(acc[1], ragged(w1, k), c);
+      const bool in = k + V <= K;
+      a[u] = b[u] = c[u] = make_uint4(0, 0, 0, 0);
+      if (in) a[u] = whole(w0, k);
+      if (GLU && in) b[u] = whole(w1, k);
+      if (in && xin) c[u] = whole(x, k);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      acc[0] = mul(acc[0], a[u], c[u]);
+      if (GLU) acc[1] = mul(acc[1], b[u], c[u]);
+    }
+    const int k = K / V * V;
+    if (k < K && k >= k0) {
+      const bool mine = G == 0;
+      const uint4 nothing = make_uint4(0, 0, 0, 0), w = mine ? ragged(w0, k) : nothing, t = mine && xin ? ragged(x, k) : nothing;
+      acc[0] = mul(acc[0], w, t);
+      if (GLU) acc[1] = mul(acc[1], mine ? ragged(w1, k) : nothing, t);
     }
   }
   meet[0][wave][lane] = make_float4(acc[0][0], acc[0][1], acc[0][2], acc[0][3]);
