@@ -77,7 +77,7 @@ struct Call {
   // Whether the kernel of few rows takes a product of `mats` weight matrices [n][k] (aligned: a tile could read them as they are).  Up to eight rows always.
   // Beyond them its reads of x, 16 rows for every 16 weight rows, cost more than the empty rows of a tile where the weights are bfloat16 and many: 16 rows, 4096 x 4096
   // 11.4 us, a tile split by four 14.3; 14336 x 4096 33.4 and 28.0; gate and up of 2048 x 5632 and down 25.3, 21.9; fp32 64 and 69, 20 and 28.  Weights that
-  // a tile needs copied first are streamed: 4096 x 4100 with one row 11 us, with copies 24.
+  // a tile needs copied first are streamed: 4096 x 4100 with one row 6 us, with copies some 20.
   bool few(int rows, int n, int k, int mats, bool aligned) const {
     if (rows > kSkinnyRows) return false;
     return rows <= 8 || dt == FTP_F32 || !aligned || (double)n * k * mats * 2 <= 40e6;
