@@ -33,8 +33,8 @@ struct TgLoad {
   uint32_t off[NQ];
   int kc;                                  // along: this lane's first reduction element in a step
   // row0: first row (of the result's side) of the tile, rows: how many the operand has; ld in elements.  half: rows from R / 2 on belong to
-  // a second matrix and count from row0 again
-  __device__ __forceinline__ void init(int wave, int lane, int row0, int rows, int64_t ld, bool half) {
+  // a second matrix, whose rows are ld_half apart, and count from row0 again
+  __device__ __forceinline__ void init(int wave, int lane, int row0, int rows, int64_t ld, bool half, int64_t ld_half) {
     kc = 0;
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
@@ -42,8 +42,9 @@ struct TgLoad {
         int r = (q * NW + wave) * 8 + (lane >> 3);
         const int c = (lane & 7) ^ (r & 7);
         kc = c * Tg<E>::V;
-        if (half && r >= R / 2) r -= R / 2;
-        off[q] = row0 + r < rows ? (uint32_t)(r * (uint32_t)ld * sizeof(E)) + c * 16 : kPast;
+        uint32_t apart = (uint32_t)ld;
+        if (half && r >= R / 2) { r -= R / 2; apart = (uint32_t)ld_half; }
+        off[q] = row0 + r < rows ? (uint32_t)(r * apart * sizeof(E)) + c * 16 : kPast;
       } else {
         constexpr int CPR = R * sizeof(E) / 16;                 // vectors to a reduction row of the tile
         const int i = (q * NW + wave) * 64 + lane, r = i / CPR, c = i % CPR;
@@ -133,18 +134,18 @@ struct TgBlock {
     s1 = s0 + p.steps < total ? s0 + p.steps : total;
     seg = nseg > 1 && s0 >= spseg ? 1 : 0;
     ks = s0 - seg * spseg;
-    la.init(wave, lane, m0, p.M, lda, false);
+    la.init(wave, lane, m0, p.M, lda, false, lda);
     aim(p);
     return true;
   }
   __device__ __forceinline__ void aim(const TgJob& p) {
     ldb = seg ? p.ldb[1] : p.ldb[0];
-    lb.init(wave, lane, j0, p.N, ldb, GLU);
+    lb.init(wave, lane, j0, p.N, ldb, GLU, p.ldb[1]);            // with TG_GLU b[1] is the up projection's weights, in rows of their own distance
     stepa = (uint32_t)((AX ? KS * lda : KS) * (int64_t)sizeof(E));
     stepb = (uint32_t)((BX ? KS * ldb : KS) * (int64_t)sizeof(E));
     pa = (const char*)(seg ? p.a[1] : p.a[0]) + (AX ? (int64_t)m0 : m0 * lda) * (int64_t)sizeof(E) + ks * (int64_t)stepa;
     pb = (const char*)(seg ? p.b[1] : p.b[0]) + (BX ? (int64_t)j0 : j0 * ldb) * (int64_t)sizeof(E) + ks * (int64_t)stepb;
-    if (GLU) pb2 = (const char*)p.b[1] + j0 * ldb * (int64_t)sizeof(E) + ks * (int64_t)stepb;
+    if (GLU) pb2 = (const char*)p.b[1] + j0 * p.ldb[1] * (int64_t)sizeof(E) + ks * (int64_t)stepb;
   }
   // the next step's descriptors: a base that moves on by a step, and a size that ends with the reduction where it runs across the rows
   // (past the last step: nothing is inside)

@@ -1,0 +1,37 @@
+"""Gated feed-forward blocks and linear layers in forms that every operand has to itself: each matrix at its own row distance and offset, inputs in 8 bits
+at any byte, infinities beside pad columns, calls without rows, the longest ones.  Against the formulas in 64 bits, with the bounds of token_ref."""
+import pytest
+
+import test_gpu_token as T
+from test_gpu_token import env  # noqa: F401  (a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def each_its_own(monkeypatch, *forms):
+    """The matrices that a case makes, in its order, get (slack, skip) one after the other: elements between rows, and in front of the first."""
+    real, left = T.matrix, list(forms)
+
+    def matrix(torch, gen, rows, cols, dtype, std=1.0, slack=0, skip=0):
+        return real(torch, gen, rows, cols, dtype, std, *left.pop(0))
+    monkeypatch.setattr(T, "matrix", matrix)
+    return left
+
+
+# gate wider apart, up wider apart, one of them copied into rows of its own while the other lies as it does
+FORMS = [((72, 0), (0, 0)), ((8, 0), (136, 8)), ((8, 1), (8, 0)), ((16, 0), (16, 1))]
+# dtype, rows, width, hidden and the tile that gate and up take
+GATED = [("bf16", 40, 72, 72, "64"), ("bf16", 40, 2056, 72, "64 split"), ("bf16", 1900, 72, 1032, "128"), ("bf16", 1900, 4104, 264, "128 split"),
+         ("bf16", 1900, 72, 2056, "256"), ("bf16", 2500, 4104, 1032, "256 split"), ("f32", 40, 72, 72, "64"), ("f32", 40, 1032, 72, "64 split"),
+         ("f32", 1900, 72, 1032, "128"), ("f32", 1900, 1032, 264, "128 split"), ("bf16", 5, 72, 40, None), ("bf16", 5, 70, 33, None)]
+
+
+@pytest.mark.parametrize("dtype,rows,d,f,tile", GATED)
+def test_gate_and_up_weights_at_their_own_distances(env, monkeypatch, dtype, rows, d, f, tile):
+    x, down = (0, 0), (8, 0)
+    for gate, up in FORMS:
+        with monkeypatch.context() as m:
+            left = each_its_own(m, x, gate, up, down)
+            with T.routes(env[1]) as took:
+                T.ffn_case(env, dtype, "silu", 0, rows, d, f, 0, 0)
+        assert not left and took.get("tok_glu") == ({tile} if tile else None), took
