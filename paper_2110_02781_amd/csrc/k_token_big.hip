@@ -283,7 +283,8 @@ __global__ __launch_bounds__(256, 1) void tg_big_k(const TgGroup grp) {
     TG_SECOND(1) mul(a1[1], b1, 1, 7);
     TG_SECOND(2) mul(a1[2], b1, 2, 7);
     TG_SECOND(3) mul(a1[3], b1, 3, 7);
-    blk.next(p);                 // the next step's descriptors, between products too (the columns' requests go on until the last turn)
+    const bool turned = blk.next_bases(p);   // the next step's descriptors, between products too; the columns' requests go on until the last turn, with the
+                                             // descriptor and the offsets of this step
     TG_SECOND(4)
     ra = blk.source_a();
     mul(a1[4], b1, 4, 7);
@@ -294,6 +295,7 @@ __global__ __launch_bounds__(256, 1) void tg_big_k(const TgGroup grp) {
     const u4s_t nb2 = blk.source_b2();
     mul(a1[6], b1, 6, 7);
     TG_SECOND(7)
+    if (turned) blk.aim_offsets(p);
     rb = nb;
     if (GLU) rb2 = nb2;
     ina = blk.in_a(), inb = blk.in_b();

@@ -139,8 +139,14 @@ struct TgBlock {
     return true;
   }
   __device__ __forceinline__ void aim(const TgJob& p) {
-    ldb = seg ? p.ldb[1] : p.ldb[0];
+    aim_bases(p);
+    aim_offsets(p);
+  }
+  __device__ __forceinline__ void aim_offsets(const TgJob& p) {
     lb.init(wave, lane, j0, p.N, ldb, GLU, p.ldb[1]);            // with TG_GLU b[1] is the up projection's weights, in rows of their own distance
+  }
+  __device__ __forceinline__ void aim_bases(const TgJob& p) {
+    ldb = seg ? p.ldb[1] : p.ldb[0];
     stepa = (uint32_t)((AX ? KS * lda : KS) * (int64_t)sizeof(E));
     stepb = (uint32_t)((BX ? KS * ldb : KS) * (int64_t)sizeof(E));
     pa = (const char*)(seg ? p.a[1] : p.a[0]) + (AX ? (int64_t)m0 : m0 * lda) * (int64_t)sizeof(E) + ks * (int64_t)stepa;
@@ -160,11 +166,19 @@ struct TgBlock {
   __device__ __forceinline__ bool in_b() const { return BX || lb.kc < K - ks * KS; }
   __device__ __forceinline__ uint32_t place(uint32_t at) const { return smem_at + at + wave * 1024; }
   __device__ __forceinline__ void next(const TgJob& p) {
+    if (next_bases(p)) aim_offsets(p);
+  }
+  // true: the second segment begins, whose rows have a distance of their own: aim_offsets() is due, after the last request of this step
+  __device__ __forceinline__ bool next_bases(const TgJob& p) {
     ++ks;
     pa += stepa;
     pb += stepb;
     if (GLU) pb2 += stepb;
-    if (LAY == TG_NN && nseg > 1 && ks == spseg && seg == 0) { seg = 1; ks = 0; aim(p); }
+    if (!(LAY == TG_NN && nseg > 1 && ks == spseg && seg == 0)) return false;
+    seg = 1;
+    ks = 0;
+    aim_bases(p);
+    return true;
   }
   // requests the next step's operands into LDS at at_a and at_b
   __device__ __forceinline__ void fetch(const TgJob& p, uint32_t at_a, uint32_t at_b) {

@@ -35,3 +35,20 @@ def test_gate_and_up_weights_at_their_own_distances(env, monkeypatch, dtype, row
             with T.routes(env[1]) as took:
                 T.ffn_case(env, dtype, "silu", 0, rows, d, f, 0, 0)
         assert not left and took.get("tok_glu") == ({tile} if tile else None), took
+
+
+# dtype, rows, width, hidden and the tile of dx, whose reduction goes over the gate weights and then the up weights: one part, or split so that a part begins
+# with the gate's and ends with the up projection's.  The last step of the gate's is a whole one (320 and 2112 are multiples of 64).
+DX = [("bf16", 4090, 2056, 320, "256"), ("bf16", 4090, 1032, 2112, "256 split"), ("bf16", 1500, 2056, 320, "128"), ("bf16", 1900, 520, 2112, "128 split"),
+      ("bf16", 300, 264, 320, "64"), ("bf16", 500, 520, 1088, "64 split"), ("f32", 1500, 2056, 320, "128"), ("f32", 500, 520, 1088, "64 split")]
+
+
+@pytest.mark.parametrize("save", [1, 2])
+@pytest.mark.parametrize("dtype,rows,d,f,tile", DX)
+def test_backward_with_weights_at_their_own_distances(env, monkeypatch, dtype, rows, d, f, tile, save):
+    for gate, up in FORMS:
+        with monkeypatch.context() as m:
+            left = each_its_own(m, (0, 0), gate, up, (8, 0), (16, 0))
+            with T.routes(env[1]) as took:
+                T.ffn_case(env, dtype, "silu", save, rows, d, f, 0, 0)
+        assert not left and tile in took["tok_linear"], took
