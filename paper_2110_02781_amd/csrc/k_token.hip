@@ -92,7 +92,7 @@ void tk_embed(int dt, hipStream_t st, const void* ids, int ids64, int64_t n, int
   });
 }
 
-// zeros: block b of nb, blocks of T threads
+// zeros: block b of nb, blocks of T threads.  Rows start at any element of two bytes or four, and end at one
 template <int T>
 __device__ __forceinline__ void tk_fill_rows(char* __restrict__ p, uint32_t rows, int64_t row_bytes, int64_t ld_bytes, uint32_t b, uint32_t nb) {
   const uint32_t per = (uint32_t)((row_bytes + 15) / 16), all = rows * per;
@@ -100,9 +100,9 @@ __device__ __forceinline__ void tk_fill_rows(char* __restrict__ p, uint32_t rows
     const uint32_t r = i / per, c = i - r * per;
     char* const q = p + (int64_t)r * ld_bytes + (int64_t)c * 16;
     const int64_t left = row_bytes - (int64_t)c * 16;
-    if (left >= 16) tk_st16<float>(reinterpret_cast<float*>(q), u4v_t{0, 0, 0, 0});
+    if (left >= 16) tk_st16<bf16_t>(reinterpret_cast<bf16_t*>(q), u4v_t{0, 0, 0, 0});
     else
-      for (int64_t o = 0; o < left; o += 4) *reinterpret_cast<float*>(q + o) = 0.f;
+      for (int64_t o = 0; o < left; o += 2) *reinterpret_cast<bf16_t*>(q + o) = 0;
   }
 }
 __global__ __launch_bounds__(256) void tk_fill_k(char* __restrict__ p, uint32_t rows, int64_t row_bytes, int64_t ld_bytes) {

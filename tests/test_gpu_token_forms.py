@@ -52,3 +52,26 @@ def test_backward_with_weights_at_their_own_distances(env, monkeypatch, dtype, r
             with T.routes(env[1]) as took:
                 T.ffn_case(env, dtype, "silu", save, rows, d, f, 0, 0)
         assert not left and tile in took["tok_linear"], took
+
+
+@pytest.mark.parametrize("grad", ["f32", "bf16"])
+@pytest.mark.parametrize("d,f", [(1, 1), (3, 5), (8, 9), (7, 1), (33, 31), (257, 1023), (16, 24)])
+def test_gradients_of_a_call_without_rows(env, d, f, grad):
+    """Zeros for each element and nothing behind the last one, whatever the gradients' lengths in bytes and their alignment."""
+    torch, P, _ = env
+    gdt, gcode = T.types(P, torch, grad)
+    sp = torch.cuda.current_stream().cuda_stream
+    w = torch.ones(f, d, device="cuda", dtype=torch.bfloat16)
+    for skip in (0, 1, 2, 3):
+        for accumulate in (0, 1) if grad == "f32" else (0,):
+            made = [T.out(torch, n, m, gdt, 0, skip) for n, m in ((f, d), (1, f), (f, d), (f, d), (d, f))]
+            dw, db, dg, du, dd = (m for m, _ in made)
+            for m, _ in made:
+                m.fill_(5.0)
+            P.linear_backward(P.linear_args(rows=0, n_in=d, n_out=f, dtype=P.BF16, w=w, ldw=d, dw=dw, dbias=db, grad_dtype=gcode, accumulate=accumulate), sp)
+            P.ffn_backward(P.ffn_args(rows=0, width=d, hidden=f, dtype=P.BF16, act=P.ACT_SILU, save=P.SAVE_FULL, w_gate=w, ldwg=d, w_up=w, ldwu=d, w_down=w, ldwd=f,
+                                      dw_gate=dg, dw_up=du, dw_down=dd, grad_dtype=gcode, accumulate=accumulate), sp)
+            torch.cuda.synchronize()
+            for m, ok in made:
+                assert bool((m == (5.0 if accumulate else 0.0)).all())
+                ok()
