@@ -137,10 +137,11 @@ int check_common(const char* who, int64_t rows, int dt, int act) {
   return FTP_OK;
 }
 // one matrix: there (unless it has no rows), aligned to its elements, rows at least `cols` apart
+enum { kBytes = -1 };                    // in place of a dtype: a matrix in 8 bits
 int check_mat(const char* who, const char* what, const void* p, int64_t ld, int64_t rows, int64_t cols, int dt, bool optional = false) {
   if (!p && (optional || rows == 0)) return FTP_OK;
   NEED(p, FTP_ERR_ARG, "%s: %s is NULL", who, what);
-  NEED(at_element(p, dt), FTP_ERR_ARG, "%s: %s is not aligned to its elements", who, what);
+  NEED(dt == kBytes || at_element(p, dt), FTP_ERR_ARG, "%s: %s is not aligned to its elements", who, what);
   NEED(ld >= cols && ld <= kMaxLd, FTP_ERR_ARG, "%s: %s has rows %lld apart (at least %lld, at most 2^20)", who, what, (long long)ld, (long long)cols);
   return FTP_OK;
 }
@@ -161,7 +162,7 @@ int check_linear(const char* who, const ftp_linear_args* a, bool backward) {
   NEED(a->n_in >= 1 && a->n_in <= kMaxDim && a->n_out >= 1 && a->n_out <= kMaxDim, FTP_ERR_ARG, "%s: n_in and n_out must be 1 .. 2^20", who);
   const bool x8 = a->x_scales != nullptr;
   if (!backward || a->dw) {
-    TRY(check_mat(who, "x", a->x, a->ldx, a->rows, a->n_in, x8 ? FTP_BF16 + 1 : a->dtype));
+    TRY(check_mat(who, "x", a->x, a->ldx, a->rows, a->n_in, x8 ? kBytes : a->dtype));
     NEED(!x8 || a->ldxs >= act8_groups(a->n_in), FTP_ERR_ARG, "%s: scales of x have rows %lld apart (%d groups)", who, (long long)a->ldxs, act8_groups(a->n_in));
   }
   if (!backward || a->dx) TRY(check_mat(who, "w", a->w, a->ldw, 1, a->n_in, a->dtype));
@@ -264,7 +265,7 @@ int check_ffn(const char* who, const ftp_ffn_args* a, bool backward) {
   const bool x8 = a->x_scales != nullptr;
   const bool grads = a->dw_gate || a->dw_up || a->dw_down;
   if (!backward || grads) {
-    TRY(check_mat(who, "x", a->x, a->ldx, a->rows, a->width, x8 ? FTP_BF16 + 1 : a->dtype));
+    TRY(check_mat(who, "x", a->x, a->ldx, a->rows, a->width, x8 ? kBytes : a->dtype));
     NEED(!x8 || a->ldxs >= act8_groups(a->width), FTP_ERR_ARG, "%s: scales of x have rows %lld apart (%d groups)", who, (long long)a->ldxs, act8_groups(a->width));
   }
   TRY(check_mat(who, "w_gate", a->w_gate, a->ldwg, 1, a->width, a->dtype));
