@@ -82,11 +82,12 @@ def test_gradients_of_a_call_without_rows(env, d, f, grad):
 def test_inputs_in_8_bits_at_any_byte(env, monkeypatch, dtype, off):
     """Packed rows and scales that start `off` bytes into their buffers, with rows of an odd number of bytes: a slice of a stash."""
     torch, P, R = env
-    encode = R.act8_encode
+    encode, alive = R.act8_encode, []
 
     def inside(t):
         buf = torch.full((off + t.numel() + 16,), 0x7F, dtype=torch.uint8, device="cuda")          # NaN around the values
         buf[off:off + t.numel()] = t.flatten()
+        alive.append(buf)                                        # a case hands on addresses, also after its names stand for something else
         return buf[off:off + t.numel()].view(t.shape)
     monkeypatch.setattr(R, "act8_encode", lambda x: tuple(inside(t) for t in encode(x)))
     for rows, k, n in ((1, 33, 8), (9, 101, 64), (40, 1001, 72), (70, 64, 40)):
