@@ -172,6 +172,13 @@ __device__ __forceinline__ void open4(const typename Tg4<E>::raw& r, float v[4])
   v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
 }
 
+// Columns from N on only pad a row to a multiple of 16 bytes, and the products that follow read them against zeros: written as zeros, because
+// what the sums hold there need not be one (an infinity times the zeros that arrive from outside is NaN; few rows multiply the last weight row again)
+__device__ __forceinline__ void tg_no_pad(float* v, int n, int N) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = n + e < N ? v[e] : 0.f;
+}
+
 template <typename E, int EPI, bool F = false> struct TgSide;
 
 template <typename E, bool F> struct TgSide<E, TG_LINEAR, F> {
@@ -243,6 +250,10 @@ template <typename E, bool F> struct TgSide<E, TG_GLUBWD, F> {
       du[e] = dh[e] * a[e];
       a[e] *= uv[e];
     }
+    if (!F && n + 3 >= p.N) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) { tg_no_pad(dg + 4 * k, n, p.N); tg_no_pad(du + 4 * k, n, p.N); tg_no_pad(a + 4 * k, n, p.N); }
+    }
     // rounded to the type of the products that follow, as their operands
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -283,7 +294,8 @@ __device__ __forceinline__ float tg_max8(float x) {
   return fmaxf(x, dpp_move<0x141>(x));
 }
 
-// act(g) * u into the hidden rows, whose pad columns (up to a multiple of 16 bytes) become zero: g and u are zero there
+// act(g) * u into the hidden rows, whose pad columns (up to a multiple of 16 bytes) become zero.  Kept in the call's type (save 1), gate and up are rounded once
+// more than the sums hold: what a stash takes is what bounds the batches in flight, and one in single precision would take twice the bytes
 template <typename E, bool F = false>
 __device__ __forceinline__ void tg_glu4(const TgJob& p, int64_t m, int n, const float g[4], const float u[4]) {
   if (p.save == 1) {
@@ -294,6 +306,7 @@ __device__ __forceinline__ void tg_glu4(const TgJob& p, int64_t m, int n, const 
   tact4(h, p.act);
 #pragma unroll
   for (int e = 0; e < 4; ++e) h[e] *= u[e];
+  if (!F && n + 3 >= p.N) tg_no_pad(h, n, p.N);
   put4<E, F>(p.out, p.ldo, m, n, (int)p.ldo, true, h);
 }
 template <bool F = false>

@@ -93,3 +93,58 @@ def test_inputs_in_8_bits_at_any_byte(env, monkeypatch, dtype, off):
     for rows, k, n in ((1, 33, 8), (9, 101, 64), (40, 1001, 72), (70, 64, 40)):
         T.linear_case(env, dtype, "silu", rows, k, n, 0, 0, x8=True)
         T.ffn_case(env, dtype, "silu", 2, rows, k, n, 0, 0, x8=True)
+
+
+# routes of gate and up, and of the gradients behind them: few rows, tiles of 64, 128 and 256, split reductions; hidden rows that end inside 16 bytes
+ODD = [("bf16", 5, 72, 33), ("bf16", 40, 72, 33), ("bf16", 40, 2056, 33), ("bf16", 1900, 72, 1031), ("bf16", 1900, 72, 2051), ("f32", 40, 72, 33), ("f32", 40, 1032, 35),
+       ("f32", 1900, 72, 1031)]
+
+
+@pytest.mark.parametrize("dtype,rows,d,f", ODD)
+def test_infinities_beside_pad_columns(env, dtype, rows, d, f):
+    """An infinity in a row of x, or of dy: what is infinite by the formula is infinite, not NaN (products of positive numbers with ReLU and without an activation:
+    no infinity meets a zero or one of the other sign), and the other rows keep their bits."""
+    torch, P, R = env
+    tdt, code = T.types(P, torch, dtype)
+    gen = torch.Generator(device="cuda").manual_seed(rows + f)
+    sp = torch.cuda.current_stream().cuda_stream
+
+    def positive(n, m, std):
+        return T.matrix(torch, gen, n, m, tdt, std, 3, 0).abs_().add_(std)
+    x, wg, wu, wd, dy = positive(rows, d, 1.0), positive(f, d, 1 / d), positive(f, d, 1 / d), positive(d, f, 1 / f), positive(rows, d, 1.0)
+    row = rows // 2
+
+    def call(x, dy, act):
+        o = dict(y=torch.empty(rows, d, dtype=tdt, device="cuda"), dx=torch.empty(rows, d, dtype=tdt, device="cuda"), dg=torch.empty(f, d, device="cuda"),
+                 du=torch.empty(f, d, device="cuda"), dd=torch.empty(d, f, device="cuda"), gate=torch.empty(rows, f, dtype=tdt, device="cuda"),
+                 up=torch.empty(rows, f, dtype=tdt, device="cuda"))
+        a = P.ffn_args(rows=rows, width=d, hidden=f, dtype=code, act=act, save=P.SAVE_FULL, gate=o["gate"], up=o["up"], x=x, ldx=x.stride(0), w_gate=wg, ldwg=wg.stride(0),
+                       w_up=wu, ldwu=wu.stride(0), w_down=wd, ldwd=wd.stride(0), y=o["y"], ldy=d, dy=dy, lddy=dy.stride(0), dx=o["dx"], lddx=d, dw_gate=o["dg"],
+                       dw_up=o["du"], dw_down=o["dd"])
+        ws, ok = T.given(a, torch, P.ffn_workspace(a))
+        P.ffn_forward(a, sp)
+        torch.cuda.synchronize()
+        ok()
+        ws, ok = T.given(a, torch, P.ffn_workspace(a, True))
+        P.ffn_backward(a, sp)
+        torch.cuda.synchronize()
+        ok()
+        return o
+    for act in (P.ACT_NONE, P.ACT_RELU):
+        plain = call(x, dy, act)
+        assert all(bool(v.isfinite().all()) for v in plain.values())
+        others = torch.arange(rows, device="cuda") != row
+        bad = x.clone()
+        bad[row, 3] = float("inf")
+        got = call(bad, dy, act)
+        for k in ("gate", "up", "y"):
+            assert bool((got[k][row] == float("inf")).all()), k
+        assert all(torch.equal(got[k][others], plain[k][others]) for k in ("gate", "up", "y", "dx"))
+        bad = dy.clone()
+        bad[row, 3] = float("inf")
+        got = call(x, bad, act)
+        assert bool((got["dx"][row] == float("inf")).all())
+        assert torch.equal(got["dx"][others], plain["dx"][others]) and torch.equal(got["y"], plain["y"])
+        # gradients of the gate and up weights take the row, those of the down weights in the row of the infinite column
+        assert bool((got["dg"] == float("inf")).all()) and bool((got["du"] == float("inf")).all())
+        assert bool((got["dd"][3] == float("inf")).all()) and torch.equal(got["dd"][4:], plain["dd"][4:])
