@@ -269,7 +269,13 @@ __global__ __launch_bounds__(256, 1) void tg_big_k(const TgGroup grp) {
     mul(fa[I], fb, I, 6);                                                             \
   }
   uint32_t u0 = 0, u1 = UNIT, u2 = 2 * UNIT, u3 = 3 * UNIT, u4 = 4 * UNIT;
-  u4s_t ra = blk.source_a(), rb = blk.source_b(), rb2 = blk.source_b2();
+  u4s_t ra = blk.source_a(), rb = blk.source_b(), rb2 = rb;
+  if constexpr (GLU) {
+    rb2 = blk.source_b2();
+    tg_settle(ra, rb, rb2);
+  } else {
+    tg_settle(ra, rb);
+  }
   bool ina = blk.in_a(), inb = blk.in_b();
   for (int s = blk.s0; s < blk.s1; ++s) {
     const uint32_t at = blk.place(u4), bt = blk.place(u0);
@@ -286,13 +292,19 @@ __global__ __launch_bounds__(256, 1) void tg_big_k(const TgGroup grp) {
     const bool turned = blk.next_bases(p);   // the next step's descriptors, between products too; the columns' requests go on until the last turn, with the
                                              // descriptor and the offsets of this step
     TG_SECOND(4)
-    ra = blk.source_a();
+    ra = blk.source_a();         // its first reader is more than five products away, as those of nb and nb2 are
+    tg_pin(ra);
     mul(a1[4], b1, 4, 7);
     TG_SECOND(5)
-    const u4s_t nb = blk.source_b();
+    u4s_t nb = blk.source_b();
+    tg_pin(nb);
     mul(a1[5], b1, 5, 7);
     TG_SECOND(6)
-    const u4s_t nb2 = blk.source_b2();
+    u4s_t nb2 = nb;
+    if constexpr (GLU) {
+      nb2 = blk.source_b2();
+      tg_pin(nb2);
+    }
     mul(a1[6], b1, 6, 7);
     TG_SECOND(7)
     if (turned) blk.aim_offsets(p);

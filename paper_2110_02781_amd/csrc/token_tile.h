@@ -62,6 +62,12 @@ __device__ __forceinline__ u4s_t tg_rsrc(const char* base, uint32_t bytes) {    
   const auto one = [](uint32_t v) __attribute__((always_inline)) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); };   // scalar registers
   return u4s_t{one((uint32_t)b), one((uint32_t)(b >> 32) & 0xffffu), one(bytes), 0x00020000u};
 }
+// A vector instruction that wrote a scalar register (the size's way through tg_rsrc) must be five wait states ahead of the memory instruction that reads it; the
+// compiler sees to that only for its own instructions, the loads below are written out.
+__device__ __forceinline__ void tg_settle(u4s_t& a, u4s_t& b) { asm volatile("s_nop 4" : "+s"(a), "+s"(b)); }
+__device__ __forceinline__ void tg_settle(u4s_t& a, u4s_t& b, u4s_t& c) { asm volatile("s_nop 4" : "+s"(a), "+s"(b), "+s"(c)); }
+// the descriptor is complete here, not only where it is used
+__device__ __forceinline__ void tg_pin(u4s_t& a) { asm volatile("" : "+s"(a)); }
 // 16 bytes per lane from the buffer to LDS, lane after lane from `lds` (an LDS byte address, the same for the wavefront).  In assembly,
 // because of the builtin the compiler waits for all of them in front of the next LDS read, whichever buffer that reads: nothing would be in
 // flight beside the products.  There is no output register; what orders these loads is tg_wait_loads and the barrier behind it.
@@ -182,7 +188,13 @@ struct TgBlock {
   }
   // requests the next step's operands into LDS at at_a and at_b
   __device__ __forceinline__ void fetch(const TgJob& p, uint32_t at_a, uint32_t at_b) {
-    const u4s_t fa = source_a(), fb = source_b(), fb2 = source_b2();
+    u4s_t fa = source_a(), fb = source_b(), fb2 = fb;
+    if constexpr (GLU) {
+      fb2 = source_b2();
+      tg_settle(fa, fb, fb2);
+    } else {
+      tg_settle(fa, fb);
+    }
     const bool ina = in_a(), inb = in_b();
 #pragma unroll
     for (int q = 0; q < la.NQ; ++q) tg_load_lds(fa, ina ? la.off[q] : la.kPast, place(at_a) + q * (NW * 1024));
