@@ -236,6 +236,15 @@ __global__ __launch_bounds__(256, 1) void tg_big_k(const TgGroup grp) {
     asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc[a][b]) : "v"(__builtin_bit_cast(bf16x8_t, fb[b])), "v"(__builtin_bit_cast(bf16x8_t, fa)));
     __builtin_amdgcn_sched_barrier(0);
   };
+  // a product between the setting of m0, to lds + ADD, and the load into LDS that goes by it (tg_load_lds has an idle instruction there): one statement, so that
+  // nothing the compiler adds comes between
+  auto mul_load = [&](const uint4& fa, const uint4 (&fb)[8], int a, uint32_t lds, auto add, const u4s_t& rs, uint32_t off) __attribute__((always_inline)) {
+    asm volatile("s_add_u32 m0, %3, %4\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0\n\tbuffer_load_dwordx4 %5, %6, 0 offen lds"
+                 : "+a"(acc[a][0])
+                 : "v"(__builtin_bit_cast(bf16x8_t, fb[0])), "v"(__builtin_bit_cast(bf16x8_t, fa)), "s"(lds), "n"(add.value), "v"(off), "s"(rs)
+                 : "memory", "scc");
+    __builtin_amdgcn_sched_barrier(0);
+  };
   blk.fetch(p, 0, UNIT);
   blk.fetch(p, 2 * UNIT, 3 * UNIT);
   tg_meet<16>();
@@ -255,9 +264,7 @@ __global__ __launch_bounds__(256, 1) void tg_big_k(const TgGroup grp) {
   // at its end: three a turn in the first half leave two turns for the last ones to arrive.
 #define TG_TURN(I, fa, fb, ra, rb, ua, ub, kk, Q, at, rs, in, off)                    \
   {                                                                                   \
-    tg_aim_lds<I * 4096>(at);                                                         \
-    mul(fa[I], fb, I, 0);                                                             \
-    tg_load_aimed(rs(I), in ? off[I] : blk.la.kPast);                                 \
+    mul_load(fa[I], fb, I, at, std::integral_constant<int, I * 4096>(), rs(I), in ? off[I] : blk.la.kPast); \
     mul(fa[I], fb, I, 1);                                                             \
     read(ra, rb, Q * I, ua, ub, kk);                                                  \
     mul(fa[I], fb, I, 2);                                                             \
@@ -320,7 +327,9 @@ __global__ __launch_bounds__(256, 1) void tg_big_k(const TgGroup grp) {
 #undef TG_B
 #undef TG_FIRST
 #undef TG_SECOND
-  asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");           // the last products' results are there (the compiler does not know when)
+  // The last products' results are there (the compiler does not know when: tests/test_token_waits.py looks whether it has put a sum's copy in front)
+  asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
   // Results: through LDS, half of the wavefront's rows at a time, so that they leave by rows (a lane has four columns, a row is 256 or 512
   // consecutive bytes) in a short loop.  Rows in LDS are 16 bytes more than their 512 apart: the 16 rows of a write are in banks of their own.
   tg_meet();                     // nobody's requests (of steps past the end: zeros) or reads are under way

@@ -68,15 +68,12 @@ __device__ __forceinline__ void tg_settle(u4s_t& a, u4s_t& b) { asm volatile("s_
 __device__ __forceinline__ void tg_settle(u4s_t& a, u4s_t& b, u4s_t& c) { asm volatile("s_nop 4" : "+s"(a), "+s"(b), "+s"(c)); }
 // the descriptor is complete here, not only where it is used
 __device__ __forceinline__ void tg_pin(u4s_t& a) { asm volatile("" : "+s"(a)); }
-// 16 bytes per lane from the buffer to LDS, lane after lane from `lds` (an LDS byte address, the same for the wavefront).  In assembly,
+// 16 bytes per lane from the buffer to LDS, lane after lane from `lds` (an LDS byte address, the same for the wavefront; m0 is set in the statement that goes by it).  In assembly,
 // because of the builtin the compiler waits for all of them in front of the next LDS read, whichever buffer that reads: nothing would be in
-// flight beside the products.  There is no output register; what orders these loads is tg_wait_loads and the barrier behind it.
+// flight beside the products.  There is no output register; what orders these loads is tg_meet.
 __device__ __forceinline__ void tg_load_lds(u4s_t rs, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(rs) : "memory");   // m0: nothing else here uses it
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(rs) : "memory");
 }
-// the same in two parts, with one instruction or more between them
-template <int ADD> __device__ __forceinline__ void tg_aim_lds(uint32_t lds) { asm volatile("s_add_u32 m0, %0, %1" ::"s"(lds), "n"(ADD) : "memory", "scc"); }
-__device__ __forceinline__ void tg_load_aimed(u4s_t rs, uint32_t off) { asm volatile("buffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(rs) : "memory"); }
 // this wavefront's loads but the N youngest are in LDS and its LDS reads done; then everybody's are
 template <int N = 0>
 __device__ __forceinline__ void tg_meet() {

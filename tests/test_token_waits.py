@@ -1,6 +1,8 @@
-"""The machine code of the token operators' products, as it lies in the library, against what hardware leaves to the program and the compiler
+"""The machine code of the token operators' products, as it lies in the library, against three rules that hardware leaves to the program and the compiler
 keeps only in its own instructions, not in written-out ones (no GPU needed):
-  * a scalar register that a vector instruction wrote is not read by a memory instruction within five wait states."""
+  * a scalar register that a vector instruction wrote is not read by a memory instruction within five wait states;
+  * between the setting of m0 and the load into LDS that goes by it nothing else sets m0, and one wait state passes;
+  * an accumulation register is read by another instruction than a product 19 wait states (those of the longest product) behind the last one at the earliest."""
 import os
 import re
 import shutil
@@ -83,13 +85,56 @@ def early_reads(code):
     return bad
 
 
+def loads_off_m0(code):
+    """loads into LDS without their own setting of m0 in the three instructions in front"""
+    bad = []
+    for i, (op, operands) in enumerate(code):
+        if op.startswith("buffer_load") and operands.endswith("lds"):
+            near = code[max(0, i - 3):i]
+            sets = [k for k, (_, o) in enumerate(near) if o.split(",")[0].strip() == "m0"]
+            if len(sets) != 1 or sum(waits(*c) for c in near[sets[0] + 1:]) < 1:
+                bad.append((near, operands))
+    return bad
+
+
+def early_sums(code):
+    """reads of accumulation registers, or copies of them, too close behind the products that wrote them"""
+    wrote, now, bad = {}, 0, []
+    for op, operands in code:
+        regs = [range(int(m[1] or m[2]), int(m[1] or m[3]) + 1) for m in re.finditer(r"\ba(?:(\d+)|\[(\d+):(\d+)\])", operands)]
+        if op.startswith("v_mfma"):
+            for r in regs[0] if regs and operands.startswith("a") else ():
+                wrote[r] = now
+        else:
+            bad += [(op, operands, r) for s in regs for r in s if r in wrote and now - wrote[r] - 1 < 19]
+        now += waits(op, operands)
+    return bad
+
+
 def test_the_scan_sees_what_it_looks_for():
     code = [["v_readfirstlane_b32", "s22, v2"], ["s_mov_b32", "m0, s37"], ["s_nop", "0"], ["buffer_load_dwordx4", "v125, s[20:23], 0 offen lds"]]
-    assert early_reads(code) == [("buffer_load_dwordx4", "v125, s[20:23], 0 offen lds", 22, 2)]
+    assert early_reads(code) == [("buffer_load_dwordx4", "v125, s[20:23], 0 offen lds", 22, 2)] and not loads_off_m0(code)
     assert not early_reads(code[:1] + [["s_nop", "2"]] + code[1:]) and not early_reads(code[:1] + [["s_mov_b32", "s22, s3"]] + code[1:])
+    assert loads_off_m0(code[:2] + code[3:]) and loads_off_m0(code[:1] + code[2:]) and loads_off_m0(code[:2] + code[1:])
+    code = [["v_mfma_f32_16x16x32_bf16", "a[0:3], v[14:17], v[62:65], a[0:3]"], ["s_nop", "15"], ["v_accvgpr_read_b32", "v1, a2"]]
+    assert early_sums(code) == [("v_accvgpr_read_b32", "v1, a2", 2)] and early_sums(code[:2] + [["ds_write_b128", "v5, a[0:3]"]])
+    assert not early_sums(code[:2] + code[1:]) and not early_sums(code[:2] + [["v_accvgpr_read_b32", "v1, a4"]])
 
 
 def test_descriptors_have_settled_when_loads_read_them(kernels):
     bad = {name: early_reads(code)[:2] for name, code in kernels.items()}
     bad = {k: v for k, v in bad.items() if v}
     assert not bad, (len(bad), list(bad.items())[:3])
+
+
+def test_loads_into_lds_go_by_their_own_m0(kernels):
+    assert all(any(o.endswith("lds") for _, o in code) for name, code in kernels.items())
+    bad = {name: loads_off_m0(code)[:2] for name, code in kernels.items()}
+    assert not any(bad.values()), [(k, v) for k, v in bad.items() if v][:3]
+
+
+def test_sums_are_read_when_they_are_there(kernels):
+    large = {name: code for name, code in kernels.items() if "tg_big_k" in name}
+    assert len(large) == 10 and all(any(op.startswith("v_mfma") and o.startswith("a[") for op, o in code) for code in large.values())
+    bad = {name: early_sums(code)[:2] for name, code in large.items()}
+    assert not any(bad.values()), [(k, v) for k, v in bad.items() if v][:3]
