@@ -302,6 +302,9 @@ TgPlan tg_plan(int dt, int epi, int M, int N, int K, size_t max_bytes) {
     if (!c.tile) break;
     const int bn = epi == TG_GLU ? c.tile / 2 : c.tile;
     const double tiles = (double)((M + c.tile - 1) / c.tile) * ((N + bn - 1) / bn);
+    // A launch of 2^32 threads or more is cut off without an error: 2^29 rows and more, of a few columns, are too many tiles of 64.  (With 8: the padding of a
+    // group's jobs.  Tiles of 128 take 2^31 rows, and more columns than the memory holds.)
+    if ((tiles + 8) * (c.tile == 64 ? 512 : 256) >= 4294967296.0) continue;
     for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
       const size_t part = tg_part_bytes(epi, M, N, s);
       if (s > 1 && (steps < 4 * s || part > max_bytes)) break;

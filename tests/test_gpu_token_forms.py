@@ -148,3 +148,66 @@ def test_infinities_beside_pad_columns(env, dtype, rows, d, f):
         # gradients of the gate and up weights take the row, those of the down weights in the row of the infinite column
         assert bool((got["dg"] == float("inf")).all()) and bool((got["du"] == float("inf")).all())
         assert bool((got["dd"][3] == float("inf")).all()) and torch.equal(got["dd"][4:], plain["dd"][4:])
+
+
+# ---- the longest calls ------------------------------------------------------------------------------------------------------------------
+def pieces(n, step=1 << 27):
+    return [slice(i, min(n, i + step)) for i in range(0, n, step)]
+
+
+@pytest.mark.parametrize("dtype", T.DTYPES)
+def test_linear_layer_of_more_than_half_a_billion_rows(env, dtype):
+    """More threads than a launch takes if the tiles were small.  One column in and out: y = x w, dx = dy w, both rounded once; dw and db of whole numbers, exact."""
+    torch, P, R = env
+    tdt, code = T.types(P, torch, dtype)
+    sp = torch.cuda.current_stream().cuda_stream
+    rows = (1 << 29) + 67
+    x, dy = (torch.empty(rows, 1, dtype=tdt, device="cuda") for _ in range(2))
+    for i in pieces(rows):
+        at = torch.arange(i.start, i.stop, device="cuda")
+        x[i, 0] = (at % 97 - 48).to(tdt)
+        dy[i, 0] = ((at * 7) % 5 - 2).to(tdt) * ((at & 1023) == 0).to(tdt)          # half a million that are not zero: sums below 2^24
+    w = torch.full((1, 1), 1.5, dtype=tdt, device="cuda")
+    y, dx = (torch.empty(rows, 1, dtype=tdt, device="cuda") for _ in range(2))
+    dw, db = torch.empty(1, 1, device="cuda"), torch.empty(1, device="cuda")
+    a = P.linear_args(rows=rows, n_in=1, n_out=1, dtype=code, x=x, ldx=1, w=w, ldw=1, y=y, ldy=1, dy=dy, lddy=1, dx=dx, lddx=1, dw=dw, dbias=db)
+    ws = torch.empty(max(P.linear_workspace(a), P.linear_workspace(a, True)), dtype=torch.uint8, device="cuda")
+    a.ws, a.ws_bytes = ws.data_ptr(), ws.numel()
+    P.linear_forward(a, sp)
+    P.linear_backward(a, sp)
+    torch.cuda.synchronize()
+    want_w = want_b = 0
+    for i in pieces(rows):
+        assert torch.equal(y[i].float(), x[i].float() * 1.5) and torch.equal(dx[i].float(), dy[i].float() * 1.5)
+        want_w += int((x[i].float() * dy[i].float()).long().sum())
+        want_b += int(dy[i].long().sum())
+    assert float(dw) == want_w and float(db) == want_b
+
+
+def test_gated_block_of_more_than_half_a_billion_rows(env):
+    """One column: gate = x, up = 2 x, hidden = 2 x^2, y = x^2; dhidden = dy / 2, dgate = dy x, dup = dy x / 2, dx = 2 dy x."""
+    torch, P, R = env
+    sp = torch.cuda.current_stream().cuda_stream
+    bf, rows = torch.bfloat16, (1 << 29) + 67
+    x, dy = (torch.empty(rows, 1, dtype=bf, device="cuda") for _ in range(2))
+    for i in pieces(rows):
+        at = torch.arange(i.start, i.stop, device="cuda")
+        x[i, 0] = (at % 15 - 7).to(bf)
+        dy[i, 0] = ((at * 7) % 5 - 2).to(bf) * ((at & 4095) == 0).to(bf)
+    one, two, half = (torch.full((1, 1), v, dtype=bf, device="cuda") for v in (1.0, 2.0, 0.5))
+    y, dx, gate, up = (torch.empty(rows, 1, dtype=bf, device="cuda") for _ in range(4))
+    dw = [torch.empty(1, 1, device="cuda") for _ in range(3)]
+    a = P.ffn_args(rows=rows, width=1, hidden=1, dtype=P.BF16, act=P.ACT_NONE, save=P.SAVE_FULL, gate=gate, up=up, x=x, ldx=1, w_gate=one, ldwg=1, w_up=two, ldwu=1,
+                   w_down=half, ldwd=1, y=y, ldy=1, dy=dy, lddy=1, dx=dx, lddx=1, dw_gate=dw[0], dw_up=dw[1], dw_down=dw[2])
+    ws = torch.empty(max(P.ffn_workspace(a), P.ffn_workspace(a, True)), dtype=torch.uint8, device="cuda")
+    a.ws, a.ws_bytes = ws.data_ptr(), ws.numel()
+    P.ffn_forward(a, sp)
+    P.ffn_backward(a, sp)
+    torch.cuda.synchronize()
+    want = [0.0, 0.0, 0.0]
+    for i in pieces(rows):
+        xi, di = x[i].float(), dy[i].float()
+        assert torch.equal(y[i].float(), xi * xi) and torch.equal(gate[i], x[i]) and torch.equal(up[i].float(), 2 * xi) and torch.equal(dx[i].float(), 2 * di * xi)
+        p = float((di * xi * xi).double().sum())
+        want = [want[0] + p, want[1] + p / 2, want[2] + 2 * p]
+    assert [float(v) for v in dw] == want
