@@ -477,7 +477,8 @@ void tk_embed_bwd(int dt, hipStream_t st, const void* ids, int ids64, int64_t n6
   const dim3 g((runs + per - 1) / per, slabs);
   if (dt == 1) hipLaunchKernelGGL(embed_sum_k<bf16_t>, g, dim3(256), lds, st, k0, p0, n, width, shift, scale, (const bf16_t*)dy, lddy, dtable, lddt, accumulate, part);
   else hipLaunchKernelGGL(embed_sum_k<float>, g, dim3(256), lds, st, k0, p0, n, width, shift, scale, (const float*)dy, lddy, dtable, lddt, accumulate, part);
-  if (runs > 1) hipLaunchKernelGGL(embed_join_k, dim3(runs, slabs), dim3(std::max(64, 1 << shift)), 0, st, k0, n, width, scale, dtable, lddt, accumulate, part);
+  // (the last run has none behind it to add; all 2^26 of 2^30 rows would be more threads than a launch takes)
+  if (runs > 1) hipLaunchKernelGGL(embed_join_k, dim3(runs - 1, slabs), dim3(std::max(64, 1 << shift)), 0, st, k0, n, width, scale, dtable, lddt, accumulate, part);
 }
 
 // ---------------------------------------------------------------- activations in 8 bits

@@ -211,3 +211,25 @@ def test_gated_block_of_more_than_half_a_billion_rows(env):
         p = float((di * xi * xi).double().sum())
         want = [want[0] + p, want[1] + p / 2, want[2] + 2 * p]
     assert [float(v) for v in dw] == want
+
+
+def test_table_gradient_of_a_billion_tokens(env):
+    """The most rows a call takes.  Whole numbers, so that sums are exact."""
+    torch, P, R = env
+    sp = torch.cuda.current_stream().cuda_stream
+    rows, vocab = 1 << 30, 1 << 16
+    ids, dy = torch.empty(rows, dtype=torch.int32, device="cuda"), torch.empty(rows, 1, dtype=torch.bfloat16, device="cuda")
+    want = torch.zeros(vocab, device="cuda")
+    for i in pieces(rows):
+        at = torch.arange(i.start, i.stop, device="cuda")
+        k = (at * 40503 + (at >> 16)) % vocab
+        ids[i] = k
+        dy[i, 0] = ((at * 13) % 7 - 3).to(torch.bfloat16)
+        want.index_add_(0, k, dy[i, 0].float())
+    g = torch.full((vocab, 1), 5.0, device="cuda")
+    a = P.embed_args(rows=rows, vocab=vocab, width=1, dtype=P.BF16, scale=1.0, ids=ids, dy=dy, lddy=1, dtable=g, lddt=1)
+    ws = torch.empty(P.embed_backward_workspace(a), dtype=torch.uint8, device="cuda")
+    a.ws, a.ws_bytes = ws.data_ptr(), ws.numel()
+    P.embed_backward(a, sp)
+    torch.cuda.synchronize()
+    assert torch.equal(g[:, 0], want)
