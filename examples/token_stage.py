@@ -1,6 +1,9 @@
 """A token model trained as pipeline stages train: a table, gated feed-forward blocks and a head, two micro-batches in flight whose activations are
 held in 8 bits, weight gradients accumulated in fp32, then one token at a time through the trained weights.
 
+What a batch in flight holds between its forward and its backward is its ids, its logits, and in 8 bits every block's gate and up rows and input and the head's
+input; the bfloat16 rows that go from unit to unit, their gradients and the workspace are the stage's, there once whichever batch is at work.
+
 The task is a fixed permutation of the vocabulary (the token behind each token), so that a model without attention can learn it.
 
     python examples/token_stage.py            # needs an MI355X
@@ -51,69 +54,91 @@ class Model:
         return [self.table, self.head] + [w for b in self.blocks for w in b.values()]
 
 
-class Slot:
-    """One batch in flight: its buffers, its stash and the calls' records, made once."""
+class Rows:
+    """What passes from unit to unit, two buffers in turn: activations and (for training) their gradients."""
 
     def __init__(self, m, rows, train=True):
-        d, f, v, self.rows = m.width, m.hidden, m.vocab, rows
-        groups = lambda n: -(-n // 32)  # noqa: E731
-        self.ids, self.labels = dev(rows, dtype=torch.int32), dev(rows, dtype=torch.int32)
-        self.x = [dev(rows, d) for _ in range(len(m.blocks) + 1)]
-        self.logits, self.loss = dev(rows, v), torch.zeros(1, device="cuda")
-        keep = self.keep = []
-        self.embed = P.embed_args(rows=rows, vocab=v, width=d, dtype=P.BF16, scale=d ** 0.5, ids=self.ids, table=m.table.work, ldt=d, out=self.x[0], ldo=d)
-        self.ffn = []
-        for i, b in enumerate(m.blocks):
-            a = P.ffn_args(rows=rows, width=d, hidden=f, dtype=P.BF16, act=P.ACT_SILU, x=self.x[i], ldx=d, w_gate=b["gate"].work, ldwg=d, w_up=b["up"].work,
-                           ldwu=d, w_down=b["down"].work, ldwd=f, residual=self.x[i], ldr=d, y=self.x[i + 1], ldy=d)
-            if train:
-                gate, up, gs, us = dev(rows, f, dtype=torch.uint8), dev(rows, f, dtype=torch.uint8), dev(rows, groups(f), dtype=torch.uint8), dev(rows, groups(f), dtype=torch.uint8)
-                keep += [gate, up, gs, us]
-                a.save, a.gate, a.up, a.gate_scales, a.up_scales = P.SAVE_ACT8, gate.data_ptr(), up.data_ptr(), gs.data_ptr(), us.data_ptr()
-                a.dw_gate, a.dw_up, a.dw_down = (b[k].grad.data_ptr() for k in ("gate", "up", "down"))
-                a.accumulate, a.dx_residual = 1, 1
-            self.ffn.append(a)
-        self.out = P.linear_args(rows=rows, n_in=d, n_out=v, dtype=P.BF16, x=self.x[-1], ldx=d, w=m.head.work, ldw=d, bias=m.bias, y=self.logits, ldy=v)
-        ws = max([P.linear_workspace(self.out)] + [P.ffn_workspace(a) for a in self.ffn])
-        if train:
-            # what the forward leaves for the backward of a block besides gate and up is its input: held in 8 bits too, so that the bfloat16 rows can go
-            self.pack = []
-            for x in self.x[:-1]:
-                q, s = dev(rows, d, dtype=torch.uint8), dev(rows, groups(d), dtype=torch.uint8)
-                keep += [q, s]
-                self.pack.append(P.act8_args(rows=rows, cols=d, dtype=P.BF16, x=x, ldx=d, q=q, ldq=d, scales=s, lds=groups(d)))
-            self.dlogits, self.dx = dev(rows, v), [dev(rows, d) for _ in range(2)]
-            o = self.out
-            o.dy, o.lddy, o.dx, o.lddx, o.dw, o.dbias, o.accumulate = self.dlogits.data_ptr(), v, self.dx[0].data_ptr(), d, m.head.grad.data_ptr(), m.bias_grad.data_ptr(), 1
-            ws = max([ws, P.linear_workspace(o, True)] + [P.ffn_workspace(self.backward_record(i), True) for i in range(len(self.ffn))])
-            e = self.embed
-            e.lddy, e.dy, e.dtable, e.lddt, e.accumulate = d, self.dx[len(self.ffn) % 2].data_ptr(), m.table.grad.data_ptr(), d, 1
-            ws = max(ws, P.embed_backward_workspace(e))
-        self.ws = dev(ws + 1, dtype=torch.uint8)
-        for a in [self.embed, self.out, *self.ffn]:
-            a.ws, a.ws_bytes = self.ws.data_ptr(), ws
+        self.x = [dev(rows, m.width) for _ in range(2)]
+        self.dx = [dev(rows, m.width) for _ in range(2)] if train else []
+        self.ws = None
 
-    def backward_record(self, i):
-        """the block's record with its input in 8 bits and the gradients' places"""
-        a, p, d = type(self.ffn[i]).from_buffer_copy(self.ffn[i]), self.pack[i], self.x[0].shape[1]
-        n = len(self.ffn) - 1 - i
-        a.x, a.ldx, a.x_scales, a.ldxs = p.q, d, p.scales, p.lds
-        a.dy, a.lddy, a.dx, a.lddx = self.dx[n % 2].data_ptr(), d, self.dx[(n + 1) % 2].data_ptr(), d
+    def space(self, n):
+        """at least n bytes of workspace, the same for all calls: they follow one another on one stream"""
+        if self.ws is None or self.ws.numel() < n:
+            self.ws = dev(max(n, 1), dtype=torch.uint8)
+        return self.ws
+
+
+class Slot:
+    """One batch in flight: its stash and the calls' records, made once."""
+
+    def __init__(self, m, rows, between, train=True):
+        d, f, v, n = m.width, m.hidden, m.vocab, len(m.blocks)
+        groups = lambda k: -(-k // 32)  # noqa: E731
+        self.rows, self.train = rows, train
+        self.ids, self.labels = dev(rows, dtype=torch.int32), dev(rows, dtype=torch.int32)
+        self.logits, self.loss = dev(rows, v), torch.zeros(1, device="cuda")
+        self.keep = []
+
+        def held(k):
+            q, s = dev(rows, k, dtype=torch.uint8), dev(rows, groups(k), dtype=torch.uint8)
+            self.keep += [q, s]
+            return q.data_ptr(), s.data_ptr()
+        x, dx = [between.x[i % 2] for i in range(n + 1)], between.dx
+        self.embed = P.embed_args(rows=rows, vocab=v, width=d, dtype=P.BF16, scale=d ** 0.5, ids=self.ids, table=m.table.work, ldt=d, out=x[0], ldo=d)
+        self.blocks = []
+        for i, b in enumerate(m.blocks):
+            a = P.ffn_args(rows=rows, width=d, hidden=f, dtype=P.BF16, act=P.ACT_SILU, x=x[i], ldx=d, w_gate=b["gate"].work, ldwg=d, w_up=b["up"].work, ldwu=d,
+                           w_down=b["down"].work, ldwd=f, residual=x[i], ldr=d, y=x[i + 1], ldy=d)
+            if train:
+                a.save = P.SAVE_ACT8
+                (a.gate, a.gate_scales), (a.up, a.up_scales) = held(f), held(f)
+            self.blocks.append(a)
+        self.head = P.linear_args(rows=rows, n_in=d, n_out=v, dtype=P.BF16, x=x[n], ldx=d, w=m.head.work, ldw=d, bias=m.bias, y=self.logits, ldy=v)
+        calls, most = [self.embed, *self.blocks, self.head], max([P.linear_workspace(self.head)] + [P.ffn_workspace(a) for a in self.blocks])
+        if train:
+            # the inputs of the blocks and of the head, in 8 bits: the backward's records read these instead of the rows, which the next unit but one overwrites
+            self.pack = []
+            for rows_in in x:
+                q, s = held(d)
+                self.pack.append(P.act8_args(rows=rows, cols=d, dtype=P.BF16, x=rows_in, ldx=d, q=q, ldq=d, scales=s, lds=groups(d)))
+            self.dlogits = dev(rows, v)
+            self.head_back = self.from_stash(self.head, n, self.dlogits, v, dx[n % 2], dw=m.head.grad, dbias=m.bias_grad)
+            self.blocks_back = [self.from_stash(a, i, dx[(i + 1) % 2], d, dx[i % 2], dx_residual=1, dw_gate=b["gate"].grad, dw_up=b["up"].grad, dw_down=b["down"].grad)
+                                for i, (a, b) in enumerate(zip(self.blocks, m.blocks))]
+            e = self.embed
+            e.dy, e.lddy, e.dtable, e.lddt, e.accumulate = dx[0].data_ptr(), d, m.table.grad.data_ptr(), d, 1
+            calls += [self.head_back, *self.blocks_back]
+            most = max([most, P.linear_workspace(self.head_back, True), P.embed_backward_workspace(e)] + [P.ffn_workspace(a, True) for a in self.blocks_back])
+        ws = between.space(most)
+        self.keep.append(ws)
+        for a in calls:
+            a.ws, a.ws_bytes = ws.data_ptr(), ws.numel()
+
+    def from_stash(self, record, unit, dy, lddy, dx, **gradients):
+        """the backward's record of a unit: its input as the slot holds it, its gradients added to what is there"""
+        a, p = type(record).from_buffer_copy(record), self.pack[unit]
+        a.x, a.ldx, a.x_scales, a.ldxs = p.q, p.ldq, p.scales, p.lds
+        a.dy, a.lddy, a.dx, a.lddx, a.accumulate = dy.data_ptr(), lddy, dx.data_ptr(), p.cols, 1
+        for name, g in gradients.items():
+            setattr(a, name, g.data_ptr() if hasattr(g, "data_ptr") else g)
         return a
 
-    def forward(self, stream, train=True):
+    def forward(self, stream):
         P.embed_forward(self.embed, stream)
-        for i, a in enumerate(self.ffn):
-            P.ffn_forward(a, stream)
-            if train:
+        for i, a in enumerate(self.blocks):
+            if self.train:
                 P.act8_pack(self.pack[i], stream)
-        P.linear_forward(self.out, stream)
+            P.ffn_forward(a, stream)
+        if self.train:
+            P.act8_pack(self.pack[-1], stream)
+        P.linear_forward(self.head, stream)
 
     def backward(self, stream):
         P.softmax_ce_static(self.logits, self.labels, self.rows, self.logits.shape[1], P.BF16, self.dlogits, self.loss, stream)
-        P.linear_backward(self.out, stream)
-        for i in reversed(range(len(self.ffn))):
-            P.ffn_backward(self.backward_record(i), stream)
+        P.linear_backward(self.head_back, stream)
+        for a in reversed(self.blocks_back):
+            P.ffn_backward(a, stream)
         P.embed_backward(self.embed, stream)
 
 
@@ -122,7 +147,8 @@ def train(steps=60, rows=512, lr=0.2, verbose=True):
     m = Model()
     gen = torch.Generator(device="cuda").manual_seed(2)
     behind = torch.randperm(m.vocab, generator=gen, device="cuda").to(torch.int32)
-    slots = [Slot(m, rows) for _ in range(2)]
+    between = Rows(m, rows)
+    slots = [Slot(m, rows, between) for _ in range(2)]
     stream, losses = torch.cuda.current_stream().cuda_stream, []
     for step in range(steps):
         for s in slots:
@@ -143,11 +169,11 @@ def train(steps=60, rows=512, lr=0.2, verbose=True):
 
 def follow(m, first, n):
     """n tokens from `first` on, one at a time"""
-    s = Slot(m, 1, train=False)
+    s = Slot(m, 1, Rows(m, 1, train=False), train=False)
     stream, got = torch.cuda.current_stream().cuda_stream, []
     s.ids.fill_(first)
     for _ in range(n):
-        s.forward(stream, train=False)
+        s.forward(stream)
         s.ids.copy_(s.logits.argmax(1))
         got.append(int(s.ids))
     return got
