@@ -206,9 +206,10 @@ __device__ __forceinline__ void tg_rows(const TgJob& p, int split, const float* 
 // behind the last read of the step's operands.
 // The instruction is written out because the sums fill all accumulation registers: compiled from the builtin a dozen of them are copied away
 // and back in every step.
-// Bound by the matrix cores and, with data that is not zeros, by the card's power: a gated block of 8192 rows, 4096 x 14336, runs its products at 1290
-// (gate and up with their 8-bit form), 1060 (their gradients), 1410 (down; dx) and 1320 TFLOP/s (weight gradients); a library product of the three operand
-// orders at 1435 to 1617, 1160 to 1390 and 960 to 1185.  The matrix cores are busy 74 to 79 % of the cycles, waits are 12 %.  Requests and reads in front of
+// Bound by the matrix cores and, with data that is not zeros, by the card's power: a gated block of 8192 rows, 4096 x 14336, runs its products at 1280
+// (gate and up with their 8-bit form), 1095 (their gradients), 1500 (down), 1410 (dx) and 1255 TFLOP/s (weight gradients); a library product of the three operand
+// orders at 1435 to 1617, 1160 to 1390 and 960 to 1185.  The matrix cores are busy 80, 71 and 68 % of the cycles in the three operand orders, 9, 12 and 15 % of the
+// wavefronts' are waits (a library product's: 87, 70, 52 and 4, 9, 11; profiles/token_pmc_matrix.txt).  Requests and reads in front of
 // eight products instead of one between two: 4096 x 4096 x 16384 439 us instead of 405; products of 32 x 32 x 16: 441 for 418.
 template <int LAY, int EPI, bool PART>
 __global__ __launch_bounds__(256, 1) void tg_big_k(const TgGroup grp) {

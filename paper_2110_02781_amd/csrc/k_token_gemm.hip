@@ -122,7 +122,7 @@ __device__ __forceinline__ void tg_results(const TgJob& p, f4v_t (&acc)[S][T], i
 // The small tiles.  KG 2: twice the wavefronts, of which one half takes the first 64 bytes of a step's reduction and the other half the second, and
 // which add up at the end: two to a SIMD where one alone waits for every LDS read, every meeting and its own last products (1024 x 1024 x 4096
 // bfloat16 in tiles of 64 19.5 us, 23 with one half).  fp32 is bound by its matrix instruction, 150 TFLOP/s at best, beside which no vector instruction
-// runs: 517 x 1024 x 5632 in 79 us, 1000 x 777 x 1001 (208 tiles for 256 CUs) in 29.
+// runs: 517 x 1024 x 5632 in 74 us, 1000 x 777 x 1001 (208 tiles for 256 CUs) in 28.
 template <typename E, int LAY, int EPI, int BM, int BN, int WM, int WN, int KG, bool PART>
 __global__ __launch_bounds__(64 * WM * WN * KG) void tg_gemm_k(const TgGroup grp) {
   typedef TgBlock<E, LAY, EPI, BM, BN, WM * WN * KG> B;
