@@ -419,9 +419,9 @@ def _calls(s):
         given(a, top=c["top"], top_ids=new("top_ids", rows, c["top"], dtype=torch.int32), top_logp=new("top_logp", rows, c["top"], dtype=f32))
     if not train:
         return [(P.logp_forward, a)], out, spaced(a, P.logp_workspace(a))
-    lse = torch.empty(rows, dtype=f32, device="cuda")
-    given(a, lse=lse, dlogp=s["dlogp"], dentropy=s["dentropy"], dlogits=new("dlogits", rows, v), lddl=v)
-    return [(P.logp_forward, a), (P.logp_backward, a)], out, (lse, spaced(a, P.logp_workspace(a)))
+    stats = torch.empty(rows, 2, dtype=f32, device="cuda")
+    given(a, stats=stats, dlogp=s["dlogp"], dentropy=s["dentropy"], dlogits=new("dlogits", rows, v), lddl=v)
+    return [(P.logp_forward, a), (P.logp_backward, a)], out, (stats, spaced(a, P.logp_workspace(a)))
 
 
 def run(state):
