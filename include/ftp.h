@@ -431,6 +431,144 @@ typedef struct {
 int ftp_act8_pack(const ftp_act8_args*, void* stream);
 int ftp_act8_unpack(const ftp_act8_args*, void* stream);
 
+/* What stands between the products: dropout, the join of a block's output with the stream and the norms around it, a gated linear
+ * recurrence along the sequences, log probabilities of tokens.  Rows, types, strides, workspaces and results as above; no stride
+ * has to be aligned and nothing is copied.  `seed`, `seed_dev`, `site`, `row0`, `p` name a mask wherever there is one. */
+
+/* A mask of dropout is never stored: it is made again wherever it is needed, by the counter-based generator Philox4x32-10 (Salmon,
+ * Moraes, Dror, Shaw: Parallel random numbers: as easy as 1, 2, 3; 2011).  Columns 8 j .. 8 j + 7 of a row have the counter (j, site,
+ * low and high word of row0 + row) under the key seed + *seed_dev (modulo 2^64, low word first; seed_dev NULL: seed); column
+ * 8 j + i has 16 bits of word i / 2, the low ones where i is even.  Values whose bits are below q = round(65536 p) become 0 (also infinities
+ * and NaN), others are multiplied by 65536 / (65536 - q).  So a mask goes by seed, site and row number alone: a call on some of the rows, a
+ * backward and a recomputation have the same one, and a captured call gets a new one with what is written at seed_dev.
+ * p: 0 <= p, q < 65536 (0: nothing is dropped).
+ * Forward: y = dropped x + residual.  Backward: dx = dropped dy.  y may be the buffer of x or of the residual, dx that of dy. */
+typedef struct {
+  int64_t rows;
+  int32_t cols, dtype;
+  float p;
+  uint32_t site;
+  uint64_t seed;
+  const uint64_t* seed_dev;
+  int64_t row0;           /* number of the first row, >= 0                          */
+  const void* x; int64_t ldx;
+  const void* residual; int64_t ldr;
+  void* y; int64_t ldy;
+  const void* dy; int64_t lddy;
+  void* dx; int64_t lddx;
+} ftp_dropout_args;
+int ftp_dropout_forward(const ftp_dropout_args*, void* stream);
+int ftp_dropout_backward(const ftp_dropout_args*, void* stream);
+
+/* Between two blocks of a model: with the stream x, the block's output b and norm(v) = (v - mean) / sqrt(var + eps) of a row
+ * (FTP_NORM_LAYER) or v / sqrt(mean of squares + eps) (FTP_NORM_RMS),
+ *   c = norm(b) * post_w + post_bias (with `post`; otherwise b),   y = x + scale * gate * dropped c,   n = norm(y) * pre_w + pre_bias.
+ * x NULL: 0; b NULL: y = x (and n is x normed: the call in front of the first block).  Weights fp32 [width], NULL: 1; biases NULL: 0.
+ * gate [ceil(rows / gate_rows)][width] of gate_dtype (fp32 or dtype): row t takes row t / gate_rows; NULL: 1.
+ * y and n each where wanted; n is of y before it is rounded.  y may be the buffer of x or of b.
+ * Backward, from x, b, gate and the weights (statistics and y are computed again): of dy, which arrives at y, and dn, which arrives at n
+ * (one of the two may be NULL), dx, db, dgate (of gate_dtype) and the weights' gradients (fp32 [width]), each where wanted; those of pre_w
+ * and pre_bias need dn.  `accumulate`: the weights' gradients are added to what is there; `gate_accumulate`: dgate is (fp32 only).
+ * dx may be the buffer of dy. */
+typedef enum { FTP_NORM_RMS = 0, FTP_NORM_LAYER = 1 } ftp_norm;
+typedef struct {
+  int64_t rows;
+  int32_t width, dtype;
+  int32_t norm;           /* ftp_norm                                               */
+  int32_t post;
+  float eps;              /* > 0, finite                                            */
+  float scale;            /* finite                                                 */
+  float p;                /* the mask of c, as above                                */
+  uint32_t site;
+  uint64_t seed;
+  const uint64_t* seed_dev;
+  int64_t row0;
+  const void* x; int64_t ldx;
+  const void* b; int64_t ldb;
+  const float *post_w, *post_bias;
+  const void* gate; int64_t ldg;
+  int64_t gate_rows;      /* >= 1 with a gate                                       */
+  int32_t gate_dtype, gate_accumulate;
+  void* y; int64_t ldy;
+  const float *pre_w, *pre_bias;
+  void* n; int64_t ldn;
+  const void* dy; int64_t lddy;
+  const void* dn; int64_t lddn;
+  void* dx; int64_t lddx;
+  void* db; int64_t lddb;
+  void* dgate; int64_t lddg;
+  float *dpost_w, *dpost_bias, *dpre_w, *dpre_bias;
+  int32_t accumulate;
+  void* ws; size_t ws_bytes;
+} ftp_join_args;
+int ftp_join_forward(const ftp_join_args*, void* stream);              /* without a workspace */
+int ftp_join_workspace(const ftp_join_args*, size_t* bytes);           /* the backward's      */
+int ftp_join_backward(const ftp_join_args*, void* stream);
+
+/* Gated linear recurrence, column by column along each sequence:
+ *   a = sigmoid(f),   h[t] = a[t] h[t-1] + c(a[t]) x[t],   y[t] = h[t] act(g[t])   (g NULL: y = h)
+ * with c = 1 (FTP_SCAN_ADD), 1 - a (FTP_SCAN_MIX) or sqrt(1 - a^2) (FTP_SCAN_UNIT).  Sequence s has the rows starts[s] ..
+ * starts[s+1] - 1 (int32 [seqs + 1] in device memory, not falling, within 0 .. rows; where they are neither, results are undefined but
+ * nothing outside the buffers is touched), or with starts NULL the rows s * length .. of rows = seqs * length.  A sequence may
+ * be empty; rows of no sequence stay as they were in every result.
+ * h0: states in front of the sequences, fp32 [seqs], NULL: 0; h_end: those behind them, where wanted, may be h0's buffer (a step of one
+ * token for each of seqs requests is length = 1).  States inside a call are fp32.
+ * Backward, from f, x, g, h0 (states are computed again): of dy (and dh_end, fp32, NULL: 0) df, dx, dg (with g) and dh0, each where
+ * wanted; dh0 may be dh_end's buffer. */
+typedef enum { FTP_SCAN_ADD = 0, FTP_SCAN_MIX = 1, FTP_SCAN_UNIT = 2 } ftp_scan_form;
+typedef struct {
+  int64_t rows, length;
+  int32_t width, seqs;
+  int32_t dtype, form, act;       /* form: ftp_scan_form                            */
+  const int32_t* starts;
+  const void* f; int64_t ldf;
+  const void* x; int64_t ldx;
+  const void* g; int64_t ldg;
+  const float* h0; int64_t ldh0;
+  void* y; int64_t ldy;
+  float* h_end; int64_t ldhe;
+  const void* dy; int64_t lddy;
+  const float* dh_end; int64_t lddhe;
+  void* df; int64_t lddf;
+  void* dx; int64_t lddx;
+  void* dg; int64_t lddg;
+  float* dh0; int64_t lddh0;
+  void* ws; size_t ws_bytes;
+} ftp_scan_args;
+int ftp_scan_workspace(const ftp_scan_args*, int backward, size_t* bytes);
+int ftp_scan_forward(const ftp_scan_args*, void* stream);
+int ftp_scan_backward(const ftp_scan_args*, void* stream);
+
+/* What a model answers: with z = scale * logits and lse = log(sum of e^z) of a row, logp = z[id] - lse, entropy = -sum of p log p
+ * (p = e^(z - lse)), and the `top` tokens of the largest logits with their log probabilities; each where wanted, fp32 (top_ids int32),
+ * top_ids and top_logp [rows][top] together.  Equal logits: the lower token first.
+ *   - A logit of -inf is a token that cannot come: p = 0, never among the top; places without a token hold -1 and -inf.
+ *   - A row with nothing but -inf: lse and logp -inf, entropy 0, gradient 0.  With NaN or +inf in a row: lse, logp, entropy,
+ *     top_logp and the row's gradient are NaN; top_ids are the largest that are numbers.
+ *   - id = pad_id: logp 0, and dlogp adds nothing; an id that is none of 0 .. vocab-1: logp NaN, and dlogp adds nothing.
+ *   - stats [rows][2]: what the backward needs, the row's largest logit and lse - scale * that (lse alone would not tell a row of the type's
+ *     lowest value from one token).
+ * Backward, from logits, stats and (with dentropy) entropy: dlogits = scale * (dlogp ([v = id] - p) - dentropy p (log p + entropy)) of
+ * dlogp and dentropy, fp32 [rows], one of which may be NULL.  dlogits may be the logits' buffer. */
+typedef struct {
+  int64_t rows;
+  int32_t vocab, dtype;
+  int32_t ids64;          /* ids are int64 (otherwise int32)                        */
+  int32_t top;            /* 0 .. 64                                                */
+  float scale;            /* > 0, finite                                            */
+  int64_t pad_id;
+  const void* logits; int64_t ldl;
+  const void* ids;
+  float *logp, *entropy, *lse, *stats;
+  int32_t* top_ids; float* top_logp;
+  const float *dlogp, *dentropy;
+  void* dlogits; int64_t lddl;
+  void* ws; size_t ws_bytes;
+} ftp_logp_args;
+int ftp_logp_workspace(const ftp_logp_args*, size_t* bytes);           /* the forward's       */
+int ftp_logp_forward(const ftp_logp_args*, void* stream);
+int ftp_logp_backward(const ftp_logp_args*, void* stream);             /* without a workspace */
+
 /* ---- diagnostics ---------------------------------------------------------------- */
 
 /* Per-kernel timing for benchmarks (not part of the paper's method).  Between

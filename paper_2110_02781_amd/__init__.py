@@ -11,5 +11,7 @@ from .binding import (  # noqa: F401
     ACT_NONE, ACT_RELU, ACT_RELU6, ACT_SILU, ACT_GELU, SAVE_NONE, SAVE_FULL, SAVE_ACT8,
     embed_args, embed_forward, embed_backward_workspace, embed_backward, linear_args, linear_workspace, linear_forward, linear_backward,
     ffn_args, ffn_workspace, ffn_forward, ffn_backward, act8_args, act8_pack, act8_unpack,
+    NORM_RMS, NORM_LAYER, SCAN_ADD, SCAN_MIX, SCAN_UNIT, dropout_args, dropout_forward, dropout_backward, join_args, join_forward, join_workspace, join_backward,
+    scan_args, scan_workspace, scan_forward, scan_backward, logp_args, logp_workspace, logp_forward, logp_backward,
 )
 from . import models  # noqa: F401

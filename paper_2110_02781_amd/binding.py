@@ -18,6 +18,8 @@ F32, BF16 = 0, 1
 UNIT_CONV, UNIT_INVRES, UNIT_GAP, UNIT_FC, UNIT_LOSS = range(5)
 ACT_NONE, ACT_RELU, ACT_RELU6, ACT_SILU, ACT_GELU = range(5)
 SAVE_NONE, SAVE_FULL, SAVE_ACT8 = range(3)
+NORM_RMS, NORM_LAYER = range(2)
+SCAN_ADD, SCAN_MIX, SCAN_UNIT = range(3)
 
 
 class FtpError(RuntimeError):
@@ -41,7 +43,7 @@ class Sgd(C.Structure):
 
 
 def _record(name, doc, *fields):
-    kinds = {"i": C.c_int32, "l": C.c_int64, "f": C.c_float, "p": C.c_void_p, "z": C.c_size_t}
+    kinds = {"i": C.c_int32, "l": C.c_int64, "f": C.c_float, "p": C.c_void_p, "z": C.c_size_t, "u": C.c_uint32, "w": C.c_uint64}
     return type(name, (C.Structure,), {"__doc__": doc, "_fields_": [(n, kinds[k]) for k, names in fields for n in names.split()]})
 
 
@@ -57,6 +59,23 @@ FfnArgs = _record("FfnArgs", "ftp_ffn_args", ("l", "rows"), ("i", "width hidden 
                   ("l", "lddy"), ("p", "dx"), ("l", "lddx"), ("p", "dw_gate dw_up dw_down ws"), ("z", "ws_bytes"))
 Act8Args = _record("Act8Args", "ftp_act8_args", ("l", "rows"), ("i", "cols dtype"), ("p", "x"), ("l", "ldx"), ("p", "q"), ("l", "ldq"),
                    ("p", "scales"), ("l", "lds"), ("p", "y"), ("l", "ldy"))
+
+
+def _mats(names):
+    """matrices, each with its row distance: "x:ldx y:ldy" """
+    return [(kind, n) for pair in names.split() for kind, n in zip("pl", pair.split(":"))]
+
+
+DropoutArgs = _record("DropoutArgs", "ftp_dropout_args", ("l", "rows"), ("i", "cols dtype"), ("f", "p"), ("u", "site"), ("w", "seed"), ("p", "seed_dev"), ("l", "row0"),
+                      *_mats("x:ldx residual:ldr y:ldy dy:lddy dx:lddx"))
+JoinArgs = _record("JoinArgs", "ftp_join_args", ("l", "rows"), ("i", "width dtype norm post"), ("f", "eps scale p"), ("u", "site"), ("w", "seed"), ("p", "seed_dev"), ("l", "row0"),
+                   *_mats("x:ldx b:ldb"), ("p", "post_w post_bias gate"), ("l", "ldg gate_rows"), ("i", "gate_dtype gate_accumulate"), *_mats("y:ldy"),
+                   ("p", "pre_w pre_bias"), *_mats("n:ldn dy:lddy dn:lddn dx:lddx db:lddb dgate:lddg"), ("p", "dpost_w dpost_bias dpre_w dpre_bias"), ("i", "accumulate"),
+                   ("p", "ws"), ("z", "ws_bytes"))
+ScanArgs = _record("ScanArgs", "ftp_scan_args", ("l", "rows length"), ("i", "width seqs dtype form act"), ("p", "starts"),
+                   *_mats("f:ldf x:ldx g:ldg h0:ldh0 y:ldy h_end:ldhe dy:lddy dh_end:lddhe df:lddf dx:lddx dg:lddg dh0:lddh0"), ("p", "ws"), ("z", "ws_bytes"))
+LogpArgs = _record("LogpArgs", "ftp_logp_args", ("l", "rows"), ("i", "vocab dtype ids64 top"), ("f", "scale"), ("l", "pad_id"), *_mats("logits:ldl"),
+                   ("p", "ids logp entropy lse stats top_ids top_logp dlogp dentropy"), *_mats("dlogits:lddl"), ("p", "ws"), ("z", "ws_bytes"))
 
 
 def _load():
@@ -128,6 +147,17 @@ _SIGS = {
     "ftp_ffn_backward": (_i, [C.POINTER(FfnArgs), _vp]),
     "ftp_act8_pack": (_i, [C.POINTER(Act8Args), _vp]),
     "ftp_act8_unpack": (_i, [C.POINTER(Act8Args), _vp]),
+    "ftp_dropout_forward": (_i, [C.POINTER(DropoutArgs), _vp]),
+    "ftp_dropout_backward": (_i, [C.POINTER(DropoutArgs), _vp]),
+    "ftp_join_forward": (_i, [C.POINTER(JoinArgs), _vp]),
+    "ftp_join_workspace": (_i, [C.POINTER(JoinArgs), C.POINTER(_sz)]),
+    "ftp_join_backward": (_i, [C.POINTER(JoinArgs), _vp]),
+    "ftp_scan_workspace": (_i, [C.POINTER(ScanArgs), _i, C.POINTER(_sz)]),
+    "ftp_scan_forward": (_i, [C.POINTER(ScanArgs), _vp]),
+    "ftp_scan_backward": (_i, [C.POINTER(ScanArgs), _vp]),
+    "ftp_logp_workspace": (_i, [C.POINTER(LogpArgs), C.POINTER(_sz)]),
+    "ftp_logp_forward": (_i, [C.POINTER(LogpArgs), _vp]),
+    "ftp_logp_backward": (_i, [C.POINTER(LogpArgs), _vp]),
     "ftp_ktrace_begin": (_i, [_i]),
     "ftp_ktrace_end": (_i, [C.POINTER(KtraceRow), _i, C.POINTER(_i)]),
 }
@@ -408,6 +438,72 @@ def act8_pack(args, stream=None):
 
 def act8_unpack(args, stream=None):
     _chk(lib.ftp_act8_unpack(C.byref(args), stream))
+
+
+def dropout_args(**kw):
+    return _fill(DropoutArgs(), kw)
+
+
+def dropout_forward(args, stream=None):
+    _chk(lib.ftp_dropout_forward(C.byref(args), stream))
+
+
+def dropout_backward(args, stream=None):
+    _chk(lib.ftp_dropout_backward(C.byref(args), stream))
+
+
+def join_args(**kw):
+    return _fill(JoinArgs(eps=1e-5, scale=1.0), kw)
+
+
+def join_forward(args, stream=None):
+    _chk(lib.ftp_join_forward(C.byref(args), stream))
+
+
+def join_workspace(args):
+    n = _sz(0)
+    _chk(lib.ftp_join_workspace(C.byref(args), C.byref(n)))
+    return n.value
+
+
+def join_backward(args, stream=None):
+    _chk(lib.ftp_join_backward(C.byref(args), stream))
+
+
+def scan_args(**kw):
+    return _fill(ScanArgs(), kw)
+
+
+def scan_workspace(args, backward=False):
+    n = _sz(0)
+    _chk(lib.ftp_scan_workspace(C.byref(args), 1 if backward else 0, C.byref(n)))
+    return n.value
+
+
+def scan_forward(args, stream=None):
+    _chk(lib.ftp_scan_forward(C.byref(args), stream))
+
+
+def scan_backward(args, stream=None):
+    _chk(lib.ftp_scan_backward(C.byref(args), stream))
+
+
+def logp_args(**kw):
+    return _fill(LogpArgs(scale=1.0, pad_id=-1), kw)
+
+
+def logp_workspace(args):
+    n = _sz(0)
+    _chk(lib.ftp_logp_workspace(C.byref(args), C.byref(n)))
+    return n.value
+
+
+def logp_forward(args, stream=None):
+    _chk(lib.ftp_logp_forward(C.byref(args), stream))
+
+
+def logp_backward(args, stream=None):
+    _chk(lib.ftp_logp_backward(C.byref(args), stream))
 
 
 # ---- diagnostics ---------------------------------------------------------------------

@@ -24,6 +24,10 @@ SOURCES = [
     ("k_token_gemm.hip", ["-x", "hip"]),
     ("k_token.hip", ["-x", "hip"]),
     ("token.cpp", ["-x", "hip"]),
+    ("k_join.hip", ["-x", "hip"]),
+    ("k_scan.hip", ["-x", "hip"]),
+    ("k_logp.hip", ["-x", "hip"]),
+    ("between.cpp", ["-x", "hip"]),
     ("stage.cpp", ["-x", "hip"]),
     ("ktrace.cpp", ["-x", "hip"]),
     ("solver.cpp", ["-x", "c++", "-ffp-contract=off"]),

@@ -8,50 +8,6 @@
 
 namespace ftp {
 
-template <typename E>
-__device__ __forceinline__ void tk_load8(const E* p, int left, float v[8]) {     // left: elements that are there
-  if (left >= 8) {
-    const u4v_t a = tk_ld16<E>(p);
-    if constexpr (sizeof(E) == 2) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(a[i] << 16);
-        v[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
-      }
-    } else {
-      const u4v_t b = tk_ld16<E>(p + 4);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) { v[i] = __uint_as_float(a[i]); v[i + 4] = __uint_as_float(b[i]); }
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e < left ? to_f32(p[e]) : 0.f;
-  }
-}
-template <typename E>
-__device__ __forceinline__ void tk_store8(E* p, int left, const float v[8]) {
-  if (left >= 8) {
-    if constexpr (sizeof(E) == 2) {
-      tk_st16<E>(p, u4v_t{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4], v[5]), f32x2_to_bf16x2(v[6], v[7])});
-    } else {
-      tk_st16<E>(p, u4v_t{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
-      tk_st16<E>(p + 4, u4v_t{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])});
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e < left) p[e] = from_f32<E>(v[e]);
-  }
-}
-
-// Calls go out in slices of rows whose vectors are numbered below 2^30, so that the division into row and place is a 32-bit one.
-template <typename F>
-static void by_rows(int64_t rows, int64_t per_row, F f) {
-  const int64_t step = std::max<int64_t>(1, ((int64_t)1 << 30) / std::max<int64_t>(per_row, 1));
-  for (int64_t r = 0; r < rows; r += step) f(r, (int)std::min(step, rows - r));
-}
-static inline unsigned blocks_of(int64_t n, int most) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>((n + 255) / 256, most)); }
-
 // ---------------------------------------------------------------- table lookup
 // out[t] = scale * table[id], 8 columns a thread; a row of NaN where the id is none of the table's.  Memory: 16384 rows of 2048 bfloat16 from 32000
 // take 22 us, 6.1 TB/s of rows read (in part from the caches) and written; 8 rows take a launch, 6.5 us with the call.

@@ -4,33 +4,15 @@
 #include <algorithm>
 #include <cmath>
 
-#include "../../include/ftp.h"
-#include "token.h"
-
-void ftp_set_error(const char* fmt, ...);
+#include "token_check.h"
 
 using namespace ftp;
 
 namespace {
 
-// Refusals: the caller's outputs are untouched, nothing has been launched.
-#define NEED(cond, status, ...)       \
-  do {                                \
-    if (!(cond)) {                    \
-      ftp_set_error(__VA_ARGS__);     \
-      return status;                  \
-    }                                 \
-  } while (0)
-
-// Offsets inside a tile are 31-bit byte offsets: 256 rows of up to 2^20 elements.
-enum { kMaxDim = 1 << 20 };
-const int64_t kMaxRows = (int64_t)1 << 30, kMaxLd = (int64_t)1 << 20;
 // what partial sums of a split reduction may take of the workspace (one product's, all of a call's share it)
 const size_t kPartBytes = (size_t)256 << 20;
 
-inline size_t esize(int dt) { return dt == FTP_BF16 ? 2 : 4; }
-inline int64_t up_to(int64_t v, int64_t a) { return (v + a - 1) / a * a; }
-inline bool at_element(const void* p, int dt) { return (uintptr_t)p % esize(dt) == 0; }
 // fours of columns of a row are aligned
 inline bool fours(const void* p, int64_t ld, size_t es) { return (uintptr_t)p % (4 * es) == 0 && ld % 4 == 0; }
 
@@ -130,32 +112,11 @@ int run(const char* who, int dt, void* ws, size_t ws_bytes, void* stream, F f) {
   return FTP_OK;
 }
 
-int check_common(const char* who, int64_t rows, int dt, int act) {
-  NEED(dt == FTP_F32 || dt == FTP_BF16, FTP_ERR_ARG, "%s: unknown dtype %d", who, dt);
-  NEED(act >= FTP_ACT_NONE && act <= FTP_ACT_GELU, FTP_ERR_ARG, "%s: unknown activation %d", who, act);
-  NEED(rows >= 0 && rows <= kMaxRows, FTP_ERR_ARG, "%s: rows must be 0 .. 2^30", who);
-  return FTP_OK;
-}
-// one matrix: there (unless it has no rows), aligned to its elements, rows at least `cols` apart
-enum { kBytes = -1 };                    // in place of a dtype: a matrix in 8 bits
-int check_mat(const char* who, const char* what, const void* p, int64_t ld, int64_t rows, int64_t cols, int dt, bool optional = false) {
-  if (!p && (optional || rows == 0)) return FTP_OK;
-  NEED(p, FTP_ERR_ARG, "%s: %s is NULL", who, what);
-  NEED(dt == kBytes || at_element(p, dt), FTP_ERR_ARG, "%s: %s is not aligned to its elements", who, what);
-  NEED(ld >= cols && ld <= kMaxLd, FTP_ERR_ARG, "%s: %s has rows %lld apart (at least %lld, at most 2^20)", who, what, (long long)ld, (long long)cols);
-  return FTP_OK;
-}
 int check_grad(const char* who, int dt, int grad_dtype, int accumulate) {
   NEED(grad_dtype == FTP_F32 || grad_dtype == dt, FTP_ERR_ARG, "%s: gradients of the weights are fp32 or of the call's type", who);
   NEED(!accumulate || grad_dtype == FTP_F32, FTP_ERR_UNSUPPORTED, "%s: only fp32 gradients accumulate", who);
   return FTP_OK;
 }
-#define TRY(x)                       \
-  do {                               \
-    const int rc_ = (x);             \
-    if (rc_) return rc_;             \
-  } while (0)
-
 int check_linear(const char* who, const ftp_linear_args* a, bool backward) {
   NEED(a, FTP_ERR_ARG, "%s: NULL argument", who);
   TRY(check_common(who, a->rows, a->dtype, a->act));
@@ -418,13 +379,6 @@ int check_embed(const char* who, const ftp_embed_args* a, bool backward) {
     TRY(check_mat(who, "dy", a->dy, a->lddy, a->rows, a->width, a->dtype));
     TRY(check_mat(who, "dtable", a->dtable, a->lddt, 1, a->width, FTP_F32));
   }
-  return FTP_OK;
-}
-
-int launched(const char* who) {
-  const hipError_t e = hipGetLastError();
-  NEED(e == hipSuccess, FTP_ERR_HIP, "%s: launch failed: %s", who, hipGetErrorString(e));
-  if (const char* why = launch_plan_failure_take()) { ftp_set_error("%s", why); return FTP_ERR_UNSUPPORTED; }
   return FTP_OK;
 }
 

@@ -1,6 +1,8 @@
 // Launch interface of the token kernels: linear layers, gated feed-forward blocks, 8-bit checkpoints, table lookups.
 // Shapes and alignment are the caller's to check (token.cpp); nothing here allocates.
 #pragma once
+#include <algorithm>
+
 #include "kernels.h"
 
 namespace ftp {
@@ -70,5 +72,13 @@ size_t tk_embed_bwd_bytes(int64_t n, int vocab, int width);
 void tk_embed_bwd(int dt, hipStream_t st, const void* ids, int ids64, int64_t n, int vocab, int width, float scale, int64_t pad_id,
                   const void* dy, int64_t lddy, float* dtable, int64_t lddt, int accumulate, void* ws);
 void tk_fill(hipStream_t st, void* p, int64_t rows, int64_t row_bytes, int64_t ld_bytes);
+
+// Calls go out in slices of rows whose vectors are numbered below 2^30, so that the division into row and place is a 32-bit one.
+template <typename F>
+static inline void by_rows(int64_t rows, int64_t per_row, F f) {
+  const int64_t step = std::max<int64_t>(1, ((int64_t)1 << 30) / std::max<int64_t>(per_row, 1));
+  for (int64_t r = 0; r < rows; r += step) f(r, (int)std::min(step, rows - r));
+}
+static inline unsigned blocks_of(int64_t n, int most) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>((n + 255) / 256, most)); }
 
 }  // namespace ftp
