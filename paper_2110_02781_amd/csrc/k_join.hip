@@ -1,4 +1,6 @@
 // Dropout and the join of a block's output with the stream and its norms, forward and backward.
+#include <type_traits>
+
 #include "between.h"
 #include "token_dev.h"
 
@@ -21,18 +23,19 @@ __device__ __forceinline__ MaskKey mask_key(const DropMask& m) {
   const uint64_t s = m.seed + (m.seed_dev ? *m.seed_dev : 0);
   return MaskKey{(uint32_t)s, (uint32_t)(s >> 32)};
 }
-// 0 or the factor of what is kept, for the columns 8 j .. 8 j + 7 of a row
-__device__ __forceinline__ void mask8(const DropMask& m, MaskKey k, uint64_t row, uint32_t j, float f[8]) {
+// the columns 8 j .. 8 j + 7 of a row: all ones where a value is kept, zero where it is dropped
+__device__ __forceinline__ void mask8(const DropMask& m, MaskKey k, uint64_t row, uint32_t j, uint32_t keep[8]) {
+  asm volatile("" : "+s"(k.k0), "+s"(k.k1));             // the rounds' keys are added up by the scalar unit each time; kept, they would take twenty registers
   const uint4 w = philox10(make_uint4(j, m.site, (uint32_t)row, (uint32_t)(row >> 32)), k.k0, k.k1);
-  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w}, under = m.least - 1;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    f[2 * i] = (u[i] & 0xffffu) >= m.least ? m.up : 0.f;
-    f[2 * i + 1] = (u[i] >> 16) >= m.least ? m.up : 0.f;
+    keep[2 * i] = (uint32_t)((int32_t)(under - (u[i] & 0xffffu)) >> 31);
+    keep[2 * i + 1] = (uint32_t)((int32_t)(under - (u[i] >> 16)) >> 31);
   }
 }
 // what is dropped is 0, whatever it was
-__device__ __forceinline__ float dropped(float v, float f) { return f == 0.f ? 0.f : v * f; }
+__device__ __forceinline__ float dropped(float v, uint32_t keep) { return __uint_as_float(__float_as_uint(v) & keep); }
 
 // ---------------------------------------------------------------- dropout
 template <typename E>
@@ -43,13 +46,14 @@ __global__ __launch_bounds__(256) void dropout_k(DropMask m, int64_t t0, int row
     const uint32_t row = i / per, j = i - row * per;
     const int64_t t = t0 + row;
     const int left = cols - (int)(j * 8);
-    float v[8], f[8], o[8];
+    float v[8], o[8];
     tk_load8<E>(x + t * ldx + j * 8, left, v);
     if (r) tk_load8<E>(r + t * ldr + j * 8, left, o);
     if (m.least) {
-      mask8(m, key, (uint64_t)(m.row0 + t), j, f);
+      uint32_t k[8];
+      mask8(m, key, (uint64_t)(m.row0 + t), j, k);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = dropped(v[e], f[e]);
+      for (int e = 0; e < 8; ++e) v[e] = dropped(v[e] * m.up, k[e]);
     }
     if (r) {
 #pragma unroll
@@ -69,19 +73,35 @@ void bt_dropout(hipStream_t st, int dt, int64_t rows, int cols, const DropMask& 
 }
 
 // ---------------------------------------------------------------- the join
-// Sum of two values over the block's threads, the same in all of them; `s` is used in turn by calls that follow one another (sum2[2][.]).
+// Sum over the block's threads of one value or of two, the same in all of them: within a wavefront into its last lane, through LDS into groups of T / 64 lanes of all
+// wavefronts, and there once more.  `s` is used in turn by calls that follow one another.
+template <int N>
+__device__ __forceinline__ float lanes_sum(float v) {            // over N consecutive lanes, 2 .. 16
+  v += dpp_move<0xB1>(v);
+  if (N > 2) v += dpp_move<0x4E>(v);
+  if (N > 4) v += dpp_move<0x141>(v);
+  if (N > 8) v += dpp_move<0x140>(v);
+  return v;
+}
+template <int T>
+__device__ __forceinline__ float block_sum(float a, float2 (*s)[T / 64], int& turn) {
+  if (T == 64) return wave_sum(a);
+  a = wave_sum_last(a);
+  float2* const p = s[turn ^= 1];
+  if ((threadIdx.x & 63) == 63) p[threadIdx.x >> 6].x = a;
+  __syncthreads();
+  return lanes_sum<T / 64>(p[threadIdx.x & (T / 64 - 1)].x);
+}
 template <int T>
 __device__ __forceinline__ float2 block_sum2(float a, float b, float2 (*s)[T / 64], int& turn) {
-  a = wave_sum(a);
-  b = wave_sum(b);
-  if (T == 64) return make_float2(a, b);
+  if (T == 64) return make_float2(wave_sum(a), wave_sum(b));
+  a = wave_sum_last(a);
+  b = wave_sum_last(b);
   float2* const p = s[turn ^= 1];
-  if ((threadIdx.x & 63) == 0) p[threadIdx.x >> 6] = make_float2(a, b);
+  if ((threadIdx.x & 63) == 63) p[threadIdx.x >> 6] = make_float2(a, b);
   __syncthreads();
-  float2 t = p[0];
-#pragma unroll
-  for (int i = 1; i < T / 64; ++i) { t.x += p[i].x; t.y += p[i].y; }
-  return t;
+  const float2 t = p[threadIdx.x & (T / 64 - 1)];
+  return make_float2(lanes_sum<T / 64>(t.x), lanes_sum<T / 64>(t.y));
 }
 
 // one row's operands, eight columns at a time
@@ -121,12 +141,11 @@ struct JoinRow {
       cc[e] = fmaf(bh[e], w[e], o[e]);
     }
   }
-  // scale * mask (keep: 0 or its factor)
-  __device__ __forceinline__ void mask(int c, float f[8]) const {
-    if (m.least) mask8(m, key, (uint64_t)(m.row0 + row), (uint32_t)c / 8, f);
+  __device__ __forceinline__ void mask(int c, uint32_t k[8]) const {
+    if (m.least) mask8(m, key, (uint64_t)(m.row0 + row), (uint32_t)c / 8, k);
     else
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = 1.f;
+      for (int e = 0; e < 8; ++e) k[e] = ~0u;
   }
   __device__ __forceinline__ void gate(int c, int left, float v[8]) const {
     if (!a.gate) {
@@ -139,14 +158,14 @@ struct JoinRow {
     else tk_load8<bf16_t>((const bf16_t*)a.gate + at, left, v);
   }
   // y; where they are wanted, what made it
-  __device__ __forceinline__ void stream(int c, int left, float y[8], float bh[8], float cc[8], float f[8], float g[8]) const {
+  __device__ __forceinline__ void stream(int c, int left, float y[8], float bh[8], float cc[8], uint32_t k[8], float g[8]) const {
     load(a.x, a.ldx, c, left, y);
     if (!a.b) return;
     branch(c, left, bh, cc);
-    mask(c, f);
+    mask(c, k);
     gate(c, left, g);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = fmaf(a.scale * g[e], dropped(cc[e], f[e]), y[e]);
+    for (int e = 0; e < 8; ++e) y[e] = fmaf(a.scale * m.up * g[e], dropped(cc[e], k[e]), y[e]);
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (e >= left) y[e] = 0.f;
@@ -177,7 +196,7 @@ struct JoinWide {
 #pragma unroll
         for (int e = 0; e < 8; ++e) t += e < left ? v[e] : 0.f;
       });
-      mean = block_sum2<kJoinT>(t, 0.f, s, turn).x / (float)N;
+      mean = block_sum<kJoinT>(t, s, turn) / (float)N;
     }
     float q = 0.f;
     columns([&](int c, int left) {
@@ -189,7 +208,7 @@ struct JoinWide {
         q = fmaf(d, d, q);
       }
     });
-    rinv = inv_dev(block_sum2<kJoinT>(q, 0.f, s, turn).x, N, r.a.eps);
+    rinv = inv_dev(block_sum<kJoinT>(q, s, turn), N, r.a.eps);
   }
   __device__ __forceinline__ void branch_deviation() {
     r.mb = 0.f;
@@ -202,7 +221,7 @@ struct JoinWide {
     }
   }
   __device__ __forceinline__ void stream_deviation(float& mean, float& rinv) {
-    deviation([&](int c, int left, float v[8]) { float bh[8], cc[8], f[8], g[8]; r.stream(c, left, v, bh, cc, f, g); }, mean, rinv);
+    deviation([&](int c, int left, float v[8]) { float bh[8], cc[8], g[8]; uint32_t k[8]; r.stream(c, left, v, bh, cc, k, g); }, mean, rinv);
   }
 };
 
@@ -217,8 +236,9 @@ __global__ __launch_bounds__(kJoinT) void join_wide_k(ftp_join_args a, DropMask 
     if (a.n) w.stream_deviation(my, ry);
     // y may lie where x or b does: everything has been read but what this thread writes
     w.columns([&](int c, int left) {
-      float y[8], bh[8], cc[8], f[8], g[8];
-      w.r.stream(c, left, y, bh, cc, f, g);
+      float y[8], bh[8], cc[8], g[8];
+      uint32_t k[8];
+      w.r.stream(c, left, y, bh, cc, k, g);
       if (a.y) tk_store8<E>((E*)a.y + row * a.ldy + c, left, y);
       if (a.n) {
         float pw[8], pb[8];
@@ -231,10 +251,304 @@ __global__ __launch_bounds__(kJoinT) void join_wide_k(ftp_join_args a, DropMask 
     });
   }
 }
+// Rows of up to kJoinHeld columns: a block of T threads has eight columns in each and everything it needs of a row in registers.  What a row costs beside its bytes are
+// the meetings of its wavefronts, one for each mean.  WHOLE: rows are a multiple of eight columns.
+enum { JK_X = 1, JK_B = 2, JK_GATE = 4, JK_DY = 8, JK_DN = 16, JK_Y = 32, JK_N = 64, JK_DX = 128, JK_DB = 256, JK_DGATE = 512, JK_POST = 1024, JK_LAYER = 2048, JK_GATE_F32 = 4096, JK_GATE_ADD = 8192 };
+// what the kernels need of a call's record, in as few scalar registers as it goes into: row distances in bytes, questions as bits
+struct JoinK {
+  const char *x, *b, *gate, *dy, *dn;
+  char *y, *n, *dx, *db, *dgate;
+  int ldx, ldb, ldg, lddy, lddn, ldy, ldn, lddx, lddb, lddg;
+  const float *pre_w, *pre_bias, *post_w, *post_bias;
+  int64_t rows, gate_rows;
+  int width, flags;
+  float eps, scale;            // scale: with the mask's factor
+};
+static JoinK join_k(const ftp_join_args& a, const DropMask& m, bool backward) {
+  JoinK k{};
+  const int es = a.dtype == FTP_BF16 ? 2 : 4, gs = a.gate_dtype == FTP_F32 ? 4 : 2;
+  const auto put = [&](const char*& p, int& ld, const void* from, int64_t l, int size, int bit) {
+    p = (const char*)from;
+    ld = (int)(l * size);
+    k.flags |= from ? bit : 0;
+  };
+  const auto put_out = [&](char*& p, int& ld, void* to, int64_t l, int size, int bit) {
+    p = (char*)to;
+    ld = (int)(l * size);
+    k.flags |= to ? bit : 0;
+  };
+  put(k.x, k.ldx, a.x, a.ldx, es, JK_X);
+  put(k.b, k.ldb, a.b, a.ldb, es, JK_B);
+  if (a.b) put(k.gate, k.ldg, a.gate, a.ldg, gs, JK_GATE);
+  if (backward) {
+    put(k.dy, k.lddy, a.dy, a.lddy, es, JK_DY);
+    put(k.dn, k.lddn, a.dn, a.lddn, es, JK_DN);
+    put_out(k.dx, k.lddx, a.dx, a.lddx, es, JK_DX);
+    put_out(k.db, k.lddb, a.db, a.lddb, es, JK_DB);
+    put_out(k.dgate, k.lddg, a.dgate, a.lddg, gs, JK_DGATE);
+  } else {
+    put_out(k.y, k.ldy, a.y, a.ldy, es, JK_Y);
+    put_out(k.n, k.ldn, a.n, a.ldn, es, JK_N);
+  }
+  k.flags |= (a.post ? JK_POST : 0) | (a.norm == FTP_NORM_LAYER ? JK_LAYER : 0) | (gs == 4 ? JK_GATE_F32 : 0) | (a.gate_accumulate ? JK_GATE_ADD : 0);
+  k.pre_w = a.pre_w; k.pre_bias = a.pre_bias; k.post_w = a.post_w; k.post_bias = a.post_bias;
+  k.rows = a.rows; k.gate_rows = a.gate ? a.gate_rows : INT64_MAX;
+  k.width = a.width; k.eps = a.eps; k.scale = a.scale * m.up;
+  return k;
+}
+
+template <typename E> struct Raw8 { u4v_t a[sizeof(E) / 2]; };
+template <typename E, bool WHOLE>
+__device__ __forceinline__ Raw8<E> raw8_load(const char* row, int c, int left) {
+  const E* const p = (const E*)row + (uint32_t)c;
+  Raw8<E> r;
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(E) / 2; ++i) r.a[i] = u4v_t{0, 0, 0, 0};
+  if (left >= 8) {
+    r.a[0] = tk_ld16<E>(p);
+    if constexpr (sizeof(E) == 4) r.a[1] = tk_ld16<E>(p + 4);
+  } else if (!WHOLE) {
+#pragma unroll
+    for (int e = 0; e < 7; ++e) {
+      if (e >= left) break;
+      if constexpr (sizeof(E) == 4) r.a[e / 4][e & 3] = __float_as_uint(p[e]);
+      else r.a[0][e / 2] |= (uint32_t)p[e] << (16 * (e & 1));
+    }
+  }
+  return r;
+}
+template <typename E>
+__device__ __forceinline__ void raw8_open(const Raw8<E>& r, float v[8]) {
+  if constexpr (sizeof(E) == 2) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(r.a[0][i] << 16);
+      v[2 * i + 1] = __uint_as_float(r.a[0][i] & 0xffff0000u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r.a[i / 4][i & 3]);
+  }
+}
+template <typename E, bool WHOLE>
+__device__ __forceinline__ void row_store8(char* row, int c, int left, const float v[8]) {
+  if (WHOLE ? left >= 8 : left > 0) tk_store8<E>((E*)row + (uint32_t)c, WHOLE ? 8 : left, v);
+}
+// the operands of a row: x, b, the gate's row, backward dy and dn as well
+template <typename E, bool BWD>
+struct JoinIn {
+  Raw8<E> x, b, dy, dn;
+  u4v_t g, g2;                 // the gate's row: bfloat16 in g
+  __device__ __forceinline__ void take(const JoinIn& o) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(E) / 2; ++i) {
+      x.a[i] = o.x.a[i];
+      b.a[i] = o.b.a[i];
+      if (BWD) { dy.a[i] = o.dy.a[i]; dn.a[i] = o.dn.a[i]; }
+    }
+    g = o.g;
+    g2 = o.g2;
+  }
+};
+// The questions of a call as they are asked in the loop over its rows: tested there anew (one scalar instruction each), because as conditions that the compiler keeps they
+// take two scalar registers each, more than there are
+__device__ __forceinline__ int join_flags(int f) {
+  asm volatile("" : "+s"(f));
+  return f;
+}
+// the rows of the operands that are asked for next
+struct JoinWalk {
+  const char *x, *b, *gate, *dy, *dn;
+  int to_next;                 // rows until the gate's next
+};
+template <bool BWD>
+__device__ __forceinline__ JoinWalk join_walk(const JoinK& k, int64_t row) {
+  JoinWalk w{k.x + row * k.ldx, k.b + row * k.ldb, k.gate, nullptr, nullptr, 0x7fffffff};
+  if (k.flags & JK_GATE) {
+    const int64_t q = k.gate_rows == 1 ? row : row / k.gate_rows, rest = k.gate_rows == 1 ? 1 : (q + 1) * k.gate_rows - row;
+    w.gate += q * k.ldg;
+    if (rest < w.to_next) w.to_next = (int)rest;
+  }
+  if (BWD) { w.dy = k.dy + row * k.lddy; w.dn = k.dn + row * k.lddn; }
+  return w;
+}
+template <typename E, bool BWD, bool WHOLE>
+__device__ __forceinline__ void join_ask(const JoinK& k, int flags, JoinWalk& w, int c, int left, JoinIn<E, BWD>& in) {
+  if (flags & JK_X) in.x = raw8_load<E, WHOLE>(w.x, c, left);
+  w.x += k.ldx;
+  if (flags & JK_B) in.b = raw8_load<E, WHOLE>(w.b, c, left);
+  w.b += k.ldb;
+  if (flags & JK_GATE) {
+    const bool wide = sizeof(E) == 4 || (flags & JK_GATE_F32);
+    const char* const p = w.gate + (uint32_t)c * (wide ? 4u : 2u);
+    u4v_t lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
+    if (left >= 8) {
+      lo = tk_ld16<bf16_t>((const bf16_t*)p);
+      if (wide) hi = tk_ld16<bf16_t>((const bf16_t*)p + 8);
+    } else if (!WHOLE) {
+#pragma unroll
+      for (int e = 0; e < 7; ++e) {
+        if (e >= left) break;
+        const uint32_t u = wide ? ((const uint32_t*)p)[e] : (uint32_t)((const bf16_t*)p)[e] << (16 * (e & 1));
+        const int at = wide ? e : e / 2;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          lo[i] |= at == i ? u : 0;
+          hi[i] |= at == i + 4 ? u : 0;
+        }
+      }
+    }
+    in.g = lo;
+    in.g2 = hi;
+    if (--w.to_next == 0) {
+      w.gate += k.ldg;
+      w.to_next = k.gate_rows < 0x7fffffff ? (int)k.gate_rows : 0x7fffffff;
+    }
+  }
+  if constexpr (BWD) {
+    if (flags & JK_DY) in.dy = raw8_load<E, WHOLE>(w.dy, c, left);
+    w.dy += k.lddy;
+    if (flags & JK_DN) in.dn = raw8_load<E, WHOLE>(w.dn, c, left);
+    w.dn += k.lddn;
+  }
+}
+template <typename E>
+__device__ __forceinline__ void join_open(bool there, const Raw8<E>& r, float v[8]) {
+  if (there) raw8_open<E>(r, v);
+  else
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 0.f;
+}
+// scale * gate
+template <typename E, bool BWD>
+__device__ __forceinline__ void join_open_gate(const JoinK& k, int flags, const JoinIn<E, BWD>& in, float g[8]) {
+  if (!(flags & JK_GATE)) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) g[e] = k.scale;
+    return;
+  }
+  const bool wide = sizeof(E) == 4 || (flags & JK_GATE_F32);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t whole = e < 4 ? in.g[e & 3] : in.g2[e & 3], half = in.g[e / 2];
+    g[e] = __uint_as_float(wide ? whole : e & 1 ? half & 0xffff0000u : half << 16);
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) g[e] *= k.scale;
+}
+template <bool WHOLE>
+__device__ __forceinline__ void join_weight(const float* w, int c, int left, float none, float v[8]) {
+  if (w) {
+    raw8_open<float>(raw8_load<float, WHOLE>((const char*)w, c, left), v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = none;
+  }
+}
+// v (zeros past the row's end) less its mean (layer), and its inverse deviation
+template <int T, bool WHOLE>
+__device__ __forceinline__ float join_deviation(const JoinK& k, int flags, float inv, int left, float v[8], float2 (*s)[T / 64], int& turn) {
+  if (flags & JK_LAYER) {
+    float t = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t += v[e];
+    const float mean = block_sum<T>(t, s, turn) * inv;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (WHOLE ? left > 0 : e < left) ? v[e] - mean : 0.f;
+  }
+  float q = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) q = fmaf(v[e], v[e], q);
+  return 1.f / sqrtf(fmaf(block_sum<T>(q, s, turn), inv, k.eps));
+}
+
+template <typename E, int T, bool WHOLE>
+__global__ __launch_bounds__(T) void join_row_k(JoinK k, DropMask m, int64_t per) {
+  __shared__ float2 s[2][T / 64];
+  const int c = threadIdx.x * 8, left = k.width - c;
+  const float inv = 1.f / (float)k.width;
+  const MaskKey key = mask_key(m);
+  const int64_t r0 = blockIdx.x * per, r1 = r0 + per < k.rows ? r0 + per : k.rows;
+  int turn = 0, flags = k.flags;
+  JoinWalk at = join_walk<false>(k, r0);
+  JoinIn<E, false> in, next;
+  join_ask<E, false, WHOLE>(k, flags, at, c, left, in);
+  char *py = k.y + r0 * k.ldy, *pn = k.n + r0 * k.ldn;
+  float pw[8], pb[8], qw[8], qb[8];
+  join_weight<WHOLE>(k.pre_w, c, left, 1.f, pw);
+  join_weight<WHOLE>(k.pre_bias, c, left, 0.f, pb);
+  join_weight<WHOLE>(k.post_w, c, left, 1.f, qw);
+  join_weight<WHOLE>(k.post_bias, c, left, 0.f, qb);
+  uint64_t number = (uint64_t)(m.row0 + r0);
+  for (int row = (int)(r1 - r0); row > 0; --row, ++number) {
+    flags = join_flags(k.flags);
+    if (row > 1) join_ask<E, false, WHOLE>(k, flags, at, c, left, next);
+    float y[8];
+    join_open<E>(flags & JK_X, in.x, y);
+    if (flags & JK_B) {
+      float v[8], g[8];
+      raw8_open<E>(in.b, v);
+      if (flags & JK_POST) {
+        const float r = join_deviation<T, WHOLE>(k, flags, inv, left, v, s, turn);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = fmaf(v[e] * r, qw[e], qb[e]);
+      }
+      join_open_gate<E, false>(k, flags, in, g);
+      if (m.least) {
+        uint32_t keep[8];
+        mask8(m, key, number, threadIdx.x, keep);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = dropped(v[e], keep[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = (WHOLE ? left > 0 : e < left) ? fmaf(g[e], v[e], y[e]) : 0.f;
+    }
+    if (flags & JK_Y) row_store8<E, WHOLE>(py, c, left, y);
+    py += k.ldy;
+    if (flags & JK_N) {
+      const float r = join_deviation<T, WHOLE>(k, flags, inv, left, y, s, turn);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = fmaf(y[e] * r, pw[e], pb[e]);
+      row_store8<E, WHOLE>(pn, c, left, y);
+    }
+    pn += k.ldn;
+    in.take(next);
+  }
+}
+enum { kJoinHeld = 8192 };
+// blocks for `rows` rows: half the card's wavefronts at most (8192 x 4096 bfloat16, forward and backward, 208 us; all of them 212, of which the blocks' sums are more)
+static int64_t join_blocks(int64_t rows, int T) { return std::max<int64_t>(1, std::min<int64_t>(256 * 1024 / T, rows)); }
+static int join_threads(int width) {
+  int t = 64;
+  while (t * 8 < width) t *= 2;
+  return t;
+}
+template <typename F>
+static void join_by_threads(int t, F f) {
+  if (t == 64) f(std::integral_constant<int, 64>());
+  else if (t == 128) f(std::integral_constant<int, 128>());
+  else if (t == 256) f(std::integral_constant<int, 256>());
+  else if (t == 512) f(std::integral_constant<int, 512>());
+  else f(std::integral_constant<int, 1024>());
+}
+
 void bt_join(hipStream_t st, const ftp_join_args& a, const DropMask& m) {
   const double n = (double)a.rows * a.width;
   KScope ks(st, "tok_join", n * (a.dtype == 1 ? 2 : 4) * ((a.x != nullptr) + (a.b != nullptr) + (a.y != nullptr) + (a.n != nullptr) + (a.gate && a.gate_rows == 1)), 15 * n,
             a.rows, a.width);
+  if (a.width <= kJoinHeld) {
+    const int t = join_threads(a.width);
+    const int64_t want = join_blocks(a.rows, t), per = (a.rows + want - 1) / want;
+    const dim3 g((unsigned)((a.rows + per - 1) / per)), b(t);
+    join_by_threads(t, [&](auto tc) {
+      constexpr int T = decltype(tc)::value;
+      const JoinK k = join_k(a, m, false);
+      const auto go = [&](auto f) { hipLaunchKernelGGL(f, g, b, 0, st, k, m, per); };
+      if (a.dtype == FTP_BF16) a.width % 8 ? go(join_row_k<bf16_t, T, false>) : go(join_row_k<bf16_t, T, true>);
+      else a.width % 8 ? go(join_row_k<float, T, false>) : go(join_row_k<float, T, true>);
+    });
+    return;
+  }
   const dim3 b((unsigned)std::min<int64_t>(a.rows, 1 << 20));
   if (a.dtype == FTP_BF16) hipLaunchKernelGGL(join_wide_k<bf16_t>, b, dim3(kJoinT), 0, st, a, m);
   else hipLaunchKernelGGL(join_wide_k<float>, b, dim3(kJoinT), 0, st, a, m);
@@ -250,7 +564,7 @@ struct JoinRanges {
   int blocks;
 };
 static JoinRanges join_ranges(const ftp_join_args& a) {
-  const int64_t want = std::max<int64_t>(1, (a.rows + 511) / 512);
+  const int64_t blocks = join_blocks(a.rows, a.width <= kJoinHeld ? join_threads(a.width) : 1024), want = std::max<int64_t>(1, (a.rows + blocks - 1) / blocks);
   JoinRanges r{want, 0, 1, 0};
   r.group = a.gate && a.gate_rows > 1 ? std::min(a.gate_rows, a.rows) : 0;
   if (r.group == 0) {
@@ -280,8 +594,26 @@ __device__ __forceinline__ void join_range(const JoinRanges& g, int64_t rows, in
   if (r1 > rows) r1 = rows;
 }
 
+// a row of dgate
+template <bool WHOLE>
+__device__ __forceinline__ void join_put_gate(int flags, char* row, int c, int left, const float v[8]) {
+  if (flags & JK_GATE_F32) {
+    if (flags & JK_GATE_ADD) {
+      float o[8];
+      raw8_open<float>(raw8_load<float, WHOLE>(row, c, left), o);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] += v[e];
+      row_store8<float, WHOLE>(row, c, left, o);
+    } else {
+      row_store8<float, WHOLE>(row, c, left, v);
+    }
+  } else {
+    row_store8<bf16_t, WHOLE>(row, c, left, v);
+  }
+}
+
 template <typename E>
-__global__ __launch_bounds__(kJoinT) void join_wide_bwd_k(ftp_join_args a, DropMask m, JoinRanges g, JoinParts parts) {
+__global__ __launch_bounds__(kJoinT) void join_wide_bwd_k(ftp_join_args a, JoinK jk, DropMask m, JoinRanges g, JoinParts parts) {
   __shared__ float2 s[2][kJoinT / 64];
   JoinWide<E> w{JoinRow<E>{a, m, mask_key(m), 0, 0.f, 1.f}, a.width, 0, s};
   const int N = a.width;
@@ -299,8 +631,9 @@ __global__ __launch_bounds__(kJoinT) void join_wide_bwd_k(ftp_join_args a, DropM
     if (a.dn) {
       w.stream_deviation(my, ry);
       w.columns([&](int c, int left) {
-        float y[8], bh[8], cc[8], f[8], gt[8], d[8], pw[8];
-        w.r.stream(c, left, y, bh, cc, f, gt);
+        float y[8], bh[8], cc[8], gt[8], d[8], pw[8];
+        uint32_t k[8];
+        w.r.stream(c, left, y, bh, cc, k, gt);
         w.r.load(a.dn, a.lddn, c, left, d);
         w.r.weight(a.pre_w, c, left, pw, 1.f);
 #pragma unroll
@@ -316,7 +649,8 @@ __global__ __launch_bounds__(kJoinT) void join_wide_bwd_k(ftp_join_args a, DropM
     }
     // gradient of y, and of c; with `add` the column sums too
     const auto at = [&](int c, int left, float dY[8], float dc[8], float bh[8], bool add) __attribute__((always_inline)) {
-      float y[8], cc[8], f[8], gt[8], dn[8], pw[8], yh[8];
+      float y[8], cc[8], gt[8], dn[8], pw[8], yh[8];
+      uint32_t f[8];
       w.r.stream(c, left, y, bh, cc, f, gt);
       w.r.load(a.dy, a.lddy, c, left, dY);
       if (a.dn) {
@@ -330,7 +664,7 @@ __global__ __launch_bounds__(kJoinT) void join_wide_bwd_k(ftp_join_args a, DropM
       }
       if (a.b) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) dc[e] = dropped(a.scale * gt[e] * dY[e], f[e]);
+        for (int e = 0; e < 8; ++e) dc[e] = dropped(a.scale * m.up * gt[e] * dY[e], f[e]);
       }
       if (!add) return;
       const auto sum = [&](int k, auto value) __attribute__((always_inline)) {
@@ -344,16 +678,7 @@ __global__ __launch_bounds__(kJoinT) void join_wide_bwd_k(ftp_join_args a, DropM
         for (int e = 0; e < 8; ++e) o[e] = fresh ? value(e) : o[e] + value(e);
         tk_store8<float>(q, left, o);
         if (k == JP_GATE && g.parts == 1 && (row + 1 == r1 || (row + 1) % g.group == 0)) {
-          const int64_t to = row / g.group * a.lddg + c;
-          if (a.gate_dtype == FTP_F32) {
-            float v[8];
-            if (a.gate_accumulate) tk_load8<float>((float*)a.dgate + to, left, v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = a.gate_accumulate ? v[e] + o[e] : o[e];
-            tk_store8<float>((float*)a.dgate + to, left, v);
-          } else {
-            tk_store8<bf16_t>((bf16_t*)a.dgate + to, left, o);
-          }
+          join_put_gate<false>(jk.flags, jk.dgate + row / g.group * jk.lddg, c, left, o);
         }
       };
       if (a.dn) {
@@ -363,21 +688,13 @@ __global__ __launch_bounds__(kJoinT) void join_wide_bwd_k(ftp_join_args a, DropM
       if (!a.b) return;
       sum(JP_POST_W, [&](int e) { return dc[e] * bh[e]; });
       sum(JP_POST_BIAS, [&](int e) { return dc[e]; });
-      const auto dg = [&](int e) { return a.scale * dropped(cc[e], f[e]) * dY[e]; };
+      const auto dg = [&](int e) { return a.scale * m.up * dropped(cc[e], f[e]) * dY[e]; };
       sum(JP_GATE, dg);
       if (a.dgate && g.group == 0) {     // a gate row for each row
-        const int64_t to = row * a.lddg + c;
         float v[8];
-        if (a.gate_dtype == FTP_F32) {
-          if (a.gate_accumulate) tk_load8<float>((float*)a.dgate + to, left, v);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = a.gate_accumulate ? v[e] + dg(e) : dg(e);
-          tk_store8<float>((float*)a.dgate + to, left, v);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = dg(e);
-          tk_store8<bf16_t>((bf16_t*)a.dgate + to, left, v);
-        }
+        for (int e = 0; e < 8; ++e) v[e] = dg(e);
+        join_put_gate<false>(jk.flags, jk.dgate + row * jk.lddg, c, left, v);
       }
     };
     const bool again = a.db && a.post;
@@ -414,12 +731,211 @@ __global__ __launch_bounds__(kJoinT) void join_wide_bwd_k(ftp_join_args a, DropM
   }
 }
 
-// Sums of the blocks' rows, in their order: 64 columns a block, sixteen threads to a column.  Results 0 .. 3 are the weights' gradients, of all blocks; from
+// Eight columns a thread.  Column sums in registers, or (blocks of 1024 threads, which have 128 registers each) in LDS, two fours a thread for each sum that is wanted.
+template <int T, bool LDS>
+struct JoinSums {
+  float r[LDS ? 1 : JP_ALL][8];
+  float4* at;                            // [sums][2][T]
+  int want;
+  // sums that are not wanted have no place in front of others
+  __device__ __forceinline__ float4* place(int k) const { return at + 2 * __popc(want & ((1 << k) - 1)) * T; }
+  __device__ __forceinline__ void start(int wanted, float4* lds) {
+    if constexpr (LDS) {
+      at = lds + threadIdx.x;
+      want = wanted;
+      for (int n = 2 * __popc(wanted) - 1; n >= 0; --n) at[n * T] = make_float4(0.f, 0.f, 0.f, 0.f);
+    } else {
+#pragma unroll
+      for (int k = 0; k < JP_ALL; ++k)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[k][e] = 0.f;
+    }
+  }
+  template <typename F>
+  __device__ __forceinline__ void add(int k, F value) {                  // value(e, old)
+    if constexpr (LDS) {
+      float4 *const p = place(k), *const q = p + T;
+      float4 u = *p, v = *q;
+      u.x = value(0, u.x); u.y = value(1, u.y); u.z = value(2, u.z); u.w = value(3, u.w);
+      v.x = value(4, v.x); v.y = value(5, v.y); v.z = value(6, v.z); v.w = value(7, v.w);
+      *p = u;
+      *q = v;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r[k][e] = value(e, r[k][e]);
+    }
+  }
+  // the sum, and zero in its place
+  __device__ __forceinline__ void take(int k, float v[8]) {
+    if constexpr (LDS) {
+      float4* const p = place(k);
+      const float4 a = p[0], b = p[T];
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+      p[0] = p[T] = make_float4(0.f, 0.f, 0.f, 0.f);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) { v[e] = r[k][e]; r[k][e] = 0.f; }
+    }
+  }
+};
+// BIAS: sums of the biases as well, and a bias behind the block
+template <typename E, int T, bool BIAS, bool WHOLE, bool LDS, bool AHEAD, bool HOLD>
+__global__ __launch_bounds__(T, T == 512 && sizeof(E) == 2 ? 4 : 1) void join_row_bwd_k(JoinK k, DropMask m, JoinRanges gr, float* parts, int64_t part_size, int wanted) {
+  __shared__ float2 s[2][T / 64];
+  extern __shared__ float4 held[];
+  const int c = threadIdx.x * 8, left = k.width - c;
+  const float inv = 1.f / (float)k.width;
+  const MaskKey key = mask_key(m);
+  int64_t r0, r1;
+  join_range(gr, k.rows, r0, r1);
+  JoinSums<T, LDS> sum;
+  sum.start(wanted, held);
+  int turn = 0, flags = k.flags, want = wanted;
+  if (r0 < r1) {
+    JoinWalk at = join_walk<true>(k, r0);
+    JoinIn<E, true> in, next;
+    join_ask<E, true, WHOLE>(k, flags, at, c, left, in);
+    const int64_t group = want >> JP_GATE & 1 ? r0 / gr.group : r0;               // dgate's row
+    char *pdx = k.dx + r0 * k.lddx, *pdb = k.db + r0 * k.lddb, *pdg = k.dgate + group * k.lddg;
+    const int64_t rest = want >> JP_GATE & 1 ? (group + 1) * gr.group - r0 : 1;
+    int to_end = gr.parts > 1 || rest > 0x7fffffff ? 0x7fffffff : (int)rest;      // rows until the group's sum is whole
+    float pw[8], qw[8], qb[8];
+    if (HOLD) {
+      join_weight<WHOLE>(k.pre_w, c, left, 1.f, pw);
+      join_weight<WHOLE>(k.post_w, c, left, 1.f, qw);
+      if (BIAS) join_weight<WHOLE>(k.post_bias, c, left, 0.f, qb);
+    }
+    uint64_t number = (uint64_t)(m.row0 + r0);
+    for (int row = (int)(r1 - r0); row > 0; --row, ++number) {
+      flags = join_flags(k.flags);
+      want = join_flags(wanted);
+      if (AHEAD && row > 1) join_ask<E, true, WHOLE>(k, flags, at, c, left, next);
+      float dY[8], bh[8], cc[8], g[8];                   // g: scale * gate; cc: what it multiplies, dropped
+      uint32_t keep[8];
+      float rb = 1.f;
+      join_open<E>(flags & JK_DY, in.dy, dY);
+      if (flags & JK_B) {
+        raw8_open<E>(in.b, bh);
+        if (flags & JK_POST) {
+          rb = join_deviation<T, WHOLE>(k, flags, inv, left, bh, s, turn);
+          if (!HOLD) {
+            join_weight<WHOLE>(k.post_w, c, left, 1.f, qw);
+            if (BIAS) join_weight<WHOLE>(k.post_bias, c, left, 0.f, qb);
+          }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            bh[e] *= rb;
+            cc[e] = BIAS ? fmaf(bh[e], qw[e], qb[e]) : bh[e] * qw[e];
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) cc[e] = bh[e];
+        }
+        join_open_gate<E, true>(k, flags, in, g);
+        if (m.least) {
+          mask8(m, key, number, threadIdx.x, keep);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) cc[e] = dropped(cc[e], keep[e]);
+        }
+      }
+      if (flags & JK_DN) {
+        float y[8], dn[8];
+        join_open<E>(flags & JK_X, in.x, y);
+        raw8_open<E>(in.dn, dn);
+        if (flags & JK_B) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] = (WHOLE ? left > 0 : e < left) ? fmaf(g[e], cc[e], y[e]) : 0.f;
+        }
+        const float ry = join_deviation<T, WHOLE>(k, flags, inv, left, y, s, turn);
+        float s1 = 0.f, s2 = 0.f;
+        if (!HOLD) join_weight<WHOLE>(k.pre_w, c, left, 1.f, pw);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] *= ry;
+        if (want >> JP_PRE_W & 1) sum.add(JP_PRE_W, [&](int e, float o) { return fmaf(dn[e], y[e], o); });
+        if (BIAS && (want >> JP_PRE_BIAS & 1)) sum.add(JP_PRE_BIAS, [&](int e, float o) { return o + dn[e]; });
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          dn[e] *= pw[e];                                // past the row's end dn is 0
+          s1 += dn[e];
+          s2 = fmaf(dn[e], y[e], s2);
+        }
+        const float2 t = block_sum2<T>((flags & JK_LAYER) ? s1 : 0.f, s2, s, turn);
+        s1 = t.x * inv;
+        s2 = t.y * inv;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dY[e] += ry * (dn[e] - fmaf(y[e], s2, s1));
+      }
+      if (flags & JK_DX) row_store8<E, WHOLE>(pdx, c, left, dY);
+      pdx += k.lddx;
+      if (flags & JK_B) {
+        if (flags & JK_DGATE) {
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = k.scale * cc[e] * dY[e];
+          const bool shared = want >> JP_GATE & 1;
+          if (shared) sum.add(JP_GATE, [&](int e, float o) { return o + v[e]; });
+          if (--to_end == 0) {
+            if (shared) sum.take(JP_GATE, v);
+            join_put_gate<WHOLE>(flags, pdg, c, left, v);
+            pdg += k.lddg;
+            to_end = shared ? (int)gr.group : 1;         // no more than a block's rows, or it would not be one's
+          } else if (row == 1 && gr.parts == 1) {        // the batch ends inside a group
+            sum.take(JP_GATE, v);
+            join_put_gate<WHOLE>(flags, pdg, c, left, v);
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dY[e] *= g[e];
+        if (m.least) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) dY[e] = dropped(dY[e], keep[e]);
+        }
+        if (flags & JK_POST) {
+          float t1 = 0.f, t2 = 0.f;
+          if (want >> JP_POST_W & 1) sum.add(JP_POST_W, [&](int e, float o) { return fmaf(dY[e], bh[e], o); });
+          if (BIAS && (want >> JP_POST_BIAS & 1)) sum.add(JP_POST_BIAS, [&](int e, float o) { return o + dY[e]; });
+          if (flags & JK_DB) {
+            if (!HOLD) join_weight<WHOLE>(k.post_w, c, left, 1.f, qw);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              dY[e] = (WHOLE ? left > 0 : e < left) ? dY[e] * qw[e] : 0.f;
+              t1 += dY[e];
+              t2 = fmaf(dY[e], bh[e], t2);
+            }
+            const float2 t = block_sum2<T>((flags & JK_LAYER) ? t1 : 0.f, t2, s, turn);
+            t1 = t.x * inv;
+            t2 = t.y * inv;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dY[e] = rb * (dY[e] - fmaf(bh[e], t2, t1));
+          }
+        }
+        if (flags & JK_DB) row_store8<E, WHOLE>(pdb, c, left, dY);
+      }
+      pdb += k.lddb;
+      if (AHEAD) in.take(next);
+      else if (row > 1) join_ask<E, true, WHOLE>(k, flags, at, c, left, in);
+    }
+  }
+  if (left <= 0) return;
+  float* to = parts + (int64_t)blockIdx.x * k.width + c;
+#pragma unroll
+  for (int j = 0; j < JP_ALL; ++j) {
+    if (!(wanted >> j & 1)) continue;
+    if ((BIAS || (j != JP_PRE_BIAS && j != JP_POST_BIAS)) && !(j == JP_GATE && gr.parts == 1)) {
+      float v[8];
+      sum.take(j, v);
+      tk_store8<float>(to, left, v);
+    }
+    to += part_size;
+  }
+}
+
+// Sums of the blocks' rows, in their order: 32 columns a block, 32 threads to a column.  Results 0 .. 3 are the weights' gradients, of all blocks; from
 // there on a row of dgate each, of its group's blocks.
 __global__ __launch_bounds__(1024) void join_sum_k(JoinParts parts, JoinRanges g, int N, float* w0, float* w1, float* w2, float* w3, int accumulate, void* dgate, int64_t lddg,
                                                    int gate_bf16, int gate_accumulate, int first, int64_t jobs) {
-  __shared__ float sum[16][64];
-  const int lane = threadIdx.x & 63, ty = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+  __shared__ float sum[32][33];
+  const int lane = threadIdx.x & 31, ty = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
   for (int64_t job = first + blockIdx.y; job < jobs; job += gridDim.y) {
     const bool gate = job >= JP_GATE;
     const float* const p = gate ? parts.p[JP_GATE] + (job - JP_GATE) * g.parts * N : parts.p[job];
@@ -428,14 +944,14 @@ __global__ __launch_bounds__(1024) void join_sum_k(JoinParts parts, JoinRanges g
     float v = 0.f;
     if (c < N) {
 #pragma unroll 8
-      for (int i = ty; i < n; i += 16) v += p[(int64_t)i * N + c];
+      for (int i = ty; i < n; i += 32) v += p[(int64_t)i * N + c];
     }
     __syncthreads();
     sum[ty][lane] = v;
     __syncthreads();
     if (ty || c >= N) continue;
 #pragma unroll
-    for (int i = 1; i < 16; ++i) v += sum[i][lane];
+    for (int i = 1; i < 32; ++i) v += sum[i][lane];
     if (gate) {
       const int64_t to = (job - JP_GATE) * lddg + c;
       if (gate_bf16) ((bf16_t*)dgate)[to] = f32_to_bf16(v);
@@ -480,19 +996,40 @@ void bt_join_bwd(hipStream_t st, const ftp_join_args& a, const DropMask& m) {
   JoinParts parts{};
   char* at = (char*)a.ws;
   bool weights = false;
+  int sums = 0, want = 0;
   for (int k = 0; k < JP_ALL; ++k) {
     if (!wanted[k]) continue;
+    ++sums;
+    want |= 1 << k;
     parts.p[k] = (float*)at;
     at += join_part_bytes(a, r);
     weights |= k < JP_GATE;
   }
-  if (a.dtype == FTP_BF16) hipLaunchKernelGGL(join_wide_bwd_k<bf16_t>, dim3(r.blocks), dim3(kJoinT), 0, st, a, m, r, parts);
-  else hipLaunchKernelGGL(join_wide_bwd_k<float>, dim3(r.blocks), dim3(kJoinT), 0, st, a, m, r, parts);
+  const JoinK k = join_k(a, m, true);
+  // five sums of 8192 columns would be all of the LDS
+  const bool held = a.width <= kJoinHeld && (sums < JP_ALL || join_threads(a.width) < 1024);
+  if (held) {
+    const int t = join_threads(a.width);
+    const bool bias = a.dpre_bias || a.dpost_bias || (a.post && a.post_bias);
+    join_by_threads(t, [&](auto tc) {
+      constexpr int T = decltype(tc)::value;
+      constexpr bool L = T >= 512;
+      const auto go = [&](auto f) { hipLaunchKernelGGL(f, dim3(r.blocks), dim3(T), L ? (size_t)sums * T * 32 : 0, st, k, m, r, (float*)a.ws, (int64_t)(join_part_bytes(a, r) / 4), want); };
+      const auto by = [&](auto* e) {
+        typedef std::remove_pointer_t<decltype(e)> E;
+        if (a.width % 8) bias ? go(join_row_bwd_k<E, T, true, false, L, !L, !L>) : go(join_row_bwd_k<E, T, false, false, L, !L, !L>);
+        else bias ? go(join_row_bwd_k<E, T, true, true, L, !L, !L>) : go(join_row_bwd_k<E, T, false, true, L, !L, !L>);
+      };
+      if (a.dtype == FTP_BF16) by((bf16_t*)nullptr);
+      else by((float*)nullptr);
+    });
+  } else if (a.dtype == FTP_BF16) hipLaunchKernelGGL(join_wide_bwd_k<bf16_t>, dim3(r.blocks), dim3(kJoinT), 0, st, a, k, m, r, parts);
+  else hipLaunchKernelGGL(join_wide_bwd_k<float>, dim3(r.blocks), dim3(kJoinT), 0, st, a, k, m, r, parts);
   const bool gate = wanted[JP_GATE] && r.parts > 1;
   if (!weights && !gate) return;
   const int first = weights ? 0 : JP_GATE;
   const int64_t jobs = JP_GATE + (gate ? (a.rows + r.group - 1) / r.group : 0);
-  hipLaunchKernelGGL(join_sum_k, dim3((a.width + 63) / 64, (unsigned)std::min<int64_t>(jobs - first, 256)), dim3(1024), 0, st, parts, r, a.width, a.dpre_w, a.dpre_bias, a.dpost_w,
+  hipLaunchKernelGGL(join_sum_k, dim3((a.width + 31) / 32, (unsigned)std::min<int64_t>(jobs - first, 256)), dim3(1024), 0, st, parts, r, a.width, a.dpre_w, a.dpre_bias, a.dpost_w,
                      a.dpost_bias, a.accumulate, a.dgate, a.lddg, a.gate_dtype == FTP_BF16, a.gate_accumulate, first, jobs);
 }
 
