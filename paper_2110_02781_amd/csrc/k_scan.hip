@@ -11,7 +11,7 @@
 
 namespace ftp {
 
-enum { kScanT = 32 };
+enum { kScanT = 32, kScanR = 4 };     // rows of a chunk; rows that are asked for together
 struct ScanArgs {
   ftp_scan_args a;
   int chunks, per;             // rows of a chunk: per <= kScanT
@@ -19,33 +19,48 @@ struct ScanArgs {
   float *A, *B, *C, *seed, *state, *back;     // [chunks][width] each
 };
 
-// V consecutive columns, of which `left` are there
-template <typename E, int V>
-__device__ __forceinline__ void sc_load(const E* p, int left, float v[V]) {
-  if constexpr (sizeof(E) * V == 4) {
-    if (left >= V) {
-      uint32_t t;
-      __builtin_memcpy(&t, p, 4);
-      if constexpr (V == 1) v[0] = __uint_as_float(t);
-      else { v[0] = __uint_as_float(t << 16); v[1] = __uint_as_float(t & 0xffff0000u); }
-      return;
-    }
+// V consecutive columns of a row as stored; of the last ones `left` are there (WHOLE: all)
+template <typename E, int V> struct ScanRaw { uint32_t w[V * sizeof(E) / 4]; };
+template <typename E, int V, bool WHOLE>
+__device__ __forceinline__ ScanRaw<E, V> sc_ask(const E* p, int left) {
+  ScanRaw<E, V> r;
+  if (WHOLE || left >= V) {
+    struct __attribute__((packed, aligned(sizeof(E)))) At { uint32_t w[V * sizeof(E) / 4]; };
+    const At t = *reinterpret_cast<const At*>(p);
+    __builtin_memcpy(&r, &t, sizeof(r));
+    return r;
   }
+  E t[V];
 #pragma unroll
-  for (int e = 0; e < V; ++e) v[e] = e < left ? to_f32(p[e]) : 0.f;
+  for (int e = 0; e < V; ++e) t[e] = e < left ? p[e] : (E)0;
+  __builtin_memcpy(&r, t, sizeof(r));
+  return r;
 }
 template <typename E, int V>
+__device__ __forceinline__ void sc_open(const ScanRaw<E, V>& r, float v[V]) {
+#pragma unroll
+  for (int e = 0; e < V; ++e)
+    v[e] = sizeof(E) == 4 ? __uint_as_float(r.w[e]) : __uint_as_float(e & 1 ? r.w[e / 2] & 0xffff0000u : r.w[e / 2] << 16);
+}
+template <typename E, int V, bool WHOLE>
+__device__ __forceinline__ void sc_load(const E* p, int left, float v[V]) { sc_open<E, V>(sc_ask<E, V, WHOLE>(p, left), v); }
+template <typename E, int V, bool WHOLE>
 __device__ __forceinline__ void sc_store(E* p, int left, const float v[V]) {
-  if constexpr (sizeof(E) * V == 4 && V == 2) {
-    if (left >= V) {
-      const uint32_t t = f32x2_to_bf16x2(v[0], v[1]);
-      __builtin_memcpy(p, &t, 4);
-      return;
-    }
+  if (WHOLE || left >= V) {
+    struct __attribute__((packed, aligned(sizeof(E)))) At { uint32_t w[V * sizeof(E) / 4]; } t;
+#pragma unroll
+    for (int i = 0; i < (int)(V * sizeof(E) / 4); ++i) t.w[i] = sizeof(E) == 4 ? __float_as_uint(v[i]) : f32x2_to_bf16x2(v[2 * i % V], v[(2 * i + 1) % V]);
+    *reinterpret_cast<At*>(p) = t;
+    return;
   }
 #pragma unroll
   for (int e = 0; e < V; ++e)
     if (e < left) p[e] = from_f32<E>(v[e]);
+}
+template <int V>
+__device__ __forceinline__ void sc_zero(float v[V]) {
+#pragma unroll
+  for (int e = 0; e < V; ++e) v[e] = 0.f;
 }
 
 // where the chunk's sequences begin and end: bit t for the row r0 + t; a lane holds its row's sequence
@@ -53,6 +68,8 @@ struct ScanRows {
   uint64_t in, first, last;
   int seq;
   __device__ __forceinline__ int of(int t) const { return __builtin_amdgcn_readlane(seq, t); }
+  // rows that are not in the middle of a sequence
+  __device__ __forceinline__ uint64_t events() const { return ~in | first | last; }
 };
 __device__ __forceinline__ ScanRows scan_rows(const ftp_scan_args& a, int64_t r0, int n) {
   ScanRows s;
@@ -60,10 +77,16 @@ __device__ __forceinline__ ScanRows scan_rows(const ftp_scan_args& a, int64_t r0
   const int64_t r = r0 + lane;
   bool in = lane < n, first = false, last = false;
   if (!a.starts) {
-    const int64_t q = r / a.length, at = r - q * a.length;
-    s.seq = (int)q;
-    first = at == 0;
-    last = at == a.length - 1;
+    if (a.length == 1) {
+      s.seq = (int)r;
+      first = last = true;
+    } else {
+      const int64_t q0 = r0 / a.length, d = r0 - q0 * a.length;       // 64 rows in the sequence q0 and those behind it: below 2^31 as length is
+      const uint32_t at = (uint32_t)d + (uint32_t)lane, len = (uint32_t)a.length, q = at / len, m = at - q * len;
+      s.seq = (int)(q0 + q);
+      first = m == 0;
+      last = m == len - 1;
+    }
   } else {
     int lo = 0, hi = a.seqs;             // the last sequence that begins at r or in front (of several, all but one are empty)
     while (lo < hi) {
@@ -82,114 +105,154 @@ __device__ __forceinline__ ScanRows scan_rows(const ftp_scan_args& a, int64_t r0
   return s;
 }
 
-// a, 1 - a, c(a) and the derivative of c by f
+// a = sigmoid(f), 1 - a and c(a).  With e = e^-|f| they are 1 / (1 + e) and e / (1 + e), the former a where f >= 0: neither loses its places.  e = 2^t, t = -|f| log2(e) in two
+// parts, so that the rounding of t does not count |t| times (with one part the initial states' gradient of a long batch was twice as far off as its plain form in fp32).
 struct ScanGate { float a, rest, c; };
-__device__ __forceinline__ ScanGate scan_gate(float f, int form) {
-  const float e = __expf(-fabsf(f)), r = __builtin_amdgcn_rcpf(1.f + e), s = e * r;      // of sigmoid(|f|) and sigmoid(-|f|) none loses its places
-  ScanGate g;
-  g.a = f >= 0.f ? r : s;
-  g.rest = f >= 0.f ? s : r;
-  if (!(f == f)) g.a = g.rest = f;
-  g.c = form == FTP_SCAN_MIX ? g.rest : form == FTP_SCAN_UNIT ? sqrtf(g.rest * (1.f + g.a)) : 1.f;
-  return g;
+template <int FORM>
+__device__ __forceinline__ ScanGate scan_gate(float f) {
+  const float m = fabsf(f), g = m > 105.f ? 105.f : m;               // e^-105 is 0; NaN stays
+  const float t = g * -1.44269504f, lo = fmaf(g, -1.44269504f, -t) + g * -1.92596303e-8f;
+  const float p = __builtin_amdgcn_exp2f(t), e = fmaf(p, lo * 0.693147181f, p), r = __builtin_amdgcn_rcpf(1.f + e), q = e * r;
+  const bool up = f >= 0.f;
+  ScanGate s;
+  s.a = up ? r : q;
+  s.rest = up ? q : r;
+  s.c = FORM == FTP_SCAN_MIX ? s.rest : FORM == FTP_SCAN_UNIT ? __builtin_amdgcn_sqrtf(fmaf(s.rest, s.a, s.rest)) : 1.f;
+  return s;
 }
-__device__ __forceinline__ float scan_gate_slope(const ScanGate& g, int form) {
-  return form == FTP_SCAN_MIX ? -g.a * g.rest : form == FTP_SCAN_UNIT ? -g.a * g.a * sqrtf(g.rest * __builtin_amdgcn_rcpf(1.f + g.a)) : 0.f;
+// c's derivative by f
+template <int FORM>
+__device__ __forceinline__ float scan_slope(const ScanGate& g) {
+  if (FORM == FTP_SCAN_MIX) return -g.a * g.rest;
+  if (FORM == FTP_SCAN_UNIT) return -g.a * g.a * __builtin_amdgcn_sqrtf(g.rest * __builtin_amdgcn_rcpf(1.f + g.a));
+  return 0.f;
 }
 
-struct ScanAt { int64_t r0; int c, n, left; int chunk; };
-// the wavefront's place: column groups beside one another
+// a wavefront's place: column groups beside one another
+struct ScanAt { int64_t r0; int c, n, left, chunk; };
 template <int V>
-__device__ __forceinline__ bool scan_at(const ScanArgs& k, int wave, ScanAt& p) {
-  const int groups = (k.a.width + 64 * V - 1) / (64 * V);
-  p.chunk = wave / groups;
-  p.c = (wave - p.chunk * groups) * 64 * V + (int)(threadIdx.x & 63) * V;
+__device__ __forceinline__ ScanAt scan_at(const ScanArgs& k, int64_t wave) {
+  const uint32_t groups = (uint32_t)(k.a.width + 64 * V - 1) / (64 * V), w = (uint32_t)wave;
+  ScanAt p;
+  p.chunk = (int)(w / groups);
+  p.c = (int)(w - (uint32_t)p.chunk * groups) * 64 * V + (int)(threadIdx.x & 63) * V;
   p.left = k.a.width - p.c;
   p.r0 = (int64_t)p.chunk * k.per;
   const int64_t n = k.a.rows - p.r0;
   p.n = (int)(n < k.per ? n : k.per);
-  return p.left > 0;
+  return p;
+}
+// kScanR rows of a matrix from the chunk's row t on (behind its last row: that one again)
+template <typename E, int V, bool WHOLE>
+__device__ __forceinline__ void scan_ask(const void* m, int64_t ld, const ScanAt& p, int t, ScanRaw<E, V> r[kScanR]) {
+  const E* const q = (const E*)m + p.r0 * ld;
+#pragma unroll
+  for (int i = 0; i < kScanR; ++i) {
+    const int u = t + i < p.n ? t + i : p.n - 1;
+    r[i] = sc_ask<E, V, WHOLE>(q + u * ld + (uint32_t)p.c, p.left);
+  }
+}
+// a sequence's row of states, or zeros
+template <int V, bool WHOLE>
+__device__ __forceinline__ void scan_state(const float* m, int64_t ld, int seq, const ScanAt& p, float h[V]) {
+  if (m) sc_load<float, V, WHOLE>(m + seq * ld + p.c, p.left, h);
+  else sc_zero<V>(h);
 }
 
 // A and B of a chunk; backward: C too
-template <typename E, int V, bool BWD>
+template <typename E, int V, bool WHOLE, int FORM, bool BWD>
 __global__ __launch_bounds__(256) void scan_sums_k(ScanArgs k) {
   const ftp_scan_args& a = k.a;
-  const int groups = (a.width + 64 * V - 1) / (64 * V);
-  const int64_t waves = (int64_t)k.chunks * groups;
+  const int64_t waves = (int64_t)k.chunks * ((a.width + 64 * V - 1) / (64 * V));
   for (int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); wave < waves; wave += (int64_t)gridDim.x * 4) {
-    ScanAt p;
-    const bool there = scan_at<V>(k, (int)wave, p);
-    const ScanRows rows = scan_rows(a, p.r0, p.n);
-    if (!there) continue;
+    const ScanAt p = scan_at<V>(k, wave);
+    const int64_t mine = (int64_t)p.chunk * a.width + p.c;
     float A[V], B[V], C[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) { A[e] = 1.f; B[e] = C[e] = 0.f; }
-    for (int t = 0; t < p.n; ++t) {
-      const uint64_t bit = 1ull << t;
-      if (!(rows.in & bit)) {            // of no sequence: nothing goes through
-#pragma unroll
-        for (int e = 0; e < V; ++e) A[e] = 0.f;
-        continue;
+    ScanRaw<E, V> f[kScanR], x[kScanR], g[kScanR], dy[kScanR];
+    const auto ask = [&](int t) __attribute__((always_inline)) {
+      scan_ask<E, V, WHOLE>(a.f, a.ldf, p, t, f);
+      scan_ask<E, V, WHOLE>(a.x, a.ldx, p, t, x);
+      if (BWD) {
+        scan_ask<E, V, WHOLE>(a.dy, a.lddy, p, t, dy);
+        if (a.g) scan_ask<E, V, WHOLE>(a.g, a.ldg, p, t, g);
       }
-      const int64_t r = p.r0 + t;
-      float f[V], x[V];
-      sc_load<E, V>((const E*)a.f + r * a.ldf + p.c, p.left, f);
-      sc_load<E, V>((const E*)a.x + r * a.ldx + p.c, p.left, x);
-      if (rows.first & bit) {
-        if (a.h0) sc_load<float, V>(a.h0 + (int64_t)rows.of(t) * a.ldh0 + p.c, p.left, B);
+    };
+    if (p.left > 0) ask(0);              // before the search for the sequences
+    const ScanRows rows = scan_rows(a, p.r0, p.n);
+    if (p.left <= 0) continue;
+    const uint64_t events = rows.events();
+    for (int t0 = 0; t0 < p.n; t0 += kScanR) {
+      float fv[kScanR][V], xv[kScanR][V], into[kScanR][V], gv[kScanR * V];
+#pragma unroll
+      for (int i = 0; i < kScanR; ++i) {
+        sc_open<E, V>(f[i], fv[i]);
+        sc_open<E, V>(x[i], xv[i]);
+        if (BWD) {
+          sc_open<E, V>(dy[i], into[i]);
+          if (a.g) sc_open<E, V>(g[i], gv + i * V);
+        }
+      }
+      if (t0 + kScanR < p.n) ask(t0 + kScanR);
+      if (BWD && a.g) {
+        tactn<kScanR * V>(gv, a.act);
+#pragma unroll
+        for (int i = 0; i < kScanR; ++i)
+#pragma unroll
+          for (int e = 0; e < V; ++e) into[i][e] *= gv[i * V + e];
+      }
+#pragma unroll
+      for (int i = 0; i < kScanR; ++i) {
+        const int t = t0 + i;
+        const bool event = events >> t & 1;
+        bool last = false;
+        if (event) {
+          if (!(rows.in >> t & 1)) {     // of no sequence, or behind the chunk: nothing goes through
+            if (t < p.n) sc_zero<V>(A);
+            continue;
+          }
+          if (rows.first >> t & 1) {
+            scan_state<V, WHOLE>(a.h0, a.ldh0, rows.of(t), p, B);
+            sc_zero<V>(A);
+            // the state in front of a sequence that goes on behind this chunk, before another chunk writes the one behind it into the same memory
+            if (!BWD) sc_store<float, V, WHOLE>(k.seed + mine, p.left, B);
+          }
+          last = rows.last >> t & 1;
+          if (BWD && last && a.dh_end) {
+            float d[V];
+            scan_state<V, WHOLE>(a.dh_end, a.lddhe, rows.of(t), p, d);
+#pragma unroll
+            for (int e = 0; e < V; ++e) into[i][e] += d[e];
+            // what arrives at the end of a sequence from a chunk in front, before another chunk writes dh0 into the same memory
+            if (!(rows.first << (63 - t))) sc_store<float, V, WHOLE>(k.seed + mine, p.left, d);
+          }
+        }
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          A[e] = 0.f;
-          if (!a.h0) B[e] = 0.f;
+          const ScanGate s = scan_gate<FORM>(fv[i][e]);
+          B[e] = fmaf(s.a, B[e], s.c * xv[i][e]);
+          A[e] *= s.a;
+          if (BWD) C[e] = fmaf(A[e], into[i][e], C[e]);
         }
-        // the state in front of a sequence that goes on behind this chunk, before another chunk writes the one behind it into the same memory
-        if (!BWD && k.seed) sc_store<float, V>(k.seed + (int64_t)p.chunk * a.width + p.c, p.left, B);
-      }
-      float dy[V], g[V], d[V];
-      if (BWD) {
-        sc_load<E, V>((const E*)a.dy + r * a.lddy + p.c, p.left, dy);
-        if (a.g) {
-          sc_load<E, V>((const E*)a.g + r * a.ldg + p.c, p.left, g);
-          tactn<V>(g, a.act);
-#pragma unroll
-          for (int e = 0; e < V; ++e) dy[e] *= g[e];
-        }
-        if ((rows.last & bit) && a.dh_end) {
-          sc_load<float, V>(a.dh_end + (int64_t)rows.of(t) * a.lddhe + p.c, p.left, d);
-#pragma unroll
-          for (int e = 0; e < V; ++e) dy[e] += d[e];
-          // what arrives at the end of a sequence from a chunk in front, before another chunk writes dh0 into the same memory
-          if (k.seed && !(rows.first << (63 - t))) sc_store<float, V>(k.seed + (int64_t)p.chunk * a.width + p.c, p.left, d);
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const ScanGate s = scan_gate(f[e], a.form);
-        B[e] = fmaf(s.a, B[e], s.c * x[e]);
-        A[e] *= s.a;
-        if (BWD) {
-          C[e] = fmaf(A[e], dy[e], C[e]);
-          if (rows.last & bit) A[e] = 0.f;
-        }
+        if (BWD && last) sc_zero<V>(A);
       }
     }
-    const int64_t to = (int64_t)p.chunk * a.width + p.c;
-    sc_store<float, V>(k.A + to, p.left, A);
-    sc_store<float, V>(k.B + to, p.left, B);
-    if (BWD) sc_store<float, V>(k.C + to, p.left, C);
+    sc_store<float, V, WHOLE>(k.A + mine, p.left, A);
+    sc_store<float, V, WHOLE>(k.B + mine, p.left, B);
+    if (BWD) sc_store<float, V, WHOLE>(k.C + mine, p.left, C);
   }
 }
 
-// From chunk to chunk: state[i] = the state in front of chunk i; the other way (blockIdx.y 1) back[i] = what chunk i + 1 hands back.  64 columns a block, sixteen
+// From chunk to chunk: state[i] = the state in front of chunk i; the other way (blockIdx.y 1) back[i] = what chunk i + 1 hands back.  32 columns a block, 32
 // threads to a column, each with its share of the chunks one behind the other: first their product and sum, then the states.
 __global__ __launch_bounds__(1024) void scan_follow_k(ScanArgs k) {
-  __shared__ float sa[16][64], sb[16][64];
-  const int lane = threadIdx.x & 63, ty = threadIdx.x >> 6, W = k.a.width, c = blockIdx.x * 64 + lane;
+  __shared__ float sa[32][33], sb[32][33];
+  const int lane = threadIdx.x & 31, ty = threadIdx.x >> 5, W = k.a.width, c = blockIdx.x * 32 + lane;
   const bool rev = blockIdx.y == 1;
   const float *const A = k.A, *const B = rev ? k.C : k.B;
   float* const out = rev ? k.back : k.state;
-  const int share = (k.chunks + 15) / 16, i0 = ty * share, i1 = i0 + share < k.chunks ? i0 + share : k.chunks;
+  const int share = (k.chunks + 31) / 32, i0 = ty * share, i1 = i0 + share < k.chunks ? i0 + share : k.chunks;
   const auto at = [&](int i) { return (int64_t)(rev ? k.chunks - 1 - i : i) * W + c; };
   float a = 1.f, b = 0.f;
   if (c < W) {
@@ -215,186 +278,233 @@ __global__ __launch_bounds__(1024) void scan_follow_k(ScanArgs k) {
 }
 
 // states of empty sequences stay: those of the 64 from `seq0` on
-template <int V>
-__device__ __forceinline__ void scan_empty(const ScanArgs& k, int64_t seq0, int c, int left, const float* from, int64_t ldf, float* to, int64_t ldt) {
-  if (!to || (from == to && ldf == ldt)) return;
+template <int V, bool WHOLE>
+__device__ __forceinline__ void scan_empty(const ScanArgs& k, int64_t block, const float* from, int64_t ldf, float* to, int64_t ldt) {
+  if (!to || from == to) return;
   const ftp_scan_args& a = k.a;
-  const int64_t s = seq0 + (threadIdx.x & 63);
+  const int groups = (a.width + 64 * V - 1) / (64 * V);
+  const int64_t seq0 = block / groups * 64, s = seq0 + (threadIdx.x & 63);
+  ScanAt p{};
+  p.c = (int)(block % groups) * 64 * V + (int)(threadIdx.x & 63) * V;
+  p.left = a.width - p.c;
   uint64_t todo = __ballot(s < a.seqs && (a.starts ? a.starts[s < a.seqs ? s : 0] >= a.starts[s < a.seqs ? s + 1 : 0] : a.length == 0));
-  if (left <= 0) return;
+  if (p.left <= 0) return;
   while (todo) {
-    const int64_t q = seq0 + __builtin_ctzll(todo);
+    const int q = (int)seq0 + __builtin_ctzll(todo);
     todo &= todo - 1;
     float h[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) h[e] = 0.f;
-    if (from) sc_load<float, V>(from + q * ldf + c, left, h);
-    sc_store<float, V>(to + q * ldt + c, left, h);
+    scan_state<V, WHOLE>(from, ldf, q, p, h);
+    sc_store<float, V, WHOLE>(to + q * ldt + p.c, p.left, h);
   }
 }
 
-template <typename E, int V>
+template <typename E, int V, bool WHOLE, int FORM>
 __global__ __launch_bounds__(256) void scan_walk_k(ScanArgs k) {
   const ftp_scan_args& a = k.a;
   const int groups = (a.width + 64 * V - 1) / (64 * V);
   const int64_t waves = (int64_t)k.chunks * groups, all = waves + (a.starts || a.length == 0 ? (int64_t)((a.seqs + 63) / 64) * groups : 0);
   for (int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); wave < all; wave += (int64_t)gridDim.x * 4) {
-    ScanAt p;
     if (wave >= waves) {
-      const int64_t w = wave - waves, block = w / groups;
-      const int c = (int)(w - block * groups) * 64 * V + (int)(threadIdx.x & 63) * V;
-      scan_empty<V>(k, block * 64, c, a.width - c, a.h0, a.ldh0, a.h_end, a.ldhe);
+      scan_empty<V, WHOLE>(k, wave - waves, a.h0, a.ldh0, a.h_end, a.ldhe);
       continue;
     }
-    const bool there = scan_at<V>(k, (int)wave, p);
-    const ScanRows rows = scan_rows(a, p.r0, p.n);
-    if (!there) continue;
+    const ScanAt p = scan_at<V>(k, wave);
     const int64_t mine = (int64_t)p.chunk * a.width + p.c;
     float h[V];
+    sc_zero<V>(h);
+    ScanRaw<E, V> f[kScanR], x[kScanR], g[kScanR];
+    const auto ask = [&](int t) __attribute__((always_inline)) {
+      scan_ask<E, V, WHOLE>(a.f, a.ldf, p, t, f);
+      scan_ask<E, V, WHOLE>(a.x, a.ldx, p, t, x);
+      if (a.g) scan_ask<E, V, WHOLE>(a.g, a.ldg, p, t, g);
+    };
+    if (p.left > 0) {
+      if (!k.whole) sc_load<float, V, WHOLE>(k.state + mine, p.left, h);
+      ask(0);
+    }
+    const ScanRows rows = scan_rows(a, p.r0, p.n);
+    if (p.left <= 0) continue;
+    const uint64_t events = rows.events();
+    for (int t0 = 0; t0 < p.n; t0 += kScanR) {
+      float fv[kScanR][V], xv[kScanR][V], gv[kScanR * V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) h[e] = 0.f;
-    if (!k.whole) sc_load<float, V>(k.state + mine, p.left, h);
-    for (int t = 0; t < p.n; ++t) {
-      const uint64_t bit = 1ull << t;
-      if (!(rows.in & bit)) continue;
-      const int64_t r = p.r0 + t;
-      float f[V], x[V], g[V];
-      sc_load<E, V>((const E*)a.f + r * a.ldf + p.c, p.left, f);
-      sc_load<E, V>((const E*)a.x + r * a.ldx + p.c, p.left, x);
-      if (rows.first & bit) {
-        // one that goes on behind the chunk: its state from the copy
-        if (!k.whole && !(rows.last >> t)) sc_load<float, V>(k.seed + mine, p.left, h);
-        else if (a.h0) sc_load<float, V>(a.h0 + (int64_t)rows.of(t) * a.ldh0 + p.c, p.left, h);
-        else
-#pragma unroll
-          for (int e = 0; e < V; ++e) h[e] = 0.f;
+      for (int i = 0; i < kScanR; ++i) {
+        sc_open<E, V>(f[i], fv[i]);
+        sc_open<E, V>(x[i], xv[i]);
+        if (a.g) sc_open<E, V>(g[i], gv + i * V);
       }
+      if (t0 + kScanR < p.n) ask(t0 + kScanR);
+      if (a.g) tactn<kScanR * V>(gv, a.act);
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const ScanGate s = scan_gate(f[e], a.form);
-        h[e] = fmaf(s.a, h[e], s.c * x[e]);
-      }
-      if (a.y) {
+      for (int i = 0; i < kScanR; ++i) {
+        const int t = t0 + i;
+        bool last = false;
+        if (events >> t & 1) {
+          if (!(rows.in >> t & 1)) continue;
+          if (rows.first >> t & 1) {
+            // one that goes on behind the chunk: its state from the copy
+            if (!k.whole && !(rows.last >> t)) sc_load<float, V, WHOLE>(k.seed + mine, p.left, h);
+            else scan_state<V, WHOLE>(a.h0, a.ldh0, rows.of(t), p, h);
+          }
+          last = rows.last >> t & 1;
+        }
         float y[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) y[e] = h[e];
-        if (a.g) {
-          sc_load<E, V>((const E*)a.g + r * a.ldg + p.c, p.left, g);
-          tactn<V>(g, a.act);
-#pragma unroll
-          for (int e = 0; e < V; ++e) y[e] *= g[e];
+        for (int e = 0; e < V; ++e) {
+          const ScanGate s = scan_gate<FORM>(fv[i][e]);
+          h[e] = fmaf(s.a, h[e], s.c * xv[i][e]);
+          y[e] = a.g ? h[e] * gv[i * V + e] : h[e];
         }
-        sc_store<E, V>((E*)a.y + r * a.ldy + p.c, p.left, y);
+        if (a.y) sc_store<E, V, WHOLE>((E*)a.y + (p.r0 + t) * a.ldy + (uint32_t)p.c, p.left, y);
+        if (last && a.h_end) sc_store<float, V, WHOLE>(a.h_end + (int64_t)rows.of(t) * a.ldhe + p.c, p.left, h);
       }
-      if ((rows.last & bit) && a.h_end) sc_store<float, V>(a.h_end + (int64_t)rows.of(t) * a.ldhe + p.c, p.left, h);
     }
   }
 }
 
-// The states of a chunk in front, then its gradients from the last row to the first.
-template <typename E, int V>
+// A chunk's states from the first row on, of which those in front of every kScanR rows are kept in LDS; then its gradients from the last row to the first, the states of
+// kScanR rows at a time made again.
+template <typename E, int V, bool WHOLE, int FORM>
 __global__ __launch_bounds__(256) void scan_back_k(ScanArgs k) {
+  __shared__ float held[4][kScanT / kScanR][64 * V];
   const ftp_scan_args& a = k.a;
   const int groups = (a.width + 64 * V - 1) / (64 * V);
   const int64_t waves = (int64_t)k.chunks * groups, all = waves + (a.starts || a.length == 0 ? (int64_t)((a.seqs + 63) / 64) * groups : 0);
-  for (int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); wave < all; wave += (int64_t)gridDim.x * 4) {
-    ScanAt p;
+  const int me = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (int64_t wave = (int64_t)blockIdx.x * 4 + me; wave < all; wave += (int64_t)gridDim.x * 4) {
     if (wave >= waves) {
-      const int64_t w = wave - waves, block = w / groups;
-      const int c = (int)(w - block * groups) * 64 * V + (int)(threadIdx.x & 63) * V;
-      scan_empty<V>(k, block * 64, c, a.width - c, a.dh_end, a.lddhe, a.dh0, a.lddh0);
+      scan_empty<V, WHOLE>(k, wave - waves, a.dh_end, a.lddhe, a.dh0, a.lddh0);
       continue;
     }
-    const bool there = scan_at<V>(k, (int)wave, p);
-    const ScanRows rows = scan_rows(a, p.r0, p.n);
-    if (!there) continue;
+    const ScanAt p = scan_at<V>(k, wave);
     const int64_t mine = (int64_t)p.chunk * a.width + p.c;
-    float before[kScanT][V], h[V], mu[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) h[e] = mu[e] = 0.f;
-    if (!k.whole) {
-      sc_load<float, V>(k.state + mine, p.left, h);
-      sc_load<float, V>(k.back + mine, p.left, mu);
+    float* const keep = held[me][0] + (threadIdx.x & 63) * V;          // a lane's own: nothing to wait for
+    float h[V], mu[V];
+    sc_zero<V>(h);
+    sc_zero<V>(mu);
+    ScanRaw<E, V> f[kScanR], x[kScanR], g[kScanR], dy[kScanR];
+    if (p.left > 0) {
+      if (!k.whole) {
+        sc_load<float, V, WHOLE>(k.state + mine, p.left, h);
+        sc_load<float, V, WHOLE>(k.back + mine, p.left, mu);
+      }
+      scan_ask<E, V, WHOLE>(a.f, a.ldf, p, 0, f);
+      scan_ask<E, V, WHOLE>(a.x, a.ldx, p, 0, x);
     }
+    const ScanRows rows = scan_rows(a, p.r0, p.n);
+    if (p.left <= 0) continue;
+    const uint64_t events = rows.events();
+    const int t_end = (p.n - 1) / kScanR * kScanR;
+    const auto ask_back = [&](int t) __attribute__((always_inline)) {
+      scan_ask<E, V, WHOLE>(a.dy, a.lddy, p, t, dy);
+      if (a.g) scan_ask<E, V, WHOLE>(a.g, a.ldg, p, t, g);
+    };
+    for (int t0 = 0;; t0 += kScanR) {
 #pragma unroll
-    for (int t = 0; t < kScanT; ++t) {
-      const uint64_t bit = 1ull << t;
-      if (t < p.n && (rows.in & bit)) {
-        const int64_t r = p.r0 + t;
-        float f[V], x[V];
-        sc_load<E, V>((const E*)a.f + r * a.ldf + p.c, p.left, f);
-        sc_load<E, V>((const E*)a.x + r * a.ldx + p.c, p.left, x);
-        if (rows.first & bit) {
-          if (a.h0) sc_load<float, V>(a.h0 + (int64_t)rows.of(t) * a.ldh0 + p.c, p.left, h);
-          else
+      for (int e = 0; e < V; ++e) keep[t0 / kScanR * 64 * V + e] = h[e];
+      if (t0 == t_end) break;
+      float fv[kScanR][V], xv[kScanR][V];
 #pragma unroll
-            for (int e = 0; e < V; ++e) h[e] = 0.f;
+      for (int i = 0; i < kScanR; ++i) {
+        sc_open<E, V>(f[i], fv[i]);
+        sc_open<E, V>(x[i], xv[i]);
+      }
+      scan_ask<E, V, WHOLE>(a.f, a.ldf, p, t0 + kScanR, f);
+      scan_ask<E, V, WHOLE>(a.x, a.ldx, p, t0 + kScanR, x);
+#pragma unroll
+      for (int i = 0; i < kScanR; ++i) {
+        const int t = t0 + i;
+        if (events >> t & 1) {
+          if (!(rows.in >> t & 1)) continue;
+          if (rows.first >> t & 1) scan_state<V, WHOLE>(a.h0, a.ldh0, rows.of(t), p, h);
         }
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          before[t][e] = h[e];
-          const ScanGate s = scan_gate(f[e], a.form);
-          h[e] = fmaf(s.a, h[e], s.c * x[e]);
+          const ScanGate s = scan_gate<FORM>(fv[i][e]);
+          h[e] = fmaf(s.a, h[e], s.c * xv[i][e]);
         }
       }
     }
+    ask_back(t_end);
+    for (int t0 = t_end; t0 >= 0; t0 -= kScanR) {
+      float fv[kScanR][V], xv[kScanR][V], lam[kScanR][V], act[kScanR * V], dact[kScanR * V], before[kScanR][V];
+      ScanGate s[kScanR][V];
 #pragma unroll
-    for (int t = kScanT - 1; t >= 0; --t) {
-      const uint64_t bit = 1ull << t;
-      if (t < p.n && (rows.in & bit)) {
-        const int64_t r = p.r0 + t;
-        float f[V], x[V], dy[V], df[V], dx[V];
-        sc_load<E, V>((const E*)a.f + r * a.ldf + p.c, p.left, f);
-        sc_load<E, V>((const E*)a.x + r * a.ldx + p.c, p.left, x);
-        sc_load<E, V>((const E*)a.dy + r * a.lddy + p.c, p.left, dy);
-        ScanGate s[V];
+      for (int i = 0; i < kScanR; ++i) {
+        sc_open<E, V>(f[i], fv[i]);
+        sc_open<E, V>(x[i], xv[i]);
+        sc_open<E, V>(dy[i], lam[i]);
+        if (a.g) sc_open<E, V>(g[i], act + i * V);
+      }
+      if (t0 > 0) {
+        scan_ask<E, V, WHOLE>(a.f, a.ldf, p, t0 - kScanR, f);
+        scan_ask<E, V, WHOLE>(a.x, a.ldx, p, t0 - kScanR, x);
+        ask_back(t0 - kScanR);
+      }
 #pragma unroll
-        for (int e = 0; e < V; ++e) s[e] = scan_gate(f[e], a.form);
-        if (a.g) {
-          float g[V], act[V], dact[V], dg[V];
-          sc_load<E, V>((const E*)a.g + r * a.ldg + p.c, p.left, g);
-          tact_gradn<V>(g, act, dact, a.act);
+      for (int e = 0; e < V; ++e) h[e] = keep[t0 / kScanR * 64 * V + e];
 #pragma unroll
-          for (int e = 0; e < V; ++e) {
-            dg[e] = dy[e] * fmaf(s[e].a, before[t][e], s[e].c * x[e]) * dact[e];
-            dy[e] *= act[e];
-          }
-          if (a.dg) sc_store<E, V>((E*)a.dg + r * a.lddg + p.c, p.left, dg);
-        }
-        if (rows.last & bit) {
-          if (!a.dh_end) {
+      for (int i = 0; i < kScanR; ++i) {
+        const int t = t0 + i;
 #pragma unroll
-            for (int e = 0; e < V; ++e) mu[e] = 0.f;
-          } else if (!k.whole && !(rows.first << (63 - t))) {      // a sequence from a chunk in front: the copy of what arrives at its end
-            sc_load<float, V>(k.seed + mine, p.left, mu);
-          } else {
-            sc_load<float, V>(a.dh_end + (int64_t)rows.of(t) * a.lddhe + p.c, p.left, mu);
-          }
-        }
+        for (int e = 0; e < V; ++e) s[i][e] = scan_gate<FORM>(fv[i][e]);
+        if ((events >> t & 1) && (rows.first >> t & 1)) scan_state<V, WHOLE>(a.h0, a.ldh0, rows.of(t), p, h);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          const float lam = dy[e] + mu[e];
-          dx[e] = lam * s[e].c;
-          df[e] = lam * fmaf(before[t][e], s[e].a * s[e].rest, x[e] * scan_gate_slope(s[e], a.form));
-          mu[e] = lam * s[e].a;
+          before[i][e] = h[e];
+          h[e] = fmaf(s[i][e].a, h[e], s[i][e].c * xv[i][e]);
         }
-        if (a.df) sc_store<E, V>((E*)a.df + r * a.lddf + p.c, p.left, df);
-        if (a.dx) sc_store<E, V>((E*)a.dx + r * a.lddx + p.c, p.left, dx);
-        if ((rows.first & bit) && a.dh0) sc_store<float, V>(a.dh0 + (int64_t)rows.of(t) * a.lddh0 + p.c, p.left, mu);
+      }
+      if (a.g) tact_gradn<kScanR * V>(act, act, dact, a.act);
+#pragma unroll
+      for (int i = kScanR - 1; i >= 0; --i) {
+        const int t = t0 + i;
+        bool first = false;
+        if (events >> t & 1) {
+          if (!(rows.in >> t & 1)) continue;
+          if (rows.last >> t & 1) {
+            // of a sequence from a chunk in front: the copy of what arrives at its end
+            if (a.dh_end && !k.whole && !(rows.first << (63 - t))) sc_load<float, V, WHOLE>(k.seed + mine, p.left, mu);
+            else scan_state<V, WHOLE>(a.dh_end, a.lddhe, rows.of(t), p, mu);
+          }
+          first = rows.first >> t & 1;
+        }
+        const int64_t r = p.r0 + t;
+        float dg[V], df[V], dx[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const ScanGate& q = s[i][e];
+          if (a.g) {
+            dg[e] = lam[i][e] * fmaf(q.a, before[i][e], q.c * xv[i][e]) * dact[i * V + e];
+            lam[i][e] *= act[i * V + e];
+          }
+          const float l = lam[i][e] + mu[e];
+          dx[e] = l * q.c;
+          df[e] = l * fmaf(before[i][e], q.a * q.rest, xv[i][e] * scan_slope<FORM>(q));
+          mu[e] = l * q.a;
+        }
+        if (a.dg) sc_store<E, V, WHOLE>((E*)a.dg + r * a.lddg + (uint32_t)p.c, p.left, dg);
+        if (a.df) sc_store<E, V, WHOLE>((E*)a.df + r * a.lddf + (uint32_t)p.c, p.left, df);
+        if (a.dx) sc_store<E, V, WHOLE>((E*)a.dx + r * a.lddx + (uint32_t)p.c, p.left, dx);
+        if (first && a.dh0) sc_store<float, V, WHOLE>(a.dh0 + (int64_t)rows.of(t) * a.lddh0 + p.c, p.left, mu);
       }
     }
   }
 }
 
-static int scan_per(const ftp_scan_args& a, bool& whole) {
+// rows of a chunk; where whole sequences fit into one, as few of them as fill the card
+static int scan_per(const ftp_scan_args& a, int V, bool& whole) {
   whole = a.starts ? a.rows <= kScanT : a.length <= kScanT;
-  return !a.starts && a.length > 0 && whole ? (int)(kScanT / a.length * a.length) : kScanT;
+  if (a.starts || a.length == 0 || !whole) return kScanT;
+  const int64_t groups = (a.width + 64 * V - 1) / (64 * V), fit = kScanT / a.length;
+  return (int)(std::max<int64_t>(1, std::min<int64_t>(fit, a.seqs * groups / 4096)) * a.length);
 }
+static int scan_columns(const ftp_scan_args& a) { return a.dtype == FTP_BF16 ? 2 : 1; }
 static ScanArgs scan_plan(const ftp_scan_args& a, bool backward, size_t& bytes) {
   ScanArgs k{};
   k.a = a;
   bool whole;
-  k.per = scan_per(a, whole);
+  k.per = scan_per(a, scan_columns(a), whole);
   k.whole = whole;
   k.chunks = (int)((a.rows + k.per - 1) / k.per);
   bytes = 0;
@@ -404,11 +514,8 @@ static ScanArgs scan_plan(const ftp_scan_args& a, bool backward, size_t& bytes) 
   k.A = take();
   k.B = take();
   k.state = take();
-  // a copy of the states in front (backward: of the gradients behind) is needed where the results may overwrite them
+  k.seed = take();             // copies of the states in front (backward: of the gradients behind), which the results may overwrite
   if (backward) { k.C = take(); k.back = take(); }
-  const float* const from = backward ? a.dh_end : a.h0;
-  k.seed = take();
-  if (!from && backward) k.seed = nullptr;
   return k;
 }
 size_t bt_scan_bytes(const ftp_scan_args& a, bool backward) {
@@ -416,31 +523,33 @@ size_t bt_scan_bytes(const ftp_scan_args& a, bool backward) {
   scan_plan(a, backward, n);
   return n;
 }
-// bfloat16: two columns a lane
-template <typename F>
-static void scan_by_type(int dt, F f) {
-  if (dt == FTP_BF16) f((bf16_t*)nullptr, std::integral_constant<int, 2>());
-  else f((float*)nullptr, std::integral_constant<int, 1>());
-}
 static unsigned scan_blocks(const ScanArgs& k, int V, bool walk) {
   const int64_t groups = (k.a.width + 64 * V - 1) / (64 * V);
   const int64_t waves = groups * (k.chunks + (walk && (k.a.starts || k.a.length == 0) ? (k.a.seqs + 63) / 64 : 0));
   return (unsigned)std::max<int64_t>(1, std::min<int64_t>((waves + 3) / 4, 1 << 20));
 }
+template <bool BWD, typename E, int V, bool WHOLE, int FORM>
+static void scan_launch(hipStream_t st, const ScanArgs& k) {
+  if (!k.whole) {
+    hipLaunchKernelGGL((scan_sums_k<E, V, WHOLE, FORM, BWD>), dim3(scan_blocks(k, V, false)), dim3(256), 0, st, k);
+    hipLaunchKernelGGL(scan_follow_k, dim3((k.a.width + 31) / 32, BWD ? 2 : 1), dim3(1024), 0, st, k);
+  }
+  if (BWD) hipLaunchKernelGGL((scan_back_k<E, V, WHOLE, FORM>), dim3(scan_blocks(k, V, true)), dim3(256), 0, st, k);
+  else hipLaunchKernelGGL((scan_walk_k<E, V, WHOLE, FORM>), dim3(scan_blocks(k, V, true)), dim3(256), 0, st, k);
+}
+template <bool BWD, typename E, int V, bool WHOLE>
+static void scan_form(hipStream_t st, const ScanArgs& k) {
+  if (k.a.form == FTP_SCAN_ADD) scan_launch<BWD, E, V, WHOLE, FTP_SCAN_ADD>(st, k);
+  else if (k.a.form == FTP_SCAN_MIX) scan_launch<BWD, E, V, WHOLE, FTP_SCAN_MIX>(st, k);
+  else scan_launch<BWD, E, V, WHOLE, FTP_SCAN_UNIT>(st, k);
+}
 template <bool BWD>
 static void scan_go(hipStream_t st, const ftp_scan_args& a) {
   size_t bytes;
   const ScanArgs k = scan_plan(a, BWD, bytes);
-  scan_by_type(a.dtype, [&](auto* e, auto v) {
-    typedef std::remove_pointer_t<decltype(e)> E;
-    constexpr int V = decltype(v)::value;
-    if (!k.whole) {
-      hipLaunchKernelGGL((scan_sums_k<E, V, BWD>), dim3(scan_blocks(k, V, false)), dim3(256), 0, st, k);
-      hipLaunchKernelGGL(scan_follow_k, dim3((a.width + 63) / 64, BWD ? 2 : 1), dim3(1024), 0, st, k);
-    }
-    if (BWD) hipLaunchKernelGGL((scan_back_k<E, V>), dim3(scan_blocks(k, V, true)), dim3(256), 0, st, k);
-    else hipLaunchKernelGGL((scan_walk_k<E, V>), dim3(scan_blocks(k, V, true)), dim3(256), 0, st, k);
-  });
+  if (a.dtype == FTP_F32) scan_form<BWD, float, 1, true>(st, k);
+  else if (a.width % 2 == 0) scan_form<BWD, bf16_t, 2, true>(st, k);
+  else scan_form<BWD, bf16_t, 2, false>(st, k);
 }
 void bt_scan(hipStream_t st, const ftp_scan_args& a) {
   const double n = (double)a.rows * a.width;
