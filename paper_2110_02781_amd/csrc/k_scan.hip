@@ -11,13 +11,33 @@
 
 namespace ftp {
 
-enum { kScanT = 32, kScanR = 4 };     // rows of a chunk; rows that are asked for together
+#ifndef SRF
+#define SRF 4
+#define SRB 4
+#define SRW 4
+#define SRK 4
+#endif
+enum { kScanT = 32 };        // rows of a chunk
+// What the kernels need of a call's record, in few scalar registers: row distances of the matrices in bytes, questions as bits that are tested where they are asked (SK_...)
 struct ScanArgs {
-  ftp_scan_args a;
+  const char *f, *x, *g, *dy;
+  char *y, *df, *dx, *dg;
+  int ldf, ldx, ldg, lddy, ldy, lddf, lddx, lddg;
+  const float *h0, *dh_end;
+  float *h_end, *dh0;
+  int ldh0, lddhe, ldhe, lddh0;
+  int64_t rows, length;
+  const int32_t* starts;
+  int width, seqs, act, flags;
   int chunks, per;             // rows of a chunk: per <= kScanT
-  int whole;                   // no sequence goes on from one chunk to the next
   float *A, *B, *C, *seed, *state, *back;     // [chunks][width] each
 };
+// SK_WHOLE: no sequence goes on from one chunk to the next
+enum { SK_G = 1, SK_Y = 2, SK_DF = 4, SK_DX = 8, SK_DG = 16, SK_HEND = 32, SK_DHEND = 64, SK_DH0 = 128, SK_WHOLE = 256 };
+__device__ __forceinline__ int scan_flags(int f) {
+  asm volatile("" : "+s"(f));
+  return f;
+}
 
 // V consecutive columns of a row as stored; of the last ones `left` are there (WHOLE: all)
 template <typename E, int V> struct ScanRaw { uint32_t w[V * sizeof(E) / 4]; };
@@ -71,33 +91,27 @@ struct ScanRows {
   // rows that are not in the middle of a sequence
   __device__ __forceinline__ uint64_t events() const { return ~in | first | last; }
 };
-__device__ __forceinline__ ScanRows scan_rows(const ftp_scan_args& a, int64_t r0, int n) {
+__device__ __forceinline__ ScanRows scan_rows(const ScanArgs& k, int64_t r0, int n) {
   ScanRows s;
   const int lane = threadIdx.x & 63;
-  const int64_t r = r0 + lane;
+  const int r = (int)r0 + lane;          // 2^30 rows at most
   bool in = lane < n, first = false, last = false;
-  if (!a.starts) {
-    if (a.length == 1) {
-      s.seq = (int)r;
-      first = last = true;
-    } else {
-      const int64_t q0 = r0 / a.length, d = r0 - q0 * a.length;       // 64 rows in the sequence q0 and those behind it: below 2^31 as length is
-      const uint32_t at = (uint32_t)d + (uint32_t)lane, len = (uint32_t)a.length, q = at / len, m = at - q * len;
-      s.seq = (int)(q0 + q);
-      first = m == 0;
-      last = m == len - 1;
-    }
+  if (!k.starts) {
+    const uint32_t len = (uint32_t)k.length, u = (uint32_t)r, q = len == 1 ? u : u / len, m = u - q * len;
+    s.seq = (int)q;
+    first = m == 0;
+    last = m == len - 1;
   } else {
-    int lo = 0, hi = a.seqs;             // the last sequence that begins at r or in front (of several, all but one are empty)
+    int lo = 0, hi = k.seqs;             // the last sequence that begins at r or in front (of several, all but one are empty)
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if ((int64_t)a.starts[mid] <= r) lo = mid;
+      if (k.starts[mid] <= r) lo = mid;
       else hi = mid - 1;
     }
-    s.seq = lo < a.seqs ? lo : a.seqs - 1;
-    in = in && lo < a.seqs && (int64_t)a.starts[lo] <= r;
-    first = in && (int64_t)a.starts[s.seq] == r;
-    last = in && (int64_t)a.starts[s.seq + 1] == r + 1;
+    s.seq = lo < k.seqs ? lo : k.seqs - 1;
+    in = in && lo < k.seqs && k.starts[lo] <= r;
+    first = in && k.starts[s.seq] == r;
+    last = in && k.starts[s.seq + 1] == r + 1;
   }
   s.in = __ballot(in);
   s.first = __ballot(in && first);
@@ -105,150 +119,150 @@ __device__ __forceinline__ ScanRows scan_rows(const ftp_scan_args& a, int64_t r0
   return s;
 }
 
-// a = sigmoid(f), 1 - a and c(a).  With e = e^-|f| they are 1 / (1 + e) and e / (1 + e), the former a where f >= 0: neither loses its places.  e = 2^t, t = -|f| log2(e) in two
-// parts, so that the rounding of t does not count |t| times (with one part the initial states' gradient of a long batch was twice as far off as its plain form in fp32).
+// a = sigmoid(f), 1 - a and c(a).  With e = e^-|f| the smaller of the first two is q = e / (1 + e), which loses none of its places, and the other 1 - q, rounded once: a
+// long product of factors next to 1 is as exact as they are (1 / (1 + e) by the hardware's reciprocal is off by a place more, and so were the states' gradients).
 struct ScanGate { float a, rest, c; };
 template <int FORM>
 __device__ __forceinline__ ScanGate scan_gate(float f) {
-  const float m = fabsf(f), g = m > 105.f ? 105.f : m;               // e^-105 is 0; NaN stays
-  const float t = g * -1.44269504f, lo = fmaf(g, -1.44269504f, -t) + g * -1.92596303e-8f;
-  const float p = __builtin_amdgcn_exp2f(t), e = fmaf(p, lo * 0.693147181f, p), r = __builtin_amdgcn_rcpf(1.f + e), q = e * r;
+  const float e = __builtin_amdgcn_exp2f(fabsf(f) * -1.44269504f), q = e * __builtin_amdgcn_rcpf(1.f + e), p = 1.f - q;
   const bool up = f >= 0.f;
   ScanGate s;
-  s.a = up ? r : q;
-  s.rest = up ? q : r;
+  s.a = up ? p : q;
+  s.rest = up ? q : p;
   s.c = FORM == FTP_SCAN_MIX ? s.rest : FORM == FTP_SCAN_UNIT ? __builtin_amdgcn_sqrtf(fmaf(s.rest, s.a, s.rest)) : 1.f;
   return s;
 }
-// c's derivative by f
+// lambda's factor in the gradient of f: da/df h + dc/df x, of which da/df = a (1 - a)
 template <int FORM>
-__device__ __forceinline__ float scan_slope(const ScanGate& g) {
-  if (FORM == FTP_SCAN_MIX) return -g.a * g.rest;
-  if (FORM == FTP_SCAN_UNIT) return -g.a * g.a * __builtin_amdgcn_sqrtf(g.rest * __builtin_amdgcn_rcpf(1.f + g.a));
-  return 0.f;
+__device__ __forceinline__ float scan_slope(const ScanGate& g, float h, float x) {
+  const float d = g.a * g.rest;
+  if (FORM == FTP_SCAN_MIX) return d * (h - x);
+  if (FORM == FTP_SCAN_UNIT) return fmaf(d, h, -g.a * g.a * x * g.c * __builtin_amdgcn_rcpf(1.f + g.a));
+  return d * h;
 }
 
 // a wavefront's place: column groups beside one another
 struct ScanAt { int64_t r0; int c, n, left, chunk; };
 template <int V>
 __device__ __forceinline__ ScanAt scan_at(const ScanArgs& k, int64_t wave) {
-  const uint32_t groups = (uint32_t)(k.a.width + 64 * V - 1) / (64 * V), w = (uint32_t)wave;
+  const uint32_t groups = (uint32_t)(k.width + 64 * V - 1) / (64 * V), w = (uint32_t)wave;
   ScanAt p;
   p.chunk = (int)(w / groups);
   p.c = (int)(w - (uint32_t)p.chunk * groups) * 64 * V + (int)(threadIdx.x & 63) * V;
-  p.left = k.a.width - p.c;
+  p.left = k.width - p.c;
   p.r0 = (int64_t)p.chunk * k.per;
-  const int64_t n = k.a.rows - p.r0;
+  const int64_t n = k.rows - p.r0;
   p.n = (int)(n < k.per ? n : k.per);
   return p;
 }
-// kScanR rows of a matrix from the chunk's row t on (behind its last row: that one again)
-template <typename E, int V, bool WHOLE>
-__device__ __forceinline__ void scan_ask(const void* m, int64_t ld, const ScanAt& p, int t, ScanRaw<E, V> r[kScanR]) {
-  const E* const q = (const E*)m + p.r0 * ld;
+// R rows of a matrix, q its rows of the chunk, from the row t on (behind its last row: that one again)
+template <typename E, int V, bool WHOLE, int R>
+__device__ __forceinline__ void scan_ask(const char* q, int ld, const ScanAt& p, int t, ScanRaw<E, V> r[R]) {
 #pragma unroll
-  for (int i = 0; i < kScanR; ++i) {
+  for (int i = 0; i < R; ++i) {
     const int u = t + i < p.n ? t + i : p.n - 1;
-    r[i] = sc_ask<E, V, WHOLE>(q + u * ld + (uint32_t)p.c, p.left);
+    r[i] = sc_ask<E, V, WHOLE>((const E*)(q + u * ld) + (uint32_t)p.c, p.left);
   }
 }
 // a sequence's row of states, or zeros
 template <int V, bool WHOLE>
-__device__ __forceinline__ void scan_state(const float* m, int64_t ld, int seq, const ScanAt& p, float h[V]) {
-  if (m) sc_load<float, V, WHOLE>(m + seq * ld + p.c, p.left, h);
+__device__ __forceinline__ void scan_state(const float* m, int ld, int seq, const ScanAt& p, float h[V]) {
+  if (m) sc_load<float, V, WHOLE>(m + (int64_t)seq * ld + p.c, p.left, h);
   else sc_zero<V>(h);
 }
 
 // A and B of a chunk; backward: C too
-template <typename E, int V, bool WHOLE, int FORM, bool BWD>
+template <typename E, int V, bool WHOLE, int FORM, bool BWD, int R>
 __global__ __launch_bounds__(256) void scan_sums_k(ScanArgs k) {
-  const ftp_scan_args& a = k.a;
-  const int64_t waves = (int64_t)k.chunks * ((a.width + 64 * V - 1) / (64 * V));
-  for (int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); wave < waves; wave += (int64_t)gridDim.x * 4) {
-    const ScanAt p = scan_at<V>(k, wave);
-    const int64_t mine = (int64_t)p.chunk * a.width + p.c;
-    float A[V], B[V], C[V];
+  const int64_t waves = (int64_t)k.chunks * ((k.width + 64 * V - 1) / (64 * V));
+  const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (wave >= waves) return;
+  const ScanAt p = scan_at<V>(k, wave);
+  const int64_t mine = (int64_t)p.chunk * k.width + p.c;
+  float A[V], B[V], C[V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) { A[e] = 1.f; B[e] = C[e] = 0.f; }
-    ScanRaw<E, V> f[kScanR], x[kScanR], g[kScanR], dy[kScanR];
-    const auto ask = [&](int t) __attribute__((always_inline)) {
-      scan_ask<E, V, WHOLE>(a.f, a.ldf, p, t, f);
-      scan_ask<E, V, WHOLE>(a.x, a.ldx, p, t, x);
+  for (int e = 0; e < V; ++e) { A[e] = 1.f; B[e] = C[e] = 0.f; }
+  ScanRaw<E, V> f[R], x[R], g[R], dy[R];
+  const char *const qf = k.f + p.r0 * k.ldf, *const qx = k.x + p.r0 * k.ldx, *const qg = k.g + p.r0 * k.ldg, *const qdy = k.dy + p.r0 * k.lddy;
+  int flags = k.flags;
+  const auto ask = [&](int t) __attribute__((always_inline)) {
+    scan_ask<E, V, WHOLE, R>(qf, k.ldf, p, t, f);
+    scan_ask<E, V, WHOLE, R>(qx, k.ldx, p, t, x);
+    if (BWD) {
+      scan_ask<E, V, WHOLE, R>(qdy, k.lddy, p, t, dy);
+      if (flags & SK_G) scan_ask<E, V, WHOLE, R>(qg, k.ldg, p, t, g);
+    }
+  };
+  if (p.left > 0) ask(0);              // before the search for the sequences
+  const ScanRows rows = scan_rows(k, p.r0, p.n);
+  if (p.left <= 0) return;
+  const uint64_t events = rows.events();
+  for (int t0 = 0; t0 < p.n; t0 += R) {
+    flags = scan_flags(k.flags);
+    float fv[R][V], xv[R][V], into[R][V], gv[R * V];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      sc_open<E, V>(f[i], fv[i]);
+      sc_open<E, V>(x[i], xv[i]);
       if (BWD) {
-        scan_ask<E, V, WHOLE>(a.dy, a.lddy, p, t, dy);
-        if (a.g) scan_ask<E, V, WHOLE>(a.g, a.ldg, p, t, g);
-      }
-    };
-    if (p.left > 0) ask(0);              // before the search for the sequences
-    const ScanRows rows = scan_rows(a, p.r0, p.n);
-    if (p.left <= 0) continue;
-    const uint64_t events = rows.events();
-    for (int t0 = 0; t0 < p.n; t0 += kScanR) {
-      float fv[kScanR][V], xv[kScanR][V], into[kScanR][V], gv[kScanR * V];
-#pragma unroll
-      for (int i = 0; i < kScanR; ++i) {
-        sc_open<E, V>(f[i], fv[i]);
-        sc_open<E, V>(x[i], xv[i]);
-        if (BWD) {
-          sc_open<E, V>(dy[i], into[i]);
-          if (a.g) sc_open<E, V>(g[i], gv + i * V);
-        }
-      }
-      if (t0 + kScanR < p.n) ask(t0 + kScanR);
-      if (BWD && a.g) {
-        tactn<kScanR * V>(gv, a.act);
-#pragma unroll
-        for (int i = 0; i < kScanR; ++i)
-#pragma unroll
-          for (int e = 0; e < V; ++e) into[i][e] *= gv[i * V + e];
-      }
-#pragma unroll
-      for (int i = 0; i < kScanR; ++i) {
-        const int t = t0 + i;
-        const bool event = events >> t & 1;
-        bool last = false;
-        if (event) {
-          if (!(rows.in >> t & 1)) {     // of no sequence, or behind the chunk: nothing goes through
-            if (t < p.n) sc_zero<V>(A);
-            continue;
-          }
-          if (rows.first >> t & 1) {
-            scan_state<V, WHOLE>(a.h0, a.ldh0, rows.of(t), p, B);
-            sc_zero<V>(A);
-            // the state in front of a sequence that goes on behind this chunk, before another chunk writes the one behind it into the same memory
-            if (!BWD) sc_store<float, V, WHOLE>(k.seed + mine, p.left, B);
-          }
-          last = rows.last >> t & 1;
-          if (BWD && last && a.dh_end) {
-            float d[V];
-            scan_state<V, WHOLE>(a.dh_end, a.lddhe, rows.of(t), p, d);
-#pragma unroll
-            for (int e = 0; e < V; ++e) into[i][e] += d[e];
-            // what arrives at the end of a sequence from a chunk in front, before another chunk writes dh0 into the same memory
-            if (!(rows.first << (63 - t))) sc_store<float, V, WHOLE>(k.seed + mine, p.left, d);
-          }
-        }
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const ScanGate s = scan_gate<FORM>(fv[i][e]);
-          B[e] = fmaf(s.a, B[e], s.c * xv[i][e]);
-          A[e] *= s.a;
-          if (BWD) C[e] = fmaf(A[e], into[i][e], C[e]);
-        }
-        if (BWD && last) sc_zero<V>(A);
+        sc_open<E, V>(dy[i], into[i]);
+        if (flags & SK_G) sc_open<E, V>(g[i], gv + i * V);
       }
     }
-    sc_store<float, V, WHOLE>(k.A + mine, p.left, A);
-    sc_store<float, V, WHOLE>(k.B + mine, p.left, B);
-    if (BWD) sc_store<float, V, WHOLE>(k.C + mine, p.left, C);
+    if (t0 + R < p.n) ask(t0 + R);
+    if (BWD && (flags & SK_G)) {
+      tactn<R * V>(gv, k.act);
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int e = 0; e < V; ++e) into[i][e] *= gv[i * V + e];
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int t = t0 + i;
+      const bool event = events >> t & 1;
+      bool last = false;
+      if (event) {
+        if (!(rows.in >> t & 1)) {     // of no sequence, or behind the chunk: nothing goes through
+          if (t < p.n) sc_zero<V>(A);
+          continue;
+        }
+        if (rows.first >> t & 1) {
+          scan_state<V, WHOLE>(k.h0, k.ldh0, rows.of(t), p, B);
+          sc_zero<V>(A);
+          // the state in front of a sequence that goes on behind this chunk, before another chunk writes the one behind it into the same memory
+          if (!BWD) sc_store<float, V, WHOLE>(k.seed + mine, p.left, B);
+        }
+        last = rows.last >> t & 1;
+        if (BWD && last && (flags & SK_DHEND)) {
+          float d[V];
+          scan_state<V, WHOLE>(k.dh_end, k.lddhe, rows.of(t), p, d);
+#pragma unroll
+          for (int e = 0; e < V; ++e) into[i][e] += d[e];
+          // what arrives at the end of a sequence from a chunk in front, before another chunk writes dh0 into the same memory
+          if (!(rows.first << (63 - t))) sc_store<float, V, WHOLE>(k.seed + mine, p.left, d);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const ScanGate s = scan_gate<FORM>(fv[i][e]);
+        B[e] = fmaf(s.a, B[e], s.c * xv[i][e]);
+        A[e] *= s.a;
+        if (BWD) C[e] = fmaf(A[e], into[i][e], C[e]);
+      }
+      if (BWD && last) sc_zero<V>(A);
+    }
   }
+  sc_store<float, V, WHOLE>(k.A + mine, p.left, A);
+  sc_store<float, V, WHOLE>(k.B + mine, p.left, B);
+  if (BWD) sc_store<float, V, WHOLE>(k.C + mine, p.left, C);
 }
 
 // From chunk to chunk: state[i] = the state in front of chunk i; the other way (blockIdx.y 1) back[i] = what chunk i + 1 hands back.  32 columns a block, 32
 // threads to a column, each with its share of the chunks one behind the other: first their product and sum, then the states.
 __global__ __launch_bounds__(1024) void scan_follow_k(ScanArgs k) {
   __shared__ float sa[32][33], sb[32][33];
-  const int lane = threadIdx.x & 31, ty = threadIdx.x >> 5, W = k.a.width, c = blockIdx.x * 32 + lane;
+  const int lane = threadIdx.x & 31, ty = threadIdx.x >> 5, W = k.width, c = blockIdx.x * 32 + lane;
   const bool rev = blockIdx.y == 1;
   const float *const A = k.A, *const B = rev ? k.C : k.B;
   float* const out = rev ? k.back : k.state;
@@ -281,13 +295,12 @@ __global__ __launch_bounds__(1024) void scan_follow_k(ScanArgs k) {
 template <int V, bool WHOLE>
 __device__ __forceinline__ void scan_empty(const ScanArgs& k, int64_t block, const float* from, int64_t ldf, float* to, int64_t ldt) {
   if (!to || from == to) return;
-  const ftp_scan_args& a = k.a;
-  const int groups = (a.width + 64 * V - 1) / (64 * V);
+  const int groups = (k.width + 64 * V - 1) / (64 * V);
   const int64_t seq0 = block / groups * 64, s = seq0 + (threadIdx.x & 63);
   ScanAt p{};
   p.c = (int)(block % groups) * 64 * V + (int)(threadIdx.x & 63) * V;
-  p.left = a.width - p.c;
-  uint64_t todo = __ballot(s < a.seqs && (a.starts ? a.starts[s < a.seqs ? s : 0] >= a.starts[s < a.seqs ? s + 1 : 0] : a.length == 0));
+  p.left = k.width - p.c;
+  uint64_t todo = __ballot(s < k.seqs && (k.starts ? k.starts[s < k.seqs ? s : 0] >= k.starts[s < k.seqs ? s + 1 : 0] : k.length == 0));
   if (p.left <= 0) return;
   while (todo) {
     const int q = (int)seq0 + __builtin_ctzll(todo);
@@ -298,214 +311,243 @@ __device__ __forceinline__ void scan_empty(const ScanArgs& k, int64_t block, con
   }
 }
 
-template <typename E, int V, bool WHOLE, int FORM>
+template <typename E, int V, bool WHOLE, int FORM, int R>
 __global__ __launch_bounds__(256) void scan_walk_k(ScanArgs k) {
-  const ftp_scan_args& a = k.a;
-  const int groups = (a.width + 64 * V - 1) / (64 * V);
-  const int64_t waves = (int64_t)k.chunks * groups, all = waves + (a.starts || a.length == 0 ? (int64_t)((a.seqs + 63) / 64) * groups : 0);
-  for (int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); wave < all; wave += (int64_t)gridDim.x * 4) {
-    if (wave >= waves) {
-      scan_empty<V, WHOLE>(k, wave - waves, a.h0, a.ldh0, a.h_end, a.ldhe);
-      continue;
+  const int groups = (k.width + 64 * V - 1) / (64 * V);
+  const int64_t waves = (int64_t)k.chunks * groups, all = waves + (k.starts || k.length == 0 ? (int64_t)((k.seqs + 63) / 64) * groups : 0);
+  const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (wave >= all) return;
+  if (wave >= waves) {
+    scan_empty<V, WHOLE>(k, wave - waves, k.h0, k.ldh0, k.h_end, k.ldhe);
+    return;
+  }
+  const ScanAt p = scan_at<V>(k, wave);
+  const int64_t mine = (int64_t)p.chunk * k.width + p.c;
+  float h[V];
+  sc_zero<V>(h);
+  ScanRaw<E, V> f[R], x[R], g[R];
+  const char *const qf = k.f + p.r0 * k.ldf, *const qx = k.x + p.r0 * k.ldx, *const qg = k.g + p.r0 * k.ldg;
+  char* const qy = k.y + p.r0 * k.ldy;
+  int flags = k.flags;
+  const auto ask = [&](int t) __attribute__((always_inline)) {
+    scan_ask<E, V, WHOLE, R>(qf, k.ldf, p, t, f);
+    scan_ask<E, V, WHOLE, R>(qx, k.ldx, p, t, x);
+    if (flags & SK_G) scan_ask<E, V, WHOLE, R>(qg, k.ldg, p, t, g);
+  };
+  if (p.left > 0) {
+    if (!(flags & SK_WHOLE)) sc_load<float, V, WHOLE>(k.state + mine, p.left, h);
+    ask(0);
+  }
+  const ScanRows rows = scan_rows(k, p.r0, p.n);
+  if (p.left <= 0) return;
+  const uint64_t events = rows.events();
+  for (int t0 = 0; t0 < p.n; t0 += R) {
+    flags = scan_flags(k.flags);
+    float fv[R][V], xv[R][V], gv[R * V];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      sc_open<E, V>(f[i], fv[i]);
+      sc_open<E, V>(x[i], xv[i]);
+      if (flags & SK_G) sc_open<E, V>(g[i], gv + i * V);
     }
-    const ScanAt p = scan_at<V>(k, wave);
-    const int64_t mine = (int64_t)p.chunk * a.width + p.c;
-    float h[V];
-    sc_zero<V>(h);
-    ScanRaw<E, V> f[kScanR], x[kScanR], g[kScanR];
-    const auto ask = [&](int t) __attribute__((always_inline)) {
-      scan_ask<E, V, WHOLE>(a.f, a.ldf, p, t, f);
-      scan_ask<E, V, WHOLE>(a.x, a.ldx, p, t, x);
-      if (a.g) scan_ask<E, V, WHOLE>(a.g, a.ldg, p, t, g);
-    };
-    if (p.left > 0) {
-      if (!k.whole) sc_load<float, V, WHOLE>(k.state + mine, p.left, h);
-      ask(0);
-    }
-    const ScanRows rows = scan_rows(a, p.r0, p.n);
-    if (p.left <= 0) continue;
-    const uint64_t events = rows.events();
-    for (int t0 = 0; t0 < p.n; t0 += kScanR) {
-      float fv[kScanR][V], xv[kScanR][V], gv[kScanR * V];
+    if (t0 + R < p.n) ask(t0 + R);
+    if (flags & SK_G) tactn<R * V>(gv, k.act);
 #pragma unroll
-      for (int i = 0; i < kScanR; ++i) {
-        sc_open<E, V>(f[i], fv[i]);
-        sc_open<E, V>(x[i], xv[i]);
-        if (a.g) sc_open<E, V>(g[i], gv + i * V);
-      }
-      if (t0 + kScanR < p.n) ask(t0 + kScanR);
-      if (a.g) tactn<kScanR * V>(gv, a.act);
-#pragma unroll
-      for (int i = 0; i < kScanR; ++i) {
-        const int t = t0 + i;
-        bool last = false;
-        if (events >> t & 1) {
-          if (!(rows.in >> t & 1)) continue;
-          if (rows.first >> t & 1) {
-            // one that goes on behind the chunk: its state from the copy
-            if (!k.whole && !(rows.last >> t)) sc_load<float, V, WHOLE>(k.seed + mine, p.left, h);
-            else scan_state<V, WHOLE>(a.h0, a.ldh0, rows.of(t), p, h);
-          }
-          last = rows.last >> t & 1;
+    for (int i = 0; i < R; ++i) {
+      const int t = t0 + i;
+      bool last = false;
+      if (events >> t & 1) {
+        if (!(rows.in >> t & 1)) continue;
+        if (rows.first >> t & 1) {
+          // one that goes on behind the chunk: its state from the copy
+          if (!(flags & SK_WHOLE) && !(rows.last >> t)) sc_load<float, V, WHOLE>(k.seed + mine, p.left, h);
+          else scan_state<V, WHOLE>(k.h0, k.ldh0, rows.of(t), p, h);
         }
-        float y[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const ScanGate s = scan_gate<FORM>(fv[i][e]);
-          h[e] = fmaf(s.a, h[e], s.c * xv[i][e]);
-          y[e] = a.g ? h[e] * gv[i * V + e] : h[e];
-        }
-        if (a.y) sc_store<E, V, WHOLE>((E*)a.y + (p.r0 + t) * a.ldy + (uint32_t)p.c, p.left, y);
-        if (last && a.h_end) sc_store<float, V, WHOLE>(a.h_end + (int64_t)rows.of(t) * a.ldhe + p.c, p.left, h);
+        last = rows.last >> t & 1;
       }
+      float y[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const ScanGate s = scan_gate<FORM>(fv[i][e]);
+        h[e] = fmaf(s.a, h[e], s.c * xv[i][e]);
+        y[e] = flags & SK_G ? h[e] * gv[i * V + e] : h[e];
+      }
+      if (flags & SK_Y) sc_store<E, V, WHOLE>((E*)(qy + t * k.ldy) + (uint32_t)p.c, p.left, y);
+      if (last && (flags & SK_HEND)) sc_store<float, V, WHOLE>(k.h_end + (int64_t)rows.of(t) * k.ldhe + p.c, p.left, h);
     }
   }
 }
 
-// A chunk's states from the first row on, of which those in front of every kScanR rows are kept in LDS; then its gradients from the last row to the first, the states of
-// kScanR rows at a time made again.
-template <typename E, int V, bool WHOLE, int FORM>
+// A chunk's states from the first row on, of which those in front of every R rows are kept in LDS; then its gradients from the last row to the first, the states of
+// R rows at a time made again.
+template <typename E, int V, bool WHOLE, int FORM, int R>
 __global__ __launch_bounds__(256) void scan_back_k(ScanArgs k) {
-  __shared__ float held[4][kScanT / kScanR][64 * V];
-  const ftp_scan_args& a = k.a;
-  const int groups = (a.width + 64 * V - 1) / (64 * V);
-  const int64_t waves = (int64_t)k.chunks * groups, all = waves + (a.starts || a.length == 0 ? (int64_t)((a.seqs + 63) / 64) * groups : 0);
+  __shared__ float held[4][kScanT / R][64 * V];
+  const int groups = (k.width + 64 * V - 1) / (64 * V);
+  const int64_t waves = (int64_t)k.chunks * groups, all = waves + (k.starts || k.length == 0 ? (int64_t)((k.seqs + 63) / 64) * groups : 0);
   const int me = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  for (int64_t wave = (int64_t)blockIdx.x * 4 + me; wave < all; wave += (int64_t)gridDim.x * 4) {
-    if (wave >= waves) {
-      scan_empty<V, WHOLE>(k, wave - waves, a.dh_end, a.lddhe, a.dh0, a.lddh0);
-      continue;
+  const int64_t wave = (int64_t)blockIdx.x * 4 + me;
+  if (wave >= all) return;
+  if (wave >= waves) {
+    scan_empty<V, WHOLE>(k, wave - waves, k.dh_end, k.lddhe, k.dh0, k.lddh0);
+    return;
+  }
+  const ScanAt p = scan_at<V>(k, wave);
+  const int64_t mine = (int64_t)p.chunk * k.width + p.c;
+  float* const keep = held[me][0] + (threadIdx.x & 63) * V;          // a lane's own: nothing to wait for
+  float h[V], mu[V];
+  sc_zero<V>(h);
+  sc_zero<V>(mu);
+  ScanRaw<E, V> f[R], x[R], g[R], dy[R];
+  const char *const qf = k.f + p.r0 * k.ldf, *const qx = k.x + p.r0 * k.ldx, *const qg = k.g + p.r0 * k.ldg, *const qdy = k.dy + p.r0 * k.lddy;
+  char *const qdf = k.df + p.r0 * k.lddf, *const qdx = k.dx + p.r0 * k.lddx, *const qdg = k.dg + p.r0 * k.lddg;
+  int flags = k.flags;
+  if (p.left > 0) {
+    if (!(flags & SK_WHOLE)) {
+      sc_load<float, V, WHOLE>(k.state + mine, p.left, h);
+      sc_load<float, V, WHOLE>(k.back + mine, p.left, mu);
     }
-    const ScanAt p = scan_at<V>(k, wave);
-    const int64_t mine = (int64_t)p.chunk * a.width + p.c;
-    float* const keep = held[me][0] + (threadIdx.x & 63) * V;          // a lane's own: nothing to wait for
-    float h[V], mu[V];
-    sc_zero<V>(h);
-    sc_zero<V>(mu);
-    ScanRaw<E, V> f[kScanR], x[kScanR], g[kScanR], dy[kScanR];
-    if (p.left > 0) {
-      if (!k.whole) {
-        sc_load<float, V, WHOLE>(k.state + mine, p.left, h);
-        sc_load<float, V, WHOLE>(k.back + mine, p.left, mu);
-      }
-      scan_ask<E, V, WHOLE>(a.f, a.ldf, p, 0, f);
-      scan_ask<E, V, WHOLE>(a.x, a.ldx, p, 0, x);
+    scan_ask<E, V, WHOLE, R>(qf, k.ldf, p, 0, f);
+    scan_ask<E, V, WHOLE, R>(qx, k.ldx, p, 0, x);
+  }
+  const ScanRows rows = scan_rows(k, p.r0, p.n);
+  if (p.left <= 0) return;
+  const uint64_t events = rows.events();
+  const int t_end = (p.n - 1) / R * R;
+  const auto ask_back = [&](int t) __attribute__((always_inline)) {
+    scan_ask<E, V, WHOLE, R>(qdy, k.lddy, p, t, dy);
+    if (flags & SK_G) scan_ask<E, V, WHOLE, R>(qg, k.ldg, p, t, g);
+  };
+  for (int t0 = 0;; t0 += R) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) keep[t0 / R * 64 * V + e] = h[e];
+    if (t0 == t_end) break;
+    float fv[R][V], xv[R][V];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      sc_open<E, V>(f[i], fv[i]);
+      sc_open<E, V>(x[i], xv[i]);
     }
-    const ScanRows rows = scan_rows(a, p.r0, p.n);
-    if (p.left <= 0) continue;
-    const uint64_t events = rows.events();
-    const int t_end = (p.n - 1) / kScanR * kScanR;
-    const auto ask_back = [&](int t) __attribute__((always_inline)) {
-      scan_ask<E, V, WHOLE>(a.dy, a.lddy, p, t, dy);
-      if (a.g) scan_ask<E, V, WHOLE>(a.g, a.ldg, p, t, g);
-    };
-    for (int t0 = 0;; t0 += kScanR) {
+    scan_ask<E, V, WHOLE, R>(qf, k.ldf, p, t0 + R, f);
+    scan_ask<E, V, WHOLE, R>(qx, k.ldx, p, t0 + R, x);
 #pragma unroll
-      for (int e = 0; e < V; ++e) keep[t0 / kScanR * 64 * V + e] = h[e];
-      if (t0 == t_end) break;
-      float fv[kScanR][V], xv[kScanR][V];
-#pragma unroll
-      for (int i = 0; i < kScanR; ++i) {
-        sc_open<E, V>(f[i], fv[i]);
-        sc_open<E, V>(x[i], xv[i]);
+    for (int i = 0; i < R; ++i) {
+      const int t = t0 + i;
+      if (events >> t & 1) {
+        if (!(rows.in >> t & 1)) continue;
+        if (rows.first >> t & 1) scan_state<V, WHOLE>(k.h0, k.ldh0, rows.of(t), p, h);
       }
-      scan_ask<E, V, WHOLE>(a.f, a.ldf, p, t0 + kScanR, f);
-      scan_ask<E, V, WHOLE>(a.x, a.ldx, p, t0 + kScanR, x);
 #pragma unroll
-      for (int i = 0; i < kScanR; ++i) {
-        const int t = t0 + i;
-        if (events >> t & 1) {
-          if (!(rows.in >> t & 1)) continue;
-          if (rows.first >> t & 1) scan_state<V, WHOLE>(a.h0, a.ldh0, rows.of(t), p, h);
-        }
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const ScanGate s = scan_gate<FORM>(fv[i][e]);
-          h[e] = fmaf(s.a, h[e], s.c * xv[i][e]);
-        }
+      for (int e = 0; e < V; ++e) {
+        const ScanGate s = scan_gate<FORM>(fv[i][e]);
+        h[e] = fmaf(s.a, h[e], s.c * xv[i][e]);
       }
     }
-    ask_back(t_end);
-    for (int t0 = t_end; t0 >= 0; t0 -= kScanR) {
-      float fv[kScanR][V], xv[kScanR][V], lam[kScanR][V], act[kScanR * V], dact[kScanR * V], before[kScanR][V];
-      ScanGate s[kScanR][V];
+  }
+  ask_back(t_end);
+  for (int t0 = t_end; t0 >= 0; t0 -= R) {
+    flags = scan_flags(k.flags);
+    float fv[R][V], xv[R][V], lam[R][V], act[R * V], dact[R * V], before[R][V], after[R][V];
+    ScanGate s[R][V];
 #pragma unroll
-      for (int i = 0; i < kScanR; ++i) {
-        sc_open<E, V>(f[i], fv[i]);
-        sc_open<E, V>(x[i], xv[i]);
-        sc_open<E, V>(dy[i], lam[i]);
-        if (a.g) sc_open<E, V>(g[i], act + i * V);
+    for (int i = 0; i < R; ++i) {
+      sc_open<E, V>(f[i], fv[i]);
+      sc_open<E, V>(x[i], xv[i]);
+      sc_open<E, V>(dy[i], lam[i]);
+      if (flags & SK_G) sc_open<E, V>(g[i], act + i * V);
+    }
+    if (t0 > 0) {
+      scan_ask<E, V, WHOLE, R>(qf, k.ldf, p, t0 - R, f);
+      scan_ask<E, V, WHOLE, R>(qx, k.ldx, p, t0 - R, x);
+      ask_back(t0 - R);
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) h[e] = keep[t0 / R * 64 * V + e];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int t = t0 + i;
+#pragma unroll
+      for (int e = 0; e < V; ++e) s[i][e] = scan_gate<FORM>(fv[i][e]);
+      if ((events >> t & 1) && (rows.first >> t & 1)) scan_state<V, WHOLE>(k.h0, k.ldh0, rows.of(t), p, h);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        before[i][e] = h[e];
+        after[i][e] = h[e] = fmaf(s[i][e].a, h[e], s[i][e].c * xv[i][e]);
       }
-      if (t0 > 0) {
-        scan_ask<E, V, WHOLE>(a.f, a.ldf, p, t0 - kScanR, f);
-        scan_ask<E, V, WHOLE>(a.x, a.ldx, p, t0 - kScanR, x);
-        ask_back(t0 - kScanR);
-      }
+    }
+    if (flags & SK_G) tact_gradn<R * V>(act, act, dact, k.act);
 #pragma unroll
-      for (int e = 0; e < V; ++e) h[e] = keep[t0 / kScanR * 64 * V + e];
-#pragma unroll
-      for (int i = 0; i < kScanR; ++i) {
-        const int t = t0 + i;
-#pragma unroll
-        for (int e = 0; e < V; ++e) s[i][e] = scan_gate<FORM>(fv[i][e]);
-        if ((events >> t & 1) && (rows.first >> t & 1)) scan_state<V, WHOLE>(a.h0, a.ldh0, rows.of(t), p, h);
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          before[i][e] = h[e];
-          h[e] = fmaf(s[i][e].a, h[e], s[i][e].c * xv[i][e]);
+    for (int i = R - 1; i >= 0; --i) {
+      const int t = t0 + i;
+      bool first = false;
+      if (events >> t & 1) {
+        if (!(rows.in >> t & 1)) continue;
+        if (rows.last >> t & 1) {
+          // of a sequence from a chunk in front: the copy of what arrives at its end
+          if ((flags & SK_DHEND) && !(flags & SK_WHOLE) && !(rows.first << (63 - t))) sc_load<float, V, WHOLE>(k.seed + mine, p.left, mu);
+          else scan_state<V, WHOLE>(k.dh_end, k.lddhe, rows.of(t), p, mu);
         }
+        first = rows.first >> t & 1;
       }
-      if (a.g) tact_gradn<kScanR * V>(act, act, dact, a.act);
+      float dg[V], df[V], dx[V];
 #pragma unroll
-      for (int i = kScanR - 1; i >= 0; --i) {
-        const int t = t0 + i;
-        bool first = false;
-        if (events >> t & 1) {
-          if (!(rows.in >> t & 1)) continue;
-          if (rows.last >> t & 1) {
-            // of a sequence from a chunk in front: the copy of what arrives at its end
-            if (a.dh_end && !k.whole && !(rows.first << (63 - t))) sc_load<float, V, WHOLE>(k.seed + mine, p.left, mu);
-            else scan_state<V, WHOLE>(a.dh_end, a.lddhe, rows.of(t), p, mu);
-          }
-          first = rows.first >> t & 1;
+      for (int e = 0; e < V; ++e) {
+        const ScanGate& q = s[i][e];
+        if (flags & SK_G) {
+          dg[e] = lam[i][e] * after[i][e] * dact[i * V + e];
+          lam[i][e] *= act[i * V + e];
         }
-        const int64_t r = p.r0 + t;
-        float dg[V], df[V], dx[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const ScanGate& q = s[i][e];
-          if (a.g) {
-            dg[e] = lam[i][e] * fmaf(q.a, before[i][e], q.c * xv[i][e]) * dact[i * V + e];
-            lam[i][e] *= act[i * V + e];
-          }
-          const float l = lam[i][e] + mu[e];
-          dx[e] = l * q.c;
-          df[e] = l * fmaf(before[i][e], q.a * q.rest, xv[i][e] * scan_slope<FORM>(q));
-          mu[e] = l * q.a;
-        }
-        if (a.dg) sc_store<E, V, WHOLE>((E*)a.dg + r * a.lddg + (uint32_t)p.c, p.left, dg);
-        if (a.df) sc_store<E, V, WHOLE>((E*)a.df + r * a.lddf + (uint32_t)p.c, p.left, df);
-        if (a.dx) sc_store<E, V, WHOLE>((E*)a.dx + r * a.lddx + (uint32_t)p.c, p.left, dx);
-        if (first && a.dh0) sc_store<float, V, WHOLE>(a.dh0 + (int64_t)rows.of(t) * a.lddh0 + p.c, p.left, mu);
+        const float l = lam[i][e] + mu[e];
+        dx[e] = l * q.c;
+        df[e] = l * scan_slope<FORM>(q, before[i][e], xv[i][e]);
+        mu[e] = l * q.a;
       }
+      if (flags & SK_DG) sc_store<E, V, WHOLE>((E*)(qdg + t * k.lddg) + (uint32_t)p.c, p.left, dg);
+      if (flags & SK_DF) sc_store<E, V, WHOLE>((E*)(qdf + t * k.lddf) + (uint32_t)p.c, p.left, df);
+      if (flags & SK_DX) sc_store<E, V, WHOLE>((E*)(qdx + t * k.lddx) + (uint32_t)p.c, p.left, dx);
+      if (first && (flags & SK_DH0)) sc_store<float, V, WHOLE>(k.dh0 + (int64_t)rows.of(t) * k.lddh0 + p.c, p.left, mu);
     }
   }
 }
 
-// rows of a chunk; where whole sequences fit into one, as few of them as fill the card
+// rows of a chunk: as few as fill the card with wavefronts (a chunk is walked row by row: 1500 x 333 fp32, forward and backward, 32 rows 51 us); where whole sequences fit
+// into one, no more than they have
 static int scan_per(const ftp_scan_args& a, int V, bool& whole) {
+  const int64_t groups = (a.width + 64 * V - 1) / (64 * V);
   whole = a.starts ? a.rows <= kScanT : a.length <= kScanT;
-  if (a.starts || a.length == 0 || !whole) return kScanT;
-  const int64_t groups = (a.width + 64 * V - 1) / (64 * V), fit = kScanT / a.length;
-  return (int)(std::max<int64_t>(1, std::min<int64_t>(fit, a.seqs * groups / 4096)) * a.length);
+  if (!a.starts && a.length > 0 && whole) return (int)(std::max<int64_t>(1, std::min<int64_t>(kScanT / a.length, a.seqs * groups / 4096)) * a.length);
+  int per = kScanT;
+  while (!whole && per > 8 && (a.rows + per - 1) / per * groups < 4096) per /= 2;
+  return per;
 }
 static int scan_columns(const ftp_scan_args& a) { return a.dtype == FTP_BF16 ? 2 : 1; }
 static ScanArgs scan_plan(const ftp_scan_args& a, bool backward, size_t& bytes) {
   ScanArgs k{};
-  k.a = a;
+  const int es = a.dtype == FTP_BF16 ? 2 : 4;
+  const auto in = [&](const char*& p, int& ld, const void* m, int64_t l, int bit) { p = (const char*)m; ld = (int)(l * es); k.flags |= m ? bit : 0; };
+  const auto to = [&](char*& p, int& ld, void* m, int64_t l, int bit) { p = (char*)m; ld = (int)(l * es); k.flags |= m ? bit : 0; };
+  in(k.f, k.ldf, a.f, a.ldf, 0);
+  in(k.x, k.ldx, a.x, a.ldx, 0);
+  in(k.g, k.ldg, a.g, a.ldg, SK_G);
+  k.h0 = a.h0; k.ldh0 = (int)a.ldh0;
+  if (backward) {
+    in(k.dy, k.lddy, a.dy, a.lddy, 0);
+    to(k.df, k.lddf, a.df, a.lddf, SK_DF);
+    to(k.dx, k.lddx, a.dx, a.lddx, SK_DX);
+    if (a.g) to(k.dg, k.lddg, a.dg, a.lddg, SK_DG);
+    k.dh_end = a.dh_end; k.lddhe = (int)a.lddhe;
+    k.dh0 = a.dh0; k.lddh0 = (int)a.lddh0;
+    k.flags |= (a.dh_end ? SK_DHEND : 0) | (a.dh0 ? SK_DH0 : 0);
+  } else {
+    to(k.y, k.ldy, a.y, a.ldy, SK_Y);
+    k.h_end = a.h_end; k.ldhe = (int)a.ldhe;
+    k.flags |= a.h_end ? SK_HEND : 0;
+  }
+  k.rows = a.rows; k.length = a.length; k.starts = a.starts;
+  k.width = a.width; k.seqs = a.seqs; k.act = a.act;
   bool whole;
   k.per = scan_per(a, scan_columns(a), whole);
-  k.whole = whole;
+  k.flags |= whole ? SK_WHOLE : 0;
   k.chunks = (int)((a.rows + k.per - 1) / k.per);
   bytes = 0;
   if (whole) return k;
@@ -524,32 +566,33 @@ size_t bt_scan_bytes(const ftp_scan_args& a, bool backward) {
   return n;
 }
 static unsigned scan_blocks(const ScanArgs& k, int V, bool walk) {
-  const int64_t groups = (k.a.width + 64 * V - 1) / (64 * V);
-  const int64_t waves = groups * (k.chunks + (walk && (k.a.starts || k.a.length == 0) ? (k.a.seqs + 63) / 64 : 0));
-  return (unsigned)std::max<int64_t>(1, std::min<int64_t>((waves + 3) / 4, 1 << 20));
+  const int64_t groups = (k.width + 64 * V - 1) / (64 * V);
+  const int64_t waves = groups * (k.chunks + (walk && (k.starts || k.length == 0) ? (k.seqs + 63) / 64 : 0));
+  return (unsigned)std::max<int64_t>(1, (waves + 3) / 4);
 }
 template <bool BWD, typename E, int V, bool WHOLE, int FORM>
 static void scan_launch(hipStream_t st, const ScanArgs& k) {
-  if (!k.whole) {
-    hipLaunchKernelGGL((scan_sums_k<E, V, WHOLE, FORM, BWD>), dim3(scan_blocks(k, V, false)), dim3(256), 0, st, k);
-    hipLaunchKernelGGL(scan_follow_k, dim3((k.a.width + 31) / 32, BWD ? 2 : 1), dim3(1024), 0, st, k);
+  if (scan_blocks(k, V, true) >= 1u << 24) return launch_plan_failed("scan: more than 2^32 threads");
+  if (!(k.flags & SK_WHOLE)) {
+    hipLaunchKernelGGL((scan_sums_k<E, V, WHOLE, FORM, BWD, BWD ? SRB : SRF>), dim3(scan_blocks(k, V, false)), dim3(256), 0, st, k);
+    hipLaunchKernelGGL(scan_follow_k, dim3((k.width + 31) / 32, BWD ? 2 : 1), dim3(1024), 0, st, k);
   }
-  if (BWD) hipLaunchKernelGGL((scan_back_k<E, V, WHOLE, FORM>), dim3(scan_blocks(k, V, true)), dim3(256), 0, st, k);
-  else hipLaunchKernelGGL((scan_walk_k<E, V, WHOLE, FORM>), dim3(scan_blocks(k, V, true)), dim3(256), 0, st, k);
+  if (BWD) hipLaunchKernelGGL((scan_back_k<E, V, WHOLE, FORM, SRK>), dim3(scan_blocks(k, V, true)), dim3(256), 0, st, k);
+  else hipLaunchKernelGGL((scan_walk_k<E, V, WHOLE, FORM, SRW>), dim3(scan_blocks(k, V, true)), dim3(256), 0, st, k);
 }
 template <bool BWD, typename E, int V, bool WHOLE>
-static void scan_form(hipStream_t st, const ScanArgs& k) {
-  if (k.a.form == FTP_SCAN_ADD) scan_launch<BWD, E, V, WHOLE, FTP_SCAN_ADD>(st, k);
-  else if (k.a.form == FTP_SCAN_MIX) scan_launch<BWD, E, V, WHOLE, FTP_SCAN_MIX>(st, k);
+static void scan_form(hipStream_t st, const ScanArgs& k, int form) {
+  if (form == FTP_SCAN_ADD) scan_launch<BWD, E, V, WHOLE, FTP_SCAN_ADD>(st, k);
+  else if (form == FTP_SCAN_MIX) scan_launch<BWD, E, V, WHOLE, FTP_SCAN_MIX>(st, k);
   else scan_launch<BWD, E, V, WHOLE, FTP_SCAN_UNIT>(st, k);
 }
 template <bool BWD>
 static void scan_go(hipStream_t st, const ftp_scan_args& a) {
   size_t bytes;
   const ScanArgs k = scan_plan(a, BWD, bytes);
-  if (a.dtype == FTP_F32) scan_form<BWD, float, 1, true>(st, k);
-  else if (a.width % 2 == 0) scan_form<BWD, bf16_t, 2, true>(st, k);
-  else scan_form<BWD, bf16_t, 2, false>(st, k);
+  if (a.dtype == FTP_F32) scan_form<BWD, float, 1, true>(st, k, a.form);
+  else if (a.width % 2 == 0) scan_form<BWD, bf16_t, 2, true>(st, k, a.form);
+  else scan_form<BWD, bf16_t, 2, false>(st, k, a.form);
 }
 void bt_scan(hipStream_t st, const ftp_scan_args& a) {
   const double n = (double)a.rows * a.width;
