@@ -3,19 +3,23 @@
 // With m the row's largest logit and t = scale (z - m):  s1 = sum e^t, s2 = sum t e^t, and
 //   lse = scale m + log s1,   logp = t[id] - log s1,   entropy = log s1 - s2 / s1.
 // m and log s1 go to the backward, not their sum: where m is large (a row of the type's lowest value) it would hold nothing of log s1.
-// A row is cut into segments where there are few of them; what a block found out about its segment (m, s1, s2 and its likeliest tokens) is joined by a second launch.
+// A block of T threads has a segment of a row in registers, read once: its largest, then the sums, then (with `top`) its likeliest tokens.  One segment is a row where there are rows enough; a
+// second launch joins several.
+#include <type_traits>
+
 #include "between.h"
 #include "token_dev.h"
 
 namespace ftp {
 
-enum { kLogpT = 256 };
+enum { kLogpHeld = 512 };             // candidates for the likeliest that a block keeps
 #define FTP_LOG2E 1.4426950408889634f
 #define FTP_LN2 0.6931471805599453f
 #define FTP_LEAST -3.402823466e38f
 
 struct LogpPlan {
   int segs, seg;               // segments of a row, columns of each (a multiple of 8)
+  int threads, vectors;        // of a block; eights of columns a thread
   float* part;                 // [rows][segs][4]: m, s1, s2
   unsigned long long* tops;    // [rows][segs][top]
 };
@@ -52,24 +56,25 @@ __device__ __forceinline__ LogpSum logp_join(LogpSum a, LogpSum b, float scale) 
   return LogpSum{m, fmaf(a.s1, ea, b.s1 * eb), ea * fmaf(logp_floor(ta), a.s1, a.s2) + eb * fmaf(logp_floor(tb), b.s1, b.s2)};
 }
 
+// the given token's logit, asked for early; NaN for an id that is no token's
+struct LogpGiven { float z; bool pad; };
 template <typename E>
-__device__ __forceinline__ float logp_logit(const ftp_logp_args& a, int64_t row, int64_t id) { return to_f32(((const E*)a.logits)[row * a.ldl + id]); }
-
+__device__ __forceinline__ LogpGiven logp_given(const ftp_logp_args& a, int64_t row) {
+  LogpGiven g{__uint_as_float(0x7fc00000u), false};
+  if (!a.logp) return g;
+  const int64_t id = a.ids64 ? ((const int64_t*)a.ids)[row] : (int64_t)((const int32_t*)a.ids)[row];
+  g.pad = id == a.pad_id;
+  if (id >= 0 && id < a.vocab) g.z = to_f32(((const E*)a.logits)[row * a.ldl + id]);
+  return g;
+}
 // a row's results but the likeliest; one thread
-template <typename E>
-__device__ __forceinline__ void logp_finish(const ftp_logp_args& a, int64_t row, LogpSum s) {
+__device__ __forceinline__ void logp_finish(const ftp_logp_args& a, int64_t row, LogpSum s, LogpGiven g) {
   const float l = __builtin_amdgcn_logf(s.s1) * FTP_LN2;         // nothing but -inf: -inf
   const bool none = s.s1 == 0.f;
   if (a.lse) a.lse[row] = none ? l : fmaf(s.m, a.scale, l);
   if (a.stats) { a.stats[2 * row] = s.m; a.stats[2 * row + 1] = l; }
   if (a.entropy) a.entropy[row] = none ? 0.f : l - s.s2 / s.s1;
-  if (a.logp) {
-    const int64_t id = a.ids64 ? ((const int64_t*)a.ids)[row] : (int64_t)((const int32_t*)a.ids)[row];
-    float v = __uint_as_float(0x7fc00000u);
-    if (id == a.pad_id) v = 0.f;
-    else if (id >= 0 && id < a.vocab) v = none ? l : (logp_logit<E>(a, row, id) - s.m) * a.scale - l;
-    a.logp[row] = v;
-  }
+  if (a.logp) a.logp[row] = g.pad ? 0.f : g.z != g.z ? g.z : none ? l : (g.z - s.m) * a.scale - l;
 }
 // place t of the likeliest
 __device__ __forceinline__ void logp_place(const ftp_logp_args& a, int64_t row, int t, unsigned long long key, LogpSum s) {
@@ -78,109 +83,301 @@ __device__ __forceinline__ void logp_place(const ftp_logp_args& a, int64_t row, 
   a.top_logp[row * a.top + t] = nan ? s.s1 : key ? (logp_value(key) - s.m) * a.scale - __builtin_amdgcn_logf(s.s1) * FTP_LN2 : -__builtin_inff();
 }
 
-template <typename E>
-__global__ __launch_bounds__(kLogpT) void logp_k(ftp_logp_args a, LogpPlan p) {
-  __shared__ LogpSum sums[kLogpT / 64];
-  __shared__ unsigned long long best[2][kLogpT / 64];
-  const int64_t jobs = a.rows * p.segs;
-  for (int64_t job = blockIdx.x; job < jobs; job += gridDim.x) {
-    const int64_t row = job / p.segs;
-    const int seg = (int)(job - row * p.segs), c0 = seg * p.seg, c1 = c0 + p.seg < a.vocab ? c0 + p.seg : a.vocab;
-    const E* const z = (const E*)a.logits + row * a.ldl;
-    LogpSum s{FTP_LEAST, 0.f, 0.f};
-    for (int c = c0 + threadIdx.x * 8; c < c1; c += kLogpT * 8) {
-      float v[8];
-      tk_load8<E>(z + c, c1 - c, v);
-      float m = s.m;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (c + e >= c1) v[e] = -__builtin_inff();
-        m = fmaxf(m, v[e]);
-      }
-      const float t0 = (s.m - m) * a.scale, e0 = logp_exp(t0);
-      s.s2 = e0 * fmaf(logp_floor(t0), s.s1, s.s2);
-      s.s1 *= e0;
-      s.m = m;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float t = (v[e] - m) * a.scale, x = logp_exp(t);
-        s.s1 += x;
-        s.s2 = fmaf(x, logp_floor(t), s.s2);
-      }
+__device__ __forceinline__ float wave_max_last(float x) {        // in the last lane
+  x = fmaxf(x, dpp_move<0xB1>(x));
+  x = fmaxf(x, dpp_move<0x4E>(x));
+  x = fmaxf(x, dpp_move<0x141>(x));
+  x = fmaxf(x, dpp_move<0x140>(x));
+  // row_bcast 15 and 31; lanes that receive nothing keep theirs
+  x = fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, x), __builtin_bit_cast(int, x), 0x142, 0xA, 0xF, false)));
+  return fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, x), __builtin_bit_cast(int, x), 0x143, 0xC, 0xF, false)));
+}
+__device__ __forceinline__ uint32_t logp_order(float v) {        // larger values, larger numbers; -0 as 0
+  const uint32_t b = __float_as_uint(v + 0.f);
+  return b ^ (b >> 31 ? 0xffffffffu : 0x80000000u);
+}
+
+// The k largest keys of a block, in their order, at put(place, key).  s.group holds the largest of each of 64 groups of T / 64 lanes beside one another (a barrier has passed).  Of these the
+// k-th is a bound that at least k keys reach (fewer groups than k with a key: any); those that do, some more than k as a rule, are shown by some(bound, f) and kept in LDS, where each
+// counts the larger ones.  Too many that are alike: one after another, each the largest below the last of those that all(f) shows.
+struct LogpTop {
+  uint32_t group[64];
+  uint32_t bound, count;
+  unsigned long long kept[kLogpHeld];
+  unsigned long long best[2][16];
+};
+template <int T, typename S, typename A, typename P>
+__device__ __forceinline__ void block_top(LogpTop& s, int k, S some, A all, P put) {
+  if (threadIdx.x < 64) {
+    const uint32_t g = s.group[threadIdx.x];
+    uint32_t b = 0;
+#pragma unroll 1
+    for (int bit = 30; bit >= 0; bit -= 2) {                     // two bits at a time: three counts that do not wait for one another
+      const uint32_t c1 = b | 1u << bit, c2 = b | 2u << bit, c3 = b | 3u << bit;
+      const int n1 = __popcll(__ballot(g >= c1)), n2 = __popcll(__ballot(g >= c2)), n3 = __popcll(__ballot(g >= c3));
+      b = n3 >= k ? c3 : n2 >= k ? c2 : n1 >= k ? c1 : b;
     }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) s = logp_join(s, LogpSum{__shfl_xor(s.m, d), __shfl_xor(s.s1, d), __shfl_xor(s.s2, d)}, a.scale);
-    __syncthreads();                     // the last job's readers are done
-    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
-    __syncthreads();
-    s = sums[0];
-#pragma unroll
-    for (int i = 1; i < kLogpT / 64; ++i) s = logp_join(s, sums[i], a.scale);
-    if (p.segs == 1) {
-      if (threadIdx.x == 0) logp_finish<E>(a, row, s);
-    } else if (threadIdx.x == 0) {
-      float* const o = p.part + job * 4;
-      o[0] = s.m; o[1] = s.s1; o[2] = s.s2;
+    if (threadIdx.x == 0) { s.bound = b ? b : 1; s.count = 0; }
+  }
+  __syncthreads();
+  some(s.bound, [&](unsigned long long key) {
+    const uint32_t at = atomicAdd(&s.count, 1u);                 // the order does not matter: places go by the keys
+    if (at < kLogpHeld) s.kept[at] = key;
+  });
+  __syncthreads();
+  const int n = (int)s.count;
+  if (n <= kLogpHeld) {
+    for (int i = threadIdx.x; i < n; i += T) {
+      const unsigned long long key = s.kept[i];
+      int larger = 0;
+#pragma unroll 8
+      for (int j = 0; j < n; ++j) larger += s.kept[j] > key;
+      if (larger < k) put(larger, key);
     }
-    // the likeliest, one after another: the largest below the last one
+    for (int i = n + threadIdx.x; i < k; i += T) put(i, 0);
+  } else {
     unsigned long long below = ~0ull;
-    for (int t = 0; t < a.top; ++t) {
+    for (int t = 0; t < k; ++t) {
       unsigned long long b = 0;
-      if (below)
-        for (int c = c0 + (int)threadIdx.x; c < c1; c += kLogpT) {
-          const unsigned long long q = logp_key(to_f32(z[c]), c);
-          if (q < below && q > b) b = q;
-        }
+      all([&](unsigned long long key) { if (key < below && key > b) b = key; });
       b = wave_max64(b);
-      unsigned long long* const w = best[t & 1];
+      unsigned long long* const w = s.best[t & 1];
       if ((threadIdx.x & 63) == 0) w[threadIdx.x >> 6] = b;
       __syncthreads();
       b = w[0];
 #pragma unroll
-      for (int i = 1; i < kLogpT / 64; ++i) b = w[i] > b ? w[i] : b;
+      for (int i = 1; i < T / 64; ++i) b = w[i] > b ? w[i] : b;
       below = b;
-      if (threadIdx.x) continue;
-      if (p.segs > 1) p.tops[job * a.top + t] = b;
-      else logp_place(a, row, t, b, s);
+      if (threadIdx.x == 0) put(t, b);
     }
   }
 }
 
-// one wavefront a row: its segments' sums in a fixed order, then the likeliest of their lists
+// eight columns as stored; what is not there: -inf
+template <typename E> struct LogpRaw { uint32_t w[2 * sizeof(E)]; };
 template <typename E>
-__global__ __launch_bounds__(64) void logp_join_k(ftp_logp_args a, LogpPlan p) {
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    LogpSum s{FTP_LEAST, 0.f, 0.f};
-    for (int i = threadIdx.x; i < p.segs; i += 64) {
-      const float* const o = p.part + (row * p.segs + i) * 4;
-      s = logp_join(s, LogpSum{o[0], o[1], o[2]}, a.scale);
-    }
+__device__ __forceinline__ LogpRaw<E> logp_load(const E* p, int left) {
+  if (left >= 8) {
+    struct __attribute__((packed, aligned(sizeof(E)))) At { uint32_t w[2 * sizeof(E)]; };
+    const At t = *reinterpret_cast<const At*>(p);
+    LogpRaw<E> r;
+    __builtin_memcpy(&r, &t, sizeof(r));
+    return r;
+  }
+  E t[8];
 #pragma unroll
-    for (int d = 32; d; d >>= 1) s = logp_join(s, LogpSum{__shfl_xor(s.m, d), __shfl_xor(s.s1, d), __shfl_xor(s.s2, d)}, a.scale);
-    if (threadIdx.x == 0) logp_finish<E>(a, row, s);
-    const unsigned long long* const t0 = p.tops + row * p.segs * a.top;
-    unsigned long long below = ~0ull;
-    for (int t = 0; t < a.top; ++t) {
-      unsigned long long b = 0;
-      for (int i = threadIdx.x; i < p.segs * a.top; i += 64) {
-        const unsigned long long q = t0[i];
-        if (q < below && q > b) b = q;
-      }
-      b = wave_max64(b);
-      below = b;
-      if (threadIdx.x == 0) logp_place(a, row, t, b, s);
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t none = sizeof(E) == 2 ? 0xff80u : 0xff800000u;
+    __builtin_memcpy(&t[e], &none, sizeof(E));
+    if (e < left) t[e] = p[e];
+  }
+  LogpRaw<E> r;
+  __builtin_memcpy(&r, t, sizeof(r));
+  return r;
+}
+template <typename E>
+__device__ __forceinline__ float logp_at(const LogpRaw<E>& r, int e) {
+  if constexpr (sizeof(E) == 4) return __uint_as_float(r.w[e]);
+  else return __uint_as_float(e & 1 ? r.w[e / 2] & 0xffff0000u : r.w[e / 2] << 16);
+}
+// the next pass opens them again: opened, they would take twice the registers
+template <typename E>
+__device__ __forceinline__ void logp_anew(LogpRaw<E>& r) {
+#pragma unroll
+  for (int i = 0; i < (int)(2 * sizeof(E)); ++i) asm volatile("" : "+v"(r.w[i]));
+}
+
+// TOP: with likeliest tokens
+template <typename E, int T, int NV, bool TOP>
+__global__ __launch_bounds__(T) void logp_k(ftp_logp_args a, LogpPlan p) {
+  __shared__ float most[T / 64];
+  __shared__ float2 sums[T / 64];
+  __shared__ typename std::conditional<TOP, LogpTop, int>::type top;
+  const int64_t jobs = a.rows * p.segs;
+  for (int64_t job = blockIdx.x; job < jobs; job += gridDim.x) {
+    const int64_t row = p.segs == 1 ? job : job / p.segs;
+    const int seg = (int)(job - row * p.segs), c0 = seg * p.seg, n = p.seg < a.vocab - c0 ? p.seg : a.vocab - c0;
+    const E* const z = (const E*)a.logits + row * a.ldl + c0;
+    LogpGiven given{};
+    if (p.segs == 1 && threadIdx.x < 64) given = logp_given<E>(a, row);
+    LogpRaw<E> r[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = (v * T + (int)threadIdx.x) * 8;
+      r[v] = logp_load<E>(z + c, n - c);
     }
+    float m = FTP_LEAST;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) m = fmaxf(m, logp_at<E>(r[v], e));
+    if constexpr (TOP) {
+      // the groups' largest (nothing above the least: no key, 0)
+      float g = m;
+      if (T > 64) g = fmaxf(g, dpp_move<0xB1>(g));
+      if (T > 128) g = fmaxf(g, dpp_move<0x4E>(g));
+      if (T > 256) g = fmaxf(g, dpp_move<0x141>(g));
+      if (T > 512) g = fmaxf(g, dpp_move<0x140>(g));
+      if ((threadIdx.x & (T / 64 - 1)) == 0) top.group[threadIdx.x / (T / 64)] = g > FTP_LEAST ? logp_order(g) : 0;
+    }
+    const float wm = wave_max_last(m);
+    if ((threadIdx.x & 63) == 63) most[threadIdx.x >> 6] = wm;
+    __syncthreads();
+    m = most[0];
+#pragma unroll
+    for (int i = 1; i < T / 64; ++i) m = fmaxf(m, most[i]);
+    // e^t = 2^d, d = k z - k m with one rounding, which leaves the rounding of k m in all of them: taken off the sum below.  Where k m is not a number that can be taken off
+    // (infinite, or nothing but -inf) d = k (z - m)
+    const float k = a.scale * FTP_LOG2E, km = m * k;
+    const bool plain = fabsf(km) < 1e30f;
+    float s1 = 0.f, s2 = 0.f;
+    const auto add = [&](auto fused) __attribute__((always_inline)) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        logp_anew<E>(r[v]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float z = logp_at<E>(r[v], e), d = fused.value ? fmaf(z, k, -km) : (z - m) * k, x = __builtin_amdgcn_exp2f(d);
+          s1 += x;
+          s2 = fmaf(x, fmaxf(d, -300.f), s2);
+        }
+      }
+    };
+    if (plain) add(std::true_type());
+    else add(std::false_type());
+    const float off = plain ? fmaf(m, k, -km) : 0.f;             // of every d
+    s1 = wave_sum_last(s1);
+    s2 = wave_sum_last(s2);
+    if ((threadIdx.x & 63) == 63) sums[threadIdx.x >> 6] = make_float2(s1, s2);
+    if (!TOP) __syncthreads();           // block_top has some
+    const auto total = [&]() {
+      LogpSum s{m, sums[0].x, sums[0].y};
+#pragma unroll
+      for (int i = 1; i < T / 64; ++i) { s.s1 += sums[i].x; s.s2 += sums[i].y; }
+      // 2^(d + off): sums off by that factor, the second by off times the first as well
+      s.s2 = fmaf(-off, s.s1, s.s2) * FTP_LN2;
+      const float f = fmaf(-off, FTP_LN2, 1.f);
+      s.s1 *= f;
+      s.s2 *= f;
+      return s;
+    };
+    if constexpr (TOP) {
+      block_top<T>(top, a.top, [&](uint32_t bound, auto f) {
+        // as a float: what is at least this has a key at least the bound (1: any logit above -inf)
+        const float lo = bound == 1 ? FTP_LEAST : logp_value((unsigned long long)bound << 32);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+          logp_anew<E>(r[v]);
+          float big = logp_at<E>(r[v], 0);
+#pragma unroll
+          for (int e = 1; e < 8; ++e) big = fmaxf(big, logp_at<E>(r[v], e));
+          if (!(big >= lo)) continue;    // few eights have one
+#pragma unroll 1
+          for (int e = 0; e < 8; ++e) {
+            float x = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x = e == i ? logp_at<E>(r[v], i) : x;
+            if (x >= lo) f(logp_key(x, c0 + (v * T + (int)threadIdx.x) * 8 + e));
+          }
+        }
+      }, [&](auto f) {
+        for (int c = threadIdx.x; c < n; c += T) f(logp_key(to_f32(z[c]), c0 + c));
+      }, [&](int t, unsigned long long key) {
+        if (p.segs > 1) p.tops[job * a.top + t] = key;
+        else logp_place(a, row, t, key, total());
+      });
+    }
+    if (threadIdx.x == 0) {
+      const LogpSum s = total();
+      if (p.segs == 1) logp_finish(a, row, s, given);
+      else {
+        float* const o = p.part + job * 4;
+        o[0] = s.m; o[1] = s.s1; o[2] = s.s2;
+      }
+    }
+    if (job + gridDim.x < jobs) __syncthreads();                 // LDS is read to the end
   }
 }
 
-// segments: enough blocks for the card, of 2048 columns at least
+// one block a row: its segments' sums in a fixed order, then the likeliest of their lists
+template <typename E>
+__global__ __launch_bounds__(256) void logp_join_k(ftp_logp_args a, LogpPlan p) {
+  __shared__ LogpSum whole;
+  __shared__ LogpTop top;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const unsigned long long* const t0 = p.tops + row * p.segs * a.top;
+    const int n = p.segs * a.top;
+    // the largest of a thread's keys, then of its group's four
+    uint32_t g = 0;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n; i += 256) {
+      const uint32_t q = (uint32_t)(t0[i] >> 32);
+      g = q > g ? q : g;
+    }
+    if (threadIdx.x < 64) {
+      const LogpGiven given = logp_given<E>(a, row);
+      LogpSum s{FTP_LEAST, 0.f, 0.f};
+      for (int i = threadIdx.x; i < p.segs; i += 64) {
+        const float* const o = p.part + (row * p.segs + i) * 4;
+        s = logp_join(s, LogpSum{o[0], o[1], o[2]}, a.scale);
+      }
+#pragma unroll
+      for (int d = 32; d; d >>= 1) s = logp_join(s, LogpSum{__shfl_xor(s.m, d), __shfl_xor(s.s1, d), __shfl_xor(s.s2, d)}, a.scale);
+      if (threadIdx.x == 0) {
+        logp_finish(a, row, s, given);
+        whole = s;
+      }
+    }
+    if (a.top) {
+      uint32_t o = __shfl_xor(g, 1);
+      g = o > g ? o : g;
+      o = __shfl_xor(g, 2);
+      g = o > g ? o : g;
+      if ((threadIdx.x & 3) == 0) top.group[threadIdx.x >> 2] = g;
+      __syncthreads();
+      block_top<256>(top, a.top, [&](uint32_t bound, auto f) {
+        for (int i = threadIdx.x; i < n; i += 256)
+          if ((uint32_t)(t0[i] >> 32) >= bound) f(t0[i]);
+      }, [&](auto f) {
+        for (int i = threadIdx.x; i < n; i += 256) f(t0[i]);
+      }, [&](int t, unsigned long long key) { logp_place(a, row, t, key, whole); });
+    }
+    __syncthreads();
+  }
+}
+
+// Segments and blocks: a row by one block where there are rows for all CUs, otherwise as many segments as make 256 blocks, of 2048 columns at least.  Blocks of 256 threads, of which
+// several share a CU and wait at different times, until their registers are full.
 static LogpPlan logp_plan(const ftp_logp_args& a) {
   LogpPlan p{};
-  const int64_t most = (a.vocab + 2047) / 2048, want = a.rows > 0 ? (1024 + a.rows - 1) / a.rows : 1;
-  p.segs = (int)std::max<int64_t>(1, std::min(most, want));
+  const int most = a.dtype == FTP_BF16 ? 65536 : 32768;
+  const int64_t want = a.rows > 0 ? (256 + a.rows - 1) / a.rows : 1;
+  p.segs = (int)std::max<int64_t>((a.vocab + most - 1) / most, std::min<int64_t>((a.vocab + 2047) / 2048, want));
   p.seg = ((a.vocab + p.segs - 1) / p.segs + 7) / 8 * 8;
   p.segs = (a.vocab + p.seg - 1) / p.seg;
+  const int eights = p.seg / 8;
+  p.threads = eights <= 64 ? 64 : eights <= most / 16 ? 256 : 512;
+  p.vectors = 1;
+  while (p.threads * p.vectors < eights) p.vectors *= 2;
   return p;
+}
+template <typename E, int T, int NV>
+static void logp_go(hipStream_t st, const ftp_logp_args& a, const LogpPlan& p) {
+  const dim3 g((unsigned)std::min<int64_t>(a.rows * p.segs, 1 << 22));
+  if (a.top) hipLaunchKernelGGL((logp_k<E, T, NV, true>), g, dim3(T), 0, st, a, p);
+  else hipLaunchKernelGGL((logp_k<E, T, NV, false>), g, dim3(T), 0, st, a, p);
+}
+template <typename E>
+static void logp_by(hipStream_t st, const ftp_logp_args& a, const LogpPlan& p) {
+  constexpr int MOST = sizeof(E) == 2 ? 16 : 8;
+  if (p.threads == 64) logp_go<E, 64, 1>(st, a, p);
+  else if (p.threads == 512) logp_go<E, 512, MOST>(st, a, p);
+  else if (p.vectors == 1) logp_go<E, 256, 1>(st, a, p);
+  else if (p.vectors == 2) logp_go<E, 256, 2>(st, a, p);
+  else if (p.vectors == 4) logp_go<E, 256, 4>(st, a, p);
+  else if (p.vectors == 8) logp_go<E, 256, 8>(st, a, p);
+  else logp_go<E, 256, MOST>(st, a, p);
+  if (p.segs > 1) hipLaunchKernelGGL(logp_join_k<E>, dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)), dim3(256), 0, st, a, p);
 }
 static size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 size_t bt_logp_bytes(const ftp_logp_args& a) {
@@ -192,12 +389,8 @@ void bt_logp(hipStream_t st, const ftp_logp_args& a) {
   LogpPlan p = logp_plan(a);
   p.part = (float*)a.ws;
   p.tops = (unsigned long long*)((char*)a.ws + up256((size_t)a.rows * p.segs * 16));
-  const dim3 g((unsigned)std::min<int64_t>(a.rows * p.segs, 1 << 20)), j((unsigned)std::min<int64_t>(a.rows, 1 << 20));
-  if (a.dtype == FTP_BF16) hipLaunchKernelGGL(logp_k<bf16_t>, g, dim3(kLogpT), 0, st, a, p);
-  else hipLaunchKernelGGL(logp_k<float>, g, dim3(kLogpT), 0, st, a, p);
-  if (p.segs == 1) return;
-  if (a.dtype == FTP_BF16) hipLaunchKernelGGL(logp_join_k<bf16_t>, j, dim3(64), 0, st, a, p);
-  else hipLaunchKernelGGL(logp_join_k<float>, j, dim3(64), 0, st, a, p);
+  if (a.dtype == FTP_BF16) logp_by<bf16_t>(st, a, p);
+  else logp_by<float>(st, a, p);
 }
 
 // dlogits = scale * (dlogp ([v = id] - p) - dentropy p (log p + entropy))
