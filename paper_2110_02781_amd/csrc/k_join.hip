@@ -38,7 +38,7 @@ __device__ __forceinline__ void mask8(const DropMask& m, MaskKey k, uint64_t row
 __device__ __forceinline__ float dropped(float v, uint32_t keep) { return __uint_as_float(__float_as_uint(v) & keep); }
 
 // ---------------------------------------------------------------- dropout
-template <typename E>
+template <typename E, bool ONCE>
 __global__ __launch_bounds__(256) void dropout_k(DropMask m, int64_t t0, int rows, int cols, const E* x, int64_t ldx, const E* r, int64_t ldr, E* y, int64_t ldy) {
   const uint32_t per = (cols + 7) / 8, all = (uint32_t)rows * per;
   const MaskKey key = mask_key(m);
@@ -47,8 +47,8 @@ __global__ __launch_bounds__(256) void dropout_k(DropMask m, int64_t t0, int row
     const int64_t t = t0 + row;
     const int left = cols - (int)(j * 8);
     float v[8], o[8];
-    tk_load8<E>(x + t * ldx + j * 8, left, v);
-    if (r) tk_load8<E>(r + t * ldr + j * 8, left, o);
+    ONCE ? tk_load8_once<E>(x + t * ldx + j * 8, left, v) : tk_load8<E>(x + t * ldx + j * 8, left, v);
+    if (r) ONCE ? tk_load8_once<E>(r + t * ldr + j * 8, left, o) : tk_load8<E>(r + t * ldr + j * 8, left, o);
     if (m.least) {
       uint32_t k[8];
       mask8(m, key, (uint64_t)(m.row0 + t), j, k);
@@ -59,16 +59,21 @@ __global__ __launch_bounds__(256) void dropout_k(DropMask m, int64_t t0, int row
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] += o[e];
     }
-    tk_store8<E>(y + t * ldy + j * 8, left, v);
+    ONCE ? tk_store8_once<E>(y + t * ldy + j * 8, left, v) : tk_store8<E>(y + t * ldy + j * 8, left, v);
   }
 }
 void bt_dropout(hipStream_t st, int dt, int64_t rows, int cols, const DropMask& m, const void* x, int64_t ldx, const void* r, int64_t ldr, void* y, int64_t ldy) {
   KScope ks(st, "tok_dropout", (double)rows * cols * (dt == 1 ? 2 : 4) * (r ? 3 : 2), 2.0 * rows * cols, rows, cols);
   const int64_t per = (cols + 7) / 8;
+  const bool once = past_the_caches((double)rows * cols * (dt == 1 ? 2 : 4) * (r ? 3 : 2));
   by_rows(rows, per, [&](int64_t t0, int n) {
-    const dim3 b(blocks_of(n * per, 1 << 20));
-    if (dt == 1) hipLaunchKernelGGL(dropout_k<bf16_t>, b, dim3(256), 0, st, m, t0, n, cols, (const bf16_t*)x, ldx, (const bf16_t*)r, ldr, (bf16_t*)y, ldy);
-    else hipLaunchKernelGGL(dropout_k<float>, b, dim3(256), 0, st, m, t0, n, cols, (const float*)x, ldx, (const float*)r, ldr, (float*)y, ldy);
+    const dim3 b(blocks_of(n * per, 8192));
+    const auto go = [&](auto k, auto* e) {
+      typedef std::remove_pointer_t<decltype(e)> E;
+      hipLaunchKernelGGL(k, b, dim3(256), 0, st, m, t0, n, cols, (const E*)x, ldx, (const E*)r, ldr, (E*)y, ldy);
+    };
+    if (dt == 1) once ? go(dropout_k<bf16_t, true>, (bf16_t*)nullptr) : go(dropout_k<bf16_t, false>, (bf16_t*)nullptr);
+    else once ? go(dropout_k<float, true>, (float*)nullptr) : go(dropout_k<float, false>, (float*)nullptr);
   });
 }
 
@@ -252,7 +257,8 @@ __global__ __launch_bounds__(kJoinT) void join_wide_k(ftp_join_args a, DropMask 
   }
 }
 // Rows of up to kJoinHeld columns: a block of T threads has eight columns in each and everything it needs of a row in registers.  What a row costs beside its bytes are
-// the meetings of its wavefronts, one for each mean.  WHOLE: rows are a multiple of eight columns.
+// the meetings of its wavefronts, one for each mean.  ROWS: 1 where they are a
+// multiple of eight columns, 2 where besides the call's operands are more than the caches hold, and go past them.
 enum { JK_X = 1, JK_B = 2, JK_GATE = 4, JK_DY = 8, JK_DN = 16, JK_Y = 32, JK_N = 64, JK_DX = 128, JK_DB = 256, JK_DGATE = 512, JK_POST = 1024, JK_LAYER = 2048, JK_GATE_F32 = 4096, JK_GATE_ADD = 8192 };
 // what the kernels need of a call's record, in as few scalar registers as it goes into: row distances in bytes, questions as bits
 struct JoinK {
@@ -298,15 +304,20 @@ static JoinK join_k(const ftp_join_args& a, const DropMask& m, bool backward) {
 }
 
 template <typename E> struct Raw8 { u4v_t a[sizeof(E) / 2]; };
-template <typename E, bool WHOLE>
+template <typename E, bool WHOLE, bool ONCE = false>
 __device__ __forceinline__ Raw8<E> raw8_load(const char* row, int c, int left) {
   const E* const p = (const E*)row + (uint32_t)c;
   Raw8<E> r;
 #pragma unroll
   for (int i = 0; i < (int)sizeof(E) / 2; ++i) r.a[i] = u4v_t{0, 0, 0, 0};
   if (left >= 8) {
-    r.a[0] = tk_ld16<E>(p);
-    if constexpr (sizeof(E) == 4) r.a[1] = tk_ld16<E>(p + 4);
+    if (ONCE) {
+      r.a[0] = tk_ld16_once<E>(p);
+      if constexpr (sizeof(E) == 4) r.a[1] = tk_ld16_once<E>(p + 4);
+    } else {
+      r.a[0] = tk_ld16<E>(p);
+      if constexpr (sizeof(E) == 4) r.a[1] = tk_ld16<E>(p + 4);
+    }
   } else if (!WHOLE) {
 #pragma unroll
     for (int e = 0; e < 7; ++e) {
@@ -330,9 +341,11 @@ __device__ __forceinline__ void raw8_open(const Raw8<E>& r, float v[8]) {
     for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r.a[i / 4][i & 3]);
   }
 }
-template <typename E, bool WHOLE>
+template <typename E, bool WHOLE, bool ONCE = false>
 __device__ __forceinline__ void row_store8(char* row, int c, int left, const float v[8]) {
-  if (WHOLE ? left >= 8 : left > 0) tk_store8<E>((E*)row + (uint32_t)c, WHOLE ? 8 : left, v);
+  if (!(WHOLE ? left >= 8 : left > 0)) return;
+  if (ONCE) tk_store8_once<E>((E*)row + (uint32_t)c, WHOLE ? 8 : left, v);
+  else tk_store8<E>((E*)row + (uint32_t)c, WHOLE ? 8 : left, v);
 }
 // the operands of a row: x, b, the gate's row, backward dy and dn as well
 template <typename E, bool BWD>
@@ -372,11 +385,11 @@ __device__ __forceinline__ JoinWalk join_walk(const JoinK& k, int64_t row) {
   if (BWD) { w.dy = k.dy + row * k.lddy; w.dn = k.dn + row * k.lddn; }
   return w;
 }
-template <typename E, bool BWD, bool WHOLE>
+template <typename E, bool BWD, bool WHOLE, bool ONCE>
 __device__ __forceinline__ void join_ask(const JoinK& k, int flags, JoinWalk& w, int c, int left, JoinIn<E, BWD>& in) {
-  if (flags & JK_X) in.x = raw8_load<E, WHOLE>(w.x, c, left);
+  if (flags & JK_X) in.x = raw8_load<E, WHOLE, ONCE>(w.x, c, left);
   w.x += k.ldx;
-  if (flags & JK_B) in.b = raw8_load<E, WHOLE>(w.b, c, left);
+  if (flags & JK_B) in.b = raw8_load<E, WHOLE, ONCE>(w.b, c, left);
   w.b += k.ldb;
   if (flags & JK_GATE) {
     const bool wide = sizeof(E) == 4 || (flags & JK_GATE_F32);
@@ -406,9 +419,9 @@ __device__ __forceinline__ void join_ask(const JoinK& k, int flags, JoinWalk& w,
     }
   }
   if constexpr (BWD) {
-    if (flags & JK_DY) in.dy = raw8_load<E, WHOLE>(w.dy, c, left);
+    if (flags & JK_DY) in.dy = raw8_load<E, WHOLE, ONCE>(w.dy, c, left);
     w.dy += k.lddy;
-    if (flags & JK_DN) in.dn = raw8_load<E, WHOLE>(w.dn, c, left);
+    if (flags & JK_DN) in.dn = raw8_load<E, WHOLE, ONCE>(w.dn, c, left);
     w.dn += k.lddn;
   }
 }
@@ -462,8 +475,9 @@ __device__ __forceinline__ float join_deviation(const JoinK& k, int flags, float
   return 1.f / sqrtf(fmaf(block_sum<T>(q, s, turn), inv, k.eps));
 }
 
-template <typename E, int T, bool WHOLE>
+template <typename E, int T, int ROWS>
 __global__ __launch_bounds__(T) void join_row_k(JoinK k, DropMask m, int64_t per) {
+  constexpr bool WHOLE = ROWS > 0, ONCE = ROWS == 2;
   __shared__ float2 s[2][T / 64];
   const int c = threadIdx.x * 8, left = k.width - c;
   const float inv = 1.f / (float)k.width;
@@ -472,7 +486,7 @@ __global__ __launch_bounds__(T) void join_row_k(JoinK k, DropMask m, int64_t per
   int turn = 0, flags = k.flags;
   JoinWalk at = join_walk<false>(k, r0);
   JoinIn<E, false> in, next;
-  join_ask<E, false, WHOLE>(k, flags, at, c, left, in);
+  join_ask<E, false, WHOLE, ONCE>(k, flags, at, c, left, in);
   char *py = k.y + r0 * k.ldy, *pn = k.n + r0 * k.ldn;
   float pw[8], pb[8], qw[8], qb[8];
   join_weight<WHOLE>(k.pre_w, c, left, 1.f, pw);
@@ -482,7 +496,7 @@ __global__ __launch_bounds__(T) void join_row_k(JoinK k, DropMask m, int64_t per
   uint64_t number = (uint64_t)(m.row0 + r0);
   for (int row = (int)(r1 - r0); row > 0; --row, ++number) {
     flags = join_flags(k.flags);
-    if (row > 1) join_ask<E, false, WHOLE>(k, flags, at, c, left, next);
+    if (row > 1) join_ask<E, false, WHOLE, ONCE>(k, flags, at, c, left, next);
     float y[8];
     join_open<E>(flags & JK_X, in.x, y);
     if (flags & JK_B) {
@@ -503,13 +517,13 @@ __global__ __launch_bounds__(T) void join_row_k(JoinK k, DropMask m, int64_t per
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] = (WHOLE ? left > 0 : e < left) ? fmaf(g[e], v[e], y[e]) : 0.f;
     }
-    if (flags & JK_Y) row_store8<E, WHOLE>(py, c, left, y);
+    if (flags & JK_Y) row_store8<E, WHOLE, ONCE>(py, c, left, y);
     py += k.ldy;
     if (flags & JK_N) {
       const float r = join_deviation<T, WHOLE>(k, flags, inv, left, y, s, turn);
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] = fmaf(y[e] * r, pw[e], pb[e]);
-      row_store8<E, WHOLE>(pn, c, left, y);
+      row_store8<E, WHOLE, ONCE>(pn, c, left, y);
     }
     pn += k.ldn;
     in.take(next);
@@ -534,8 +548,9 @@ static void join_by_threads(int t, F f) {
 
 void bt_join(hipStream_t st, const ftp_join_args& a, const DropMask& m) {
   const double n = (double)a.rows * a.width;
-  KScope ks(st, "tok_join", n * (a.dtype == 1 ? 2 : 4) * ((a.x != nullptr) + (a.b != nullptr) + (a.y != nullptr) + (a.n != nullptr) + (a.gate && a.gate_rows == 1)), 15 * n,
-            a.rows, a.width);
+  const double bytes = n * (a.dtype == 1 ? 2 : 4) * ((a.x != nullptr) + (a.b != nullptr) + (a.y != nullptr) + (a.n != nullptr) + (a.gate && a.gate_rows == 1));
+  KScope ks(st, "tok_join", bytes, 15 * n, a.rows, a.width);
+  const bool once = past_the_caches(bytes);
   if (a.width <= kJoinHeld) {
     const int t = join_threads(a.width);
     const int64_t want = join_blocks(a.rows, t), per = (a.rows + want - 1) / want;
@@ -544,8 +559,12 @@ void bt_join(hipStream_t st, const ftp_join_args& a, const DropMask& m) {
       constexpr int T = decltype(tc)::value;
       const JoinK k = join_k(a, m, false);
       const auto go = [&](auto f) { hipLaunchKernelGGL(f, g, b, 0, st, k, m, per); };
-      if (a.dtype == FTP_BF16) a.width % 8 ? go(join_row_k<bf16_t, T, false>) : go(join_row_k<bf16_t, T, true>);
-      else a.width % 8 ? go(join_row_k<float, T, false>) : go(join_row_k<float, T, true>);
+      const auto by = [&](auto* e) {
+        typedef std::remove_pointer_t<decltype(e)> E;
+        a.width % 8 ? go(join_row_k<E, T, 0>) : once ? go(join_row_k<E, T, 2>) : go(join_row_k<E, T, 1>);
+      };
+      if (a.dtype == FTP_BF16) by((bf16_t*)nullptr);
+      else by((float*)nullptr);
     });
     return;
   }
@@ -779,8 +798,9 @@ struct JoinSums {
   }
 };
 // BIAS: sums of the biases as well, and a bias behind the block
-template <typename E, int T, bool BIAS, bool WHOLE, bool LDS, bool AHEAD, bool HOLD>
+template <typename E, int T, bool BIAS, int ROWS, bool LDS, bool AHEAD, bool HOLD>
 __global__ __launch_bounds__(T, T == 512 && sizeof(E) == 2 ? 4 : 1) void join_row_bwd_k(JoinK k, DropMask m, JoinRanges gr, float* parts, int64_t part_size, int wanted) {
+  constexpr bool WHOLE = ROWS > 0, ONCE = ROWS == 2;
   __shared__ float2 s[2][T / 64];
   extern __shared__ float4 held[];
   const int c = threadIdx.x * 8, left = k.width - c;
@@ -794,7 +814,7 @@ __global__ __launch_bounds__(T, T == 512 && sizeof(E) == 2 ? 4 : 1) void join_ro
   if (r0 < r1) {
     JoinWalk at = join_walk<true>(k, r0);
     JoinIn<E, true> in, next;
-    join_ask<E, true, WHOLE>(k, flags, at, c, left, in);
+    join_ask<E, true, WHOLE, ONCE>(k, flags, at, c, left, in);
     const int64_t group = want >> JP_GATE & 1 ? r0 / gr.group : r0;               // dgate's row
     char *pdx = k.dx + r0 * k.lddx, *pdb = k.db + r0 * k.lddb, *pdg = k.dgate + group * k.lddg;
     const int64_t rest = want >> JP_GATE & 1 ? (group + 1) * gr.group - r0 : 1;
@@ -809,7 +829,7 @@ __global__ __launch_bounds__(T, T == 512 && sizeof(E) == 2 ? 4 : 1) void join_ro
     for (int row = (int)(r1 - r0); row > 0; --row, ++number) {
       flags = join_flags(k.flags);
       want = join_flags(wanted);
-      if (AHEAD && row > 1) join_ask<E, true, WHOLE>(k, flags, at, c, left, next);
+      if (AHEAD && row > 1) join_ask<E, true, WHOLE, ONCE>(k, flags, at, c, left, next);
       float dY[8], bh[8], cc[8], g[8];                   // g: scale * gate; cc: what it multiplies, dropped
       uint32_t keep[8];
       float rb = 1.f;
@@ -865,7 +885,7 @@ __global__ __launch_bounds__(T, T == 512 && sizeof(E) == 2 ? 4 : 1) void join_ro
 #pragma unroll
         for (int e = 0; e < 8; ++e) dY[e] += ry * (dn[e] - fmaf(y[e], s2, s1));
       }
-      if (flags & JK_DX) row_store8<E, WHOLE>(pdx, c, left, dY);
+      if (flags & JK_DX) row_store8<E, WHOLE, ONCE>(pdx, c, left, dY);
       pdx += k.lddx;
       if (flags & JK_B) {
         if (flags & JK_DGATE) {
@@ -909,11 +929,11 @@ __global__ __launch_bounds__(T, T == 512 && sizeof(E) == 2 ? 4 : 1) void join_ro
             for (int e = 0; e < 8; ++e) dY[e] = rb * (dY[e] - fmaf(bh[e], t2, t1));
           }
         }
-        if (flags & JK_DB) row_store8<E, WHOLE>(pdb, c, left, dY);
+        if (flags & JK_DB) row_store8<E, WHOLE, ONCE>(pdb, c, left, dY);
       }
       pdb += k.lddb;
       if (AHEAD) in.take(next);
-      else if (row > 1) join_ask<E, true, WHOLE>(k, flags, at, c, left, in);
+      else if (row > 1) join_ask<E, true, WHOLE, ONCE>(k, flags, at, c, left, in);
     }
   }
   if (left <= 0) return;
@@ -988,8 +1008,10 @@ void bt_join_bwd(hipStream_t st, const ftp_join_args& a, const DropMask& m) {
     return;
   }
   const double n = (double)a.rows * a.width;
-  KScope ks(st, "tok_join_bwd", n * (a.dtype == 1 ? 2 : 4) * ((a.x != nullptr) + (a.b != nullptr) + (a.dy != nullptr) + (a.dn != nullptr) + (a.dx != nullptr) + (a.db != nullptr) +
-            (a.gate && a.gate_rows == 1 ? 1 + (a.dgate != nullptr) : 0)), 50 * n, a.rows, a.width);
+  const double bytes = n * (a.dtype == 1 ? 2 : 4) * ((a.x != nullptr) + (a.b != nullptr) + (a.dy != nullptr) + (a.dn != nullptr) + (a.dx != nullptr) + (a.db != nullptr) +
+                       (a.gate && a.gate_rows == 1 ? 1 + (a.dgate != nullptr) : 0));
+  KScope ks(st, "tok_join_bwd", bytes, 50 * n, a.rows, a.width);
+  const bool once = past_the_caches(bytes);
   const JoinRanges r = join_ranges(a);
   bool wanted[JP_ALL];
   join_wanted(a, r, wanted);
@@ -1017,8 +1039,9 @@ void bt_join_bwd(hipStream_t st, const ftp_join_args& a, const DropMask& m) {
       const auto go = [&](auto f) { hipLaunchKernelGGL(f, dim3(r.blocks), dim3(T), L ? (size_t)sums * T * 32 : 0, st, k, m, r, (float*)a.ws, (int64_t)(join_part_bytes(a, r) / 4), want); };
       const auto by = [&](auto* e) {
         typedef std::remove_pointer_t<decltype(e)> E;
-        if (a.width % 8) bias ? go(join_row_bwd_k<E, T, true, false, L, !L, !L>) : go(join_row_bwd_k<E, T, false, false, L, !L, !L>);
-        else bias ? go(join_row_bwd_k<E, T, true, true, L, !L, !L>) : go(join_row_bwd_k<E, T, false, true, L, !L, !L>);
+        if (a.width % 8) bias ? go(join_row_bwd_k<E, T, true, 0, L, !L, !L>) : go(join_row_bwd_k<E, T, false, 0, L, !L, !L>);
+        else if (once) bias ? go(join_row_bwd_k<E, T, true, 2, L, !L, !L>) : go(join_row_bwd_k<E, T, false, 2, L, !L, !L>);
+        else bias ? go(join_row_bwd_k<E, T, true, 1, L, !L, !L>) : go(join_row_bwd_k<E, T, false, 1, L, !L, !L>);
       };
       if (a.dtype == FTP_BF16) by((bf16_t*)nullptr);
       else by((float*)nullptr);

@@ -79,6 +79,8 @@ static inline void by_rows(int64_t rows, int64_t per_row, F f) {
   const int64_t step = std::max<int64_t>(1, ((int64_t)1 << 30) / std::max<int64_t>(per_row, 1));
   for (int64_t r = 0; r < rows; r += step) f(r, (int)std::min(step, rows - r));
 }
+// whether what a call moves is more than the card's last cache (256 MB) holds: then nothing of it is there when it is next asked for
+static inline bool past_the_caches(double bytes) { return bytes > 256e6; }
 static inline unsigned blocks_of(int64_t n, int most) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>((n + 255) / 256, most)); }
 
 }  // namespace ftp
