@@ -32,7 +32,7 @@ class Weight:
 
 
 class Model:
-    def __init__(self, vocab=96, width=128, hidden=256, drop=0.1, dtype="bf16", seed=1):
+    def __init__(self, vocab=24, width=128, hidden=256, drop=0.05, dtype="bf16", seed=1):
         gen = torch.Generator(device="cuda").manual_seed(seed)
         self.vocab, self.width, self.hidden, self.drop = vocab, width, hidden, drop
         self.dtype, self.code = TYPES[dtype]
@@ -152,7 +152,7 @@ def batch(gen, vocab, starts):
     return ids, targets
 
 
-def train(steps=200, seqs=96, longest=12, lr=0.3, verbose=True):
+def train(steps=400, seqs=256, longest=8, lr=0.5, verbose=True):
     """-> (model, the losses)"""
     m = Model()
     gen = torch.Generator(device="cuda").manual_seed(2)
@@ -171,9 +171,9 @@ def train(steps=200, seqs=96, longest=12, lr=0.3, verbose=True):
         r.forward(stream)
         r.backward(stream)
         for w in m.w.values():
-            w.update(lr)
+            w.update(lr * (1 - step / steps))
         losses.append(-float(r.logp.sum()) / seqs)
-        if verbose and step % 20 == 0:
+        if verbose and step % 50 == 0:
             print(f"step {step}: loss {losses[-1]:.4f}", flush=True)
     return m, losses
 
@@ -192,7 +192,7 @@ def ask(m, prompts, top=3):
 
 if __name__ == "__main__":
     model, losses = train()
-    prompts = torch.randint(0, model.vocab, (16, 8), device="cuda", dtype=torch.int32)
+    prompts = torch.randint(0, model.vocab, (64, 6), device="cuda", dtype=torch.int32)
     ids, logp = ask(model, prompts)
     right = int((ids[:, 0] == prompts[:, 0]).sum())
     print(f"loss {losses[0]:.3f} -> {losses[-1]:.4f}; {right} of {len(prompts)} requests remembered, the likeliest with probability {float(logp[:, 0].exp().mean()):.3f}")

@@ -433,7 +433,7 @@ int ftp_act8_unpack(const ftp_act8_args*, void* stream);
 
 /* What stands between the products: dropout, the join of a block's output with the stream and the norms around it, a gated linear
  * recurrence along the sequences, log probabilities of tokens.  Rows, types, strides, workspaces and results as above; no stride
- * has to be aligned and nothing is copied.  `seed`, `seed_dev`, `site`, `row0`, `p` name a mask wherever there is one. */
+ * has to be aligned and nothing is copied.  Where a result may lie in an operand's buffer it has that operand's row distance.  `seed`, `seed_dev`, `site`, `row0`, `p` name a mask wherever there is one. */
 
 /* A mask of dropout is never stored: it is made again wherever it is needed, by the counter-based generator Philox4x32-10 (Salmon,
  * Moraes, Dror, Shaw: Parallel random numbers: as easy as 1, 2, 3; 2011).  Columns 8 j .. 8 j + 7 of a row have the counter (j, site,

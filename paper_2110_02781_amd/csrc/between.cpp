@@ -19,6 +19,11 @@ int check_space(const char* who, const void* ws, size_t have, size_t need) {
   NEED(need == 0 || (uintptr_t)ws % 16 == 0, FTP_ERR_ARG, "%s: the workspace must start on 16 bytes", who);
   return FTP_OK;
 }
+// a result in an operand's buffer: element for element
+int check_same(const char* who, const char* out, const void* o, int64_t ldo, const char* in, const void* i, int64_t ldi) {
+  NEED(!o || o != i || ldo == ldi, FTP_ERR_ARG, "%s: %s in the buffer of %s has to have its row distance", who, out, in);
+  return FTP_OK;
+}
 template <typename A>
 int check_mask(const char* who, const A* a) {
   NEED(std::isfinite(a->p) && a->p >= 0.f && drop_least(a->p) < 65536, FTP_ERR_VALUE, "%s: p must be in [0, 1), with some of 2^-16 left", who);
@@ -41,9 +46,12 @@ int check_dropout(const char* who, const ftp_dropout_args* a, bool backward) {
     TRY(check_mat(who, "x", a->x, a->ldx, a->rows, a->cols, a->dtype));
     TRY(check_mat(who, "residual", a->residual, a->ldr, a->rows, a->cols, a->dtype, true));
     TRY(check_mat(who, "y", a->y, a->ldy, a->rows, a->cols, a->dtype));
+    TRY(check_same(who, "y", a->y, a->ldy, "x", a->x, a->ldx));
+    TRY(check_same(who, "y", a->y, a->ldy, "residual", a->residual, a->ldr));
   } else {
     TRY(check_mat(who, "dy", a->dy, a->lddy, a->rows, a->cols, a->dtype));
     TRY(check_mat(who, "dx", a->dx, a->lddx, a->rows, a->cols, a->dtype));
+    TRY(check_same(who, "dx", a->dx, a->lddx, "dy", a->dy, a->lddy));
   }
   return FTP_OK;
 }
@@ -72,6 +80,8 @@ int check_join(const char* who, const ftp_join_args* a, bool backward) {
     NEED(a->rows == 0 || a->y || a->n, FTP_ERR_ARG, "%s: neither y nor n is wanted", who);
     TRY(check_mat(who, "y", a->y, a->ldy, a->rows, a->width, a->dtype, true));
     TRY(check_mat(who, "n", a->n, a->ldn, a->rows, a->width, a->dtype, true));
+    TRY(check_same(who, "y", a->y, a->ldy, "x", a->x, a->ldx));
+    TRY(check_same(who, "y", a->y, a->ldy, "b", a->b, a->ldb));
     return FTP_OK;
   }
   NEED(a->dx || a->db || a->dgate || a->dpost_w || a->dpost_bias || a->dpre_w || a->dpre_bias, FTP_ERR_ARG, "%s: no gradient is asked for", who);
@@ -80,6 +90,7 @@ int check_join(const char* who, const ftp_join_args* a, bool backward) {
   TRY(check_mat(who, "dn", a->dn, a->lddn, a->rows, a->width, a->dtype, true));
   TRY(check_mat(who, "dx", a->dx, a->lddx, a->rows, a->width, a->dtype, true));
   TRY(check_mat(who, "db", a->db, a->lddb, a->rows, a->width, a->dtype, true));
+  TRY(check_same(who, "dx", a->dx, a->lddx, "dy", a->dy, a->lddy));
   NEED(a->rows == 0 || a->b || !(a->db || a->dgate || a->dpost_w || a->dpost_bias), FTP_ERR_ARG, "%s: a gradient of the block's side without b", who);
   NEED(a->post || !(a->dpost_w || a->dpost_bias), FTP_ERR_ARG, "%s: gradients of the weights behind the block without post", who);
   NEED(a->rows == 0 || a->dn || !(a->dpre_w || a->dpre_bias), FTP_ERR_ARG, "%s: dpre_w and dpre_bias need dn", who);
@@ -114,7 +125,7 @@ int check_scan(const char* who, const ftp_scan_args* a, bool backward) {
     NEED(a->rows == 0 || a->y || a->h_end, FTP_ERR_ARG, "%s: neither y nor h_end is wanted", who);
     TRY(check_mat(who, "y", a->y, a->ldy, a->rows, a->width, a->dtype, true));
     TRY(check_mat(who, "h_end", a->h_end, a->ldhe, a->seqs, a->width, FTP_F32, true));
-    NEED(!a->h_end || a->h_end != a->h0 || a->ldhe == a->ldh0, FTP_ERR_ARG, "%s: h_end in h0's buffer has to have its row distance", who);
+    TRY(check_same(who, "h_end", a->h_end, a->ldhe, "h0", a->h0, a->ldh0));
     return FTP_OK;
   }
   NEED(a->df || a->dx || a->dg || a->dh0, FTP_ERR_ARG, "%s: no gradient is asked for", who);
@@ -125,7 +136,7 @@ int check_scan(const char* who, const ftp_scan_args* a, bool backward) {
   TRY(check_mat(who, "dx", a->dx, a->lddx, a->rows, a->width, a->dtype, true));
   TRY(check_mat(who, "dg", a->dg, a->lddg, a->rows, a->width, a->dtype, true));
   TRY(check_mat(who, "dh0", a->dh0, a->lddh0, a->seqs, a->width, FTP_F32, true));
-  NEED(!a->dh0 || a->dh0 != a->dh_end || a->lddh0 == a->lddhe, FTP_ERR_ARG, "%s: dh0 in dh_end's buffer has to have its row distance", who);
+  TRY(check_same(who, "dh0", a->dh0, a->lddh0, "dh_end", a->dh_end, a->lddhe));
   return FTP_OK;
 }
 
@@ -156,6 +167,7 @@ int check_logp(const char* who, const ftp_logp_args* a, bool backward) {
   TRY(check_floats(who, "dlogp", a->dlogp));
   TRY(check_floats(who, "dentropy", a->dentropy));
   TRY(check_mat(who, "dlogits", a->dlogits, a->lddl, a->rows, a->vocab, a->dtype));
+  TRY(check_same(who, "dlogits", a->dlogits, a->lddl, "logits", a->logits, a->ldl));
   return FTP_OK;
 }
 

@@ -198,3 +198,15 @@ def test_the_generator_against_its_authors_vectors():
                                ((0xffffffff,) * 4, (0xffffffff,) * 2, (0x408f276d, 0x41c83b0e, 0xa20bc7c6, 0x6d5451fd)),
                                ((0x243f6a88, 0x85a308d3, 0x13198a2e, 0x03707344), (0xa4093822, 0x299f31d0), (0xd16cfe09, 0x94fdcceb, 0x5001e420, 0x24126ea1))):
         assert tuple(R.philox(counter, key)) == want
+
+
+def test_results_in_an_operands_buffer_have_its_rows(P):
+    B = 3 << 20
+    for kw in (dict(y=B, x=B, ldy=11), dict(y=B, residual=B, ldy=11), dict(y=B, x=B, ldx=12)):
+        refused(P, P.dropout_forward, dropout(P, **kw))
+    refused(P, P.dropout_backward, dropout(P, dx=B, dy=B, lddx=11))
+    for kw in (dict(y=B, x=B, ldy=17), dict(y=B, b=B, ldb=18)):
+        refused(P, P.join_forward, join(P, **kw))
+    refused(P, P.join_backward, join(P, dx=B, dy=B, lddy=17))
+    refused(P, P.scan_backward, scan(P, dh0=B, dh_end=B, lddhe=17))
+    refused(P, P.logp_backward, logp(P, dlogits=B, logits=B, lddl=11))

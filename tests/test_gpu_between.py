@@ -198,6 +198,14 @@ def test_join_many_rows(env, gate, gate_rows):
     join_case(env, "bf16", 5003, 96, True, True, gate, gate_rows, p=0.1, gate_f32=gate_rows == 700)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("width", [4104, 6001, 8192])
+@pytest.mark.parametrize("layer,gate,weights", [(True, "row", True), (False, "none", False), (True, "all", True), (False, "group", False)])
+def test_join_of_the_longest_rows_that_are_held(env, dtype, width, layer, gate, weights):
+    """column sums in LDS, up to four of them; five go another way"""
+    join_case(env, dtype, 37, width, layer, True, gate, 5, p=0.1, weights=weights, gate_f32=gate == "all")
+
+
 def test_join_in_place_and_twice(env):
     torch, P, _ = env
     for width in (200, 40000):
@@ -456,6 +464,16 @@ def test_logp_masks_and_ties(env, dtype, rows, vocab):
     ids[:6] = torch.tensor([0, vocab // 2, vocab - 1, -1, 0, vocab])
     logp_case(env, dtype, rows, vocab, 20, logits=z, ids=ids.cuda())
     logp_case(env, dtype, rows, vocab, 3, logits=z, ids=(ids - 5).cuda(), pad_id=-6, scale=0.5, ids64=True)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_logp_ties_in_many_segments(env, dtype):
+    """one value everywhere, and few of them: more candidates than a block keeps, within segments and where they are joined"""
+    torch = env[0]
+    for vocab in (131072, 50001):
+        z = torch.zeros(2, vocab, device="cuda")
+        z[1] = (torch.arange(vocab, device="cuda") % 3).float()
+        logp_case(env, dtype, 2, vocab, 64, logits=z)
 
 
 @pytest.mark.parametrize("rows,vocab", [(5, 90), (5, 6000), (1200, 700)])
