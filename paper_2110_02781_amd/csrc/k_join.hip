@@ -965,7 +965,7 @@ __global__ __launch_bounds__(1024) void join_sum_k(JoinParts parts, JoinRanges g
     const int n = gate ? g.parts : g.blocks;
     float v = 0.f;
     if (c < N) {
-#pragma unroll 8
+#pragma unroll 16
       for (int i = ty; i < n; i += 32) v += p[(int64_t)i * N + c];
     }
     __syncthreads();

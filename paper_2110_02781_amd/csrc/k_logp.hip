@@ -98,7 +98,7 @@ __device__ __forceinline__ uint32_t logp_order(float v) {        // larger value
 }
 
 // The k largest keys of a block, in their order, at put(place, key).  s.group holds the largest of each of 64 groups of T / 64 lanes beside one another (a barrier has passed).  Of these the
-// k-th is a bound that at least k keys reach (fewer groups than k with a key: any); those that do, some more than k as a rule, are shown by some(bound, f) and kept in LDS, where each
+// k-th, without its last sixteen bits, is a bound that at least k keys reach (fewer groups than k with a key: any); those that do, some more than k as a rule, are shown by some(bound, f) and kept in LDS, where each
 // counts the larger ones.  Too many that are alike: one after another, each the largest below the last of those that all(f) shows.
 struct LogpTop {
   uint32_t group[64];
@@ -112,7 +112,7 @@ __device__ __forceinline__ void block_top(LogpTop& s, int k, S some, A all, P pu
     const uint32_t g = s.group[threadIdx.x];
     uint32_t b = 0;
 #pragma unroll 1
-    for (int bit = 30; bit >= 0; bit -= 2) {                     // two bits at a time: three counts that do not wait for one another
+    for (int bit = 30; bit >= 16; bit -= 2) {                    // two bits at a time: three counts that do not wait for one another
       const uint32_t c1 = b | 1u << bit, c2 = b | 2u << bit, c3 = b | 3u << bit;
       const int n1 = __popcll(__ballot(g >= c1)), n2 = __popcll(__ballot(g >= c2)), n3 = __popcll(__ballot(g >= c3));
       b = n3 >= k ? c3 : n2 >= k ? c2 : n1 >= k ? c1 : b;

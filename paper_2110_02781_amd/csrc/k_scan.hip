@@ -271,26 +271,60 @@ __global__ __launch_bounds__(1024) void scan_follow_k(ScanArgs k) {
   float* const out = rev ? k.back : k.state;
   const int share = (k.chunks + 31) / 32, i0 = ty * share, i1 = i0 + share < k.chunks ? i0 + share : k.chunks;
   const auto at = [&](int i) { return (int64_t)(rev ? k.chunks - 1 - i : i) * W + c; };
-  float a = 1.f, b = 0.f;
+  float a = 1.f, b = 0.f, u[8], v[8];
+  const bool few = share <= 8;           // kept for the second time
   if (c < W) {
+    if (few) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const bool in = i0 + q < i1;
+        u[q] = in ? A[at(in ? i0 + q : 0)] : 1.f;
+        v[q] = in ? B[at(in ? i0 + q : 0)] : 0.f;
+      }
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        b = fmaf(u[q], b, v[q]);
+        a *= u[q];
+      }
+    } else {
 #pragma unroll 8
-    for (int i = i0; i < i1; ++i) {
-      const float u = A[at(i)], v = B[at(i)];
-      b = fmaf(u, b, v);
-      a *= u;
+      for (int i = i0; i < i1; ++i) {
+        const float p = A[at(i)], q = B[at(i)];
+        b = fmaf(p, b, q);
+        a *= p;
+      }
     }
   }
-  sa[ty][lane] = a;
+  // each share's product and sum with those of the 1, 2, 4, ... shares in front
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    sa[ty][lane] = a;
+    sb[ty][lane] = b;
+    __syncthreads();
+    if (ty >= d) {
+      b = fmaf(a, sb[ty - d][lane], b);
+      a *= sa[ty - d][lane];
+    }
+    __syncthreads();
+  }
   sb[ty][lane] = b;
   __syncthreads();
   if (c >= W) return;
-  float h = 0.f;
-  for (int j = 0; j < ty; ++j) h = fmaf(sa[j][lane], h, sb[j][lane]);
+  float h = ty ? sb[ty - 1][lane] : 0.f;
+  if (few) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      if (i0 + q >= i1) break;
+      out[at(i0 + q)] = h;
+      h = fmaf(u[q], h, v[q]);
+    }
+  } else {
 #pragma unroll 8
-  for (int i = i0; i < i1; ++i) {
-    const float u = A[at(i)], v = B[at(i)];
-    out[at(i)] = h;
-    h = fmaf(u, h, v);
+    for (int i = i0; i < i1; ++i) {
+      const float p = A[at(i)], q = B[at(i)];
+      out[at(i)] = h;
+      h = fmaf(p, h, q);
+    }
   }
 }
 
