@@ -218,7 +218,17 @@ __global__ __launch_bounds__(T, 1) void logp_k(ftp_logp_args a, LogpPlan p) {
     for (int v = 0; v < NV; ++v)
 #pragma unroll
       for (int e = 0; e < 8; ++e) m = fmaxf(m, logp_at<E>(r[v], e));
-    if constexpr (TOP) {
+    if constexpr (TOP && NV == 1) {
+      // A short segment: columns are dealt to the groups one by one, so that no group is empty while another has two (by lanes, 1240 columns with 50 wanted would fill 39 groups, and
+      // every logit be a candidate: 5 x 2478 took 73 us)
+      if (threadIdx.x < 64) top.group[threadIdx.x] = 0;
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float v = logp_at<E>(r[0], e);
+        if (v > FTP_LEAST) atomicMax(&top.group[(threadIdx.x * 8 + e) & 63], logp_order(v));
+      }
+    } else if constexpr (TOP) {
       // the groups' largest (nothing above the least: no key, 0)
       float g = m;
       if (T > 64) g = fmaxf(g, dpp_move<0xB1>(g));
@@ -357,7 +367,8 @@ __global__ __launch_bounds__(256) void logp_join_k(ftp_logp_args a, LogpPlan p) 
 // several share a CU and wait at different times, until their registers are full.
 static LogpPlan logp_plan(const ftp_logp_args& a) {
   LogpPlan p{};
-  const int most = a.dtype == FTP_BF16 ? 65536 : 32768;
+  // with the likeliest, half as many columns a thread: twice would leave two wavefronts to a SIMD (2048 x 32000 bfloat16 with 5 alternatives 50 us, so 44)
+  const int most = (a.dtype == FTP_BF16 ? 65536 : 32768) / (a.top ? 2 : 1);
   const int64_t want = a.rows > 0 ? (256 + a.rows - 1) / a.rows : 1;
   p.segs = (int)std::max<int64_t>((a.vocab + most - 1) / most, std::min<int64_t>((a.vocab + 2047) / 2048, want));
   p.seg = ((a.vocab + p.segs - 1) / p.segs + 7) / 8 * 8;
@@ -366,8 +377,6 @@ static LogpPlan logp_plan(const ftp_logp_args& a) {
   p.threads = eights <= 64 ? 64 : eights <= most / 16 ? 256 : 512;
   p.vectors = 1;
   while (p.threads * p.vectors < eights) p.vectors *= 2;
-  // with the likeliest, sixteen eights leave two wavefronts to a SIMD (2048 x 32000 with 5 alternatives 50 us, eight a thread 44)
-  if (a.top && a.dtype == FTP_BF16 && p.threads == 256 && p.vectors == 16) p = LogpPlan{p.segs, p.seg, 512, 8, nullptr, nullptr};
   return p;
 }
 template <typename E, int T, int NV>
@@ -376,20 +385,24 @@ static void logp_go(hipStream_t st, const ftp_logp_args& a, const LogpPlan& p) {
   // kept for a backward, what the caches hold of the logits is read again (8192 x 32000 bfloat16, forward and backward: 285 us, past them 303; forward alone 113 and 91)
   const bool once = !a.stats && past_the_caches((double)a.rows * a.vocab * sizeof(E));
   const auto go = [&](auto k) { hipLaunchKernelGGL(k, g, dim3(T), 0, st, a, p); };
-  if (a.top) once ? go(logp_k<E, T, NV, true, true>) : go(logp_k<E, T, NV, true, false>);
-  else once ? go(logp_k<E, T, NV, false, true>) : go(logp_k<E, T, NV, false, false>);
+  constexpr int HELD = NV * (int)sizeof(E) / 2;                  // a quarter of a thread's registers for its columns: 16 at most, 8 with the likeliest
+  if (a.top) {
+    if constexpr (T == 512 ? HELD == 8 : HELD <= 8) once ? go(logp_k<E, T, NV, true, true>) : go(logp_k<E, T, NV, true, false>);
+  } else {
+    if constexpr (T == 512 ? HELD == 16 : HELD <= 16) once ? go(logp_k<E, T, NV, false, true>) : go(logp_k<E, T, NV, false, false>);
+  }
 }
 template <typename E>
 static void logp_by(hipStream_t st, const ftp_logp_args& a, const LogpPlan& p) {
-  constexpr int MOST = sizeof(E) == 2 ? 16 : 8;
   if (p.threads == 64) logp_go<E, 64, 1>(st, a, p);
-  else if (p.threads == 512 && p.vectors == 8) logp_go<E, 512, 8>(st, a, p);
-  else if (p.threads == 512) logp_go<E, 512, MOST>(st, a, p);
-  else if (p.vectors == 1) logp_go<E, 256, 1>(st, a, p);
-  else if (p.vectors == 2) logp_go<E, 256, 2>(st, a, p);
-  else if (p.vectors == 4) logp_go<E, 256, 4>(st, a, p);
-  else if (p.vectors == 8) logp_go<E, 256, 8>(st, a, p);
-  else logp_go<E, 256, MOST>(st, a, p);
+  else if (p.threads == 256 && p.vectors == 1) logp_go<E, 256, 1>(st, a, p);
+  else if (p.threads == 256 && p.vectors == 2) logp_go<E, 256, 2>(st, a, p);
+  else if (p.threads == 256 && p.vectors == 4) logp_go<E, 256, 4>(st, a, p);
+  else if (p.threads == 256 && p.vectors == 8) logp_go<E, 256, 8>(st, a, p);
+  else if (p.threads == 256) logp_go<E, 256, 16>(st, a, p);
+  else if (p.vectors == 4) logp_go<E, 512, 4>(st, a, p);
+  else if (p.vectors == 8) logp_go<E, 512, 8>(st, a, p);
+  else logp_go<E, 512, 16>(st, a, p);
   if (p.segs > 1) hipLaunchKernelGGL(logp_join_k<E>, dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)), dim3(256), 0, st, a, p);
 }
 static size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }

@@ -547,14 +547,20 @@ __global__ __launch_bounds__(256) void scan_back_k(ScanArgs k) {
   }
 }
 
-// rows of a chunk: as few as fill the card with wavefronts (a chunk is walked row by row: 1500 x 333 fp32, forward and backward, 32 rows 51 us); where whole sequences fit
-// into one, no more than they have
-static int scan_per(const ftp_scan_args& a, int V, bool& whole) {
-  const int64_t groups = (a.width + 64 * V - 1) / (64 * V);
+// Rows of a chunk.  Where whole sequences fit into one, no more than they have.  Otherwise by what the launches cost in steps of a row: rounds of wavefronts (eight to a SIMD forward, four
+// backward) of a chunk's rows and six steps' worth of beginning, and a step for each 64 chunks that the states are followed through (1500 x 333 fp32, forward and backward: chunks of 8
+// 32 us, of 32 51).
+static int scan_per(const ftp_scan_args& a, int V, bool backward, bool& whole) {
+  const int64_t groups = (a.width + 64 * V - 1) / (64 * V), slots = backward ? 4096 : 8192;
   whole = a.starts ? a.rows <= kScanT : a.length <= kScanT;
   if (!a.starts && a.length > 0 && whole) return (int)(std::max<int64_t>(1, std::min<int64_t>(kScanT / a.length, a.seqs * groups / 4096)) * a.length);
+  if (whole) return kScanT;
   int per = kScanT;
-  while (!whole && per > 8 && (a.rows + per - 1) / per * groups < 4096) per /= 2;
+  int64_t least = INT64_MAX;
+  for (int p = kScanT; p >= 8; p -= kScanR) {
+    const int64_t chunks = (a.rows + p - 1) / p, cost = (chunks * groups + slots - 1) / slots * (p + 6) * 64 + chunks;
+    if (cost < least) { least = cost; per = p; }
+  }
   return per;
 }
 static int scan_columns(const ftp_scan_args& a) { return a.dtype == FTP_BF16 ? 2 : 1; }
@@ -583,7 +589,7 @@ static ScanArgs scan_plan(const ftp_scan_args& a, bool backward, size_t& bytes) 
   k.rows = a.rows; k.length = a.length; k.starts = a.starts;
   k.width = a.width; k.seqs = a.seqs; k.act = a.act;
   bool whole;
-  k.per = scan_per(a, scan_columns(a), whole);
+  k.per = scan_per(a, scan_columns(a), backward, whole);
   k.flags |= whole ? SK_WHOLE : 0;
   k.chunks = (int)((a.rows + k.per - 1) / k.per);
   bytes = 0;
