@@ -105,16 +105,42 @@ __device__ __forceinline__ ScanRows scan_rows(const ScanArgs& k, int64_t r0, int
     first = m == 0;
     last = m == len - 1;
   } else {
-    int lo = 0, hi = k.seqs;             // the last sequence that begins at r or in front (of several, all but one are empty)
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (k.starts[mid] <= r) lo = mid;
-      else hi = mid - 1;
+    // how many starts are at r0 or in front, 64 places at a time (by halves, each lane its row's, it is a load behind another for each halving)
+    const int all = k.seqs + 1, row0 = (int)r0;
+    int from = 0, span = all;            // the first start behind r0 is in from .. from + span
+    while (span > 0) {
+      const int step = (span + 63) >> 6, i = from + lane * step;
+      const int ahead = (int)__popcll(__ballot(i < from + span && k.starts[i < all ? i : 0] <= row0));       // of the places looked at, those not behind r0
+      if (ahead == 0) break;
+      const int to = from + (ahead - 1) * step + 1;              // one behind the last of them
+      span = step == 1 ? 0 : (to - 1 + step < from + span ? to - 1 + step : from + span) - to;
+      from = to;
     }
-    s.seq = lo < k.seqs ? lo : k.seqs - 1;
-    in = in && lo < k.seqs && k.starts[lo] <= r;
-    first = in && k.starts[s.seq] == r;
-    last = in && k.starts[s.seq + 1] == r + 1;
+    // the starts behind r0, one a lane; of a row's, those at it or in front count
+    const int next = from + lane < all ? k.starts[from + lane] : 0x7fffffff, in_front = from > 0 ? k.starts[from - 1] : -1;
+    if (__ballot(next > row0 + 63) || from + 64 >= all) {
+      int c = 0;
+      for (int t = 0; t < n; ++t) {
+        const int m = (int)__popcll(__ballot(next <= row0 + t));
+        c = lane == t ? m : c;
+      }
+      const int begin = __shfl(next, c > 0 ? c - 1 : 0), end = __shfl(next, c < 63 ? c : 63), q = from + c - 1;
+      in = in && q >= 0 && q < k.seqs;
+      first = (c > 0 ? begin : in_front) == r;
+      last = end == r + 1;
+      s.seq = q < 0 ? 0 : q < k.seqs ? q : k.seqs - 1;
+    } else {                             // more than 64 empty sequences here: the last one that begins at r or in front
+      int lo = 0, hi = k.seqs;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (k.starts[mid] <= r) lo = mid;
+        else hi = mid - 1;
+      }
+      s.seq = lo < k.seqs ? lo : k.seqs - 1;
+      in = in && lo < k.seqs && k.starts[lo] <= r;
+      first = in && k.starts[s.seq] == r;
+      last = in && k.starts[s.seq + 1] == r + 1;
+    }
   }
   s.in = __ballot(in);
   s.first = __ballot(in && first);
@@ -174,15 +200,11 @@ __device__ __forceinline__ void scan_state(const float* m, int ld, int seq, cons
   else sc_zero<V>(h);
 }
 
-// A and B of a chunk; backward: C too
+// A and B of a chunk; backward: C too.  `seed` (true is returned where there is one): the state in front of the last sequence that begins here, or what arrives at the end of one from a
+// chunk in front, read before another chunk writes its result into the same memory.
 template <typename E, int V, bool WHOLE, int FORM, bool BWD, int R>
-__global__ __launch_bounds__(256) void scan_sums_k(ScanArgs k) {
-  const int64_t waves = (int64_t)k.chunks * ((k.width + 64 * V - 1) / (64 * V));
-  const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (wave >= waves) return;
-  const ScanAt p = scan_at<V>(k, wave);
-  const int64_t mine = (int64_t)p.chunk * k.width + p.c;
-  float A[V], B[V], C[V];
+__device__ __forceinline__ bool scan_sums(const ScanArgs& k, const ScanAt& p, ScanRows& rows, float A[V], float B[V], float C[V], float seed[V]) {
+  bool seeded = false;
 #pragma unroll
   for (int e = 0; e < V; ++e) { A[e] = 1.f; B[e] = C[e] = 0.f; }
   ScanRaw<E, V> f[R], x[R], g[R], dy[R];
@@ -197,8 +219,8 @@ __global__ __launch_bounds__(256) void scan_sums_k(ScanArgs k) {
     }
   };
   if (p.left > 0) ask(0);              // before the search for the sequences
-  const ScanRows rows = scan_rows(k, p.r0, p.n);
-  if (p.left <= 0) return;
+  rows = scan_rows(k, p.r0, p.n);
+  if (p.left <= 0) return false;
   const uint64_t events = rows.events();
   for (int t0 = 0; t0 < p.n; t0 += R) {
     flags = scan_flags(k.flags);
@@ -233,8 +255,11 @@ __global__ __launch_bounds__(256) void scan_sums_k(ScanArgs k) {
         if (rows.first >> t & 1) {
           scan_state<V, WHOLE>(k.h0, k.ldh0, rows.of(t), p, B);
           sc_zero<V>(A);
-          // the state in front of a sequence that goes on behind this chunk, before another chunk writes the one behind it into the same memory
-          if (!BWD) sc_store<float, V, WHOLE>(k.seed + mine, p.left, B);
+          if (!BWD) {
+            seeded = true;
+#pragma unroll
+            for (int e = 0; e < V; ++e) seed[e] = B[e];
+          }
         }
         last = rows.last >> t & 1;
         if (BWD && last && (flags & SK_DHEND)) {
@@ -242,8 +267,11 @@ __global__ __launch_bounds__(256) void scan_sums_k(ScanArgs k) {
           scan_state<V, WHOLE>(k.dh_end, k.lddhe, rows.of(t), p, d);
 #pragma unroll
           for (int e = 0; e < V; ++e) into[i][e] += d[e];
-          // what arrives at the end of a sequence from a chunk in front, before another chunk writes dh0 into the same memory
-          if (!(rows.first << (63 - t))) sc_store<float, V, WHOLE>(k.seed + mine, p.left, d);
+          if (!(rows.first << (63 - t))) {
+            seeded = true;
+#pragma unroll
+            for (int e = 0; e < V; ++e) seed[e] = d[e];
+          }
         }
       }
 #pragma unroll
@@ -256,6 +284,20 @@ __global__ __launch_bounds__(256) void scan_sums_k(ScanArgs k) {
       if (BWD && last) sc_zero<V>(A);
     }
   }
+  return seeded;
+}
+template <typename E, int V, bool WHOLE, int FORM, bool BWD, int R>
+__global__ __launch_bounds__(256) void scan_sums_k(ScanArgs k) {
+  const int64_t waves = (int64_t)k.chunks * ((k.width + 64 * V - 1) / (64 * V));
+  const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (wave >= waves) return;
+  const ScanAt p = scan_at<V>(k, wave);
+  const int64_t mine = (int64_t)p.chunk * k.width + p.c;
+  float A[V], B[V], C[V], seed[V];
+  ScanRows rows;
+  const bool seeded = scan_sums<E, V, WHOLE, FORM, BWD, R>(k, p, rows, A, B, C, seed);
+  if (p.left <= 0) return;
+  if (seeded) sc_store<float, V, WHOLE>(k.seed + mine, p.left, seed);
   sc_store<float, V, WHOLE>(k.A + mine, p.left, A);
   sc_store<float, V, WHOLE>(k.B + mine, p.left, B);
   if (BWD) sc_store<float, V, WHOLE>(k.C + mine, p.left, C);
@@ -348,20 +390,65 @@ __device__ __forceinline__ void scan_empty(const ScanArgs& k, int64_t block, con
   }
 }
 
-template <typename E, int V, bool WHOLE, int FORM, int R, bool ONCE>
-__global__ __launch_bounds__(256) void scan_walk_k(ScanArgs k) {
+// Few rows: a block has all chunks of its 64 V columns, a wavefront each, and the states go from one to the next through LDS: one launch instead of three (57 x 496 float 8.0 us
+// instead of 13.5, with the gradients 17.6 instead of 28).  Sixteen wavefronts forward; backward eight, which have the registers it needs.  Past 128 rows a wavefront waits more
+// often for its rows than the launches cost (250 x 1024: 17.4 us and 34.3, with three launches 14.3 and 30.9).
+constexpr int scan_few_waves(bool backward) { return backward ? 8 : 16; }
+enum { kScanFew = 128, kScanFewR = 8 };        // rows at most; rows that are asked for together: nothing else hides what a load takes
+// the number that the wavefront has where chunks are dealt to blocks of any: of chunk `me`, -1 where there is none; blocks behind the groups' have the empty sequences
+__device__ __forceinline__ int64_t scan_few_wave(const ScanArgs& k, int n, int groups, int me) {
+  const int b = (int)blockIdx.x;
+  if (b >= groups) return (int64_t)k.chunks * groups + (int64_t)(b - groups) * n + me;
+  return me < k.chunks ? (int64_t)me * groups + b : -1;
+}
+// h and (backward) mu of the wavefront's chunk; false where it has none
+template <typename E, int V, bool WHOLE, int FORM, bool BWD, int R, int N>
+__device__ __forceinline__ bool scan_pass(const ScanArgs& k, const ScanAt& p, ScanRows& rows, int64_t wave, int me, float h[V], float mu[V], float seed[V]) {
+  __shared__ float sA[N][64 * V], sB[N][64 * V], sC[BWD ? N : 1][64 * V];
+  const int at = (threadIdx.x & 63) * V;
+  if (wave >= 0) {
+    float A[V], B[V], C[V];
+    scan_sums<E, V, WHOLE, FORM, BWD, R>(k, p, rows, A, B, C, seed);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      sA[me][at + e] = A[e];
+      sB[me][at + e] = B[e];
+      if (BWD) sC[me][at + e] = C[e];
+    }
+  }
+  __syncthreads();
+  if (wave < 0) return false;
+  for (int j = 0; j < me; ++j)
+#pragma unroll
+    for (int e = 0; e < V; ++e) h[e] = fmaf(sA[j][at + e], h[e], sB[j][at + e]);
+  if (BWD)
+    for (int j = k.chunks - 1; j > me; --j)
+#pragma unroll
+      for (int e = 0; e < V; ++e) mu[e] = fmaf(sA[j][at + e], mu[e], sC[j][at + e]);
+  return true;
+}
+
+// FEW: the states in front by scan_pass, otherwise from memory
+template <typename E, int V, bool WHOLE, int FORM, int R, bool ONCE, bool FEW>
+__global__ __launch_bounds__(64 * (FEW ? scan_few_waves(false) : 4)) void scan_walk_k(ScanArgs k) {
+  constexpr int N = FEW ? scan_few_waves(false) : 4;
   const int groups = (k.width + 64 * V - 1) / (64 * V);
   const int64_t waves = (int64_t)k.chunks * groups, all = waves + (k.starts || k.length == 0 ? (int64_t)((k.seqs + 63) / 64) * groups : 0);
-  const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (wave >= all) return;
+  const int me = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t wave = FEW ? scan_few_wave(k, N, groups, me) : (int64_t)blockIdx.x * 4 + me;
+  if (!FEW && wave >= all) return;
   if (wave >= waves) {
-    scan_empty<V, WHOLE>(k, wave - waves, k.h0, k.ldh0, k.h_end, k.ldhe);
+    if (wave < all) scan_empty<V, WHOLE>(k, wave - waves, k.h0, k.ldh0, k.h_end, k.ldhe);
     return;
   }
-  const ScanAt p = scan_at<V>(k, wave);
+  const ScanAt p = scan_at<V>(k, wave < 0 ? 0 : wave);
   const int64_t mine = (int64_t)p.chunk * k.width + p.c;
-  float h[V];
+  float h[V], seed[FEW ? V : 1];
+  ScanRows rows;
   sc_zero<V>(h);
+  if constexpr (FEW) {
+    if (!scan_pass<E, V, WHOLE, FORM, false, R, N>(k, p, rows, wave, me, h, h, seed)) return;
+  }
   ScanRaw<E, V> f[R], x[R], g[R];
   const char *const qf = k.f + p.r0 * k.ldf, *const qx = k.x + p.r0 * k.ldx, *const qg = k.g + p.r0 * k.ldg;
   char* const qy = k.y + p.r0 * k.ldy;
@@ -372,10 +459,10 @@ __global__ __launch_bounds__(256) void scan_walk_k(ScanArgs k) {
     if (flags & SK_G) scan_ask<E, V, WHOLE, R, ONCE>(qg, k.ldg, p, t, g);
   };
   if (p.left > 0) {
-    if (!(flags & SK_WHOLE)) sc_load<float, V, WHOLE>(k.state + mine, p.left, h);
+    if (!FEW && !(flags & SK_WHOLE)) sc_load<float, V, WHOLE>(k.state + mine, p.left, h);
     ask(0);
   }
-  const ScanRows rows = scan_rows(k, p.r0, p.n);
+  if constexpr (!FEW) rows = scan_rows(k, p.r0, p.n);
   if (p.left <= 0) return;
   const uint64_t events = rows.events();
   for (int t0 = 0; t0 < p.n; t0 += R) {
@@ -397,8 +484,12 @@ __global__ __launch_bounds__(256) void scan_walk_k(ScanArgs k) {
         if (!(rows.in >> t & 1)) continue;
         if (rows.first >> t & 1) {
           // one that goes on behind the chunk: its state from the copy
-          if (!(flags & SK_WHOLE) && !(rows.last >> t)) sc_load<float, V, WHOLE>(k.seed + mine, p.left, h);
-          else scan_state<V, WHOLE>(k.h0, k.ldh0, rows.of(t), p, h);
+          if (!(flags & SK_WHOLE) && !(rows.last >> t)) {
+            if constexpr (FEW)
+#pragma unroll
+              for (int e = 0; e < V; ++e) h[e] = seed[e];
+            else sc_load<float, V, WHOLE>(k.seed + mine, p.left, h);
+          } else scan_state<V, WHOLE>(k.h0, k.ldh0, rows.of(t), p, h);
         }
         last = rows.last >> t & 1;
       }
@@ -417,37 +508,42 @@ __global__ __launch_bounds__(256) void scan_walk_k(ScanArgs k) {
 
 // A chunk's states from the first row on, of which those in front of every R rows are kept in LDS; then its gradients from the last row to the first, the states of
 // R rows at a time made again.
-template <typename E, int V, bool WHOLE, int FORM, int R, bool ONCE>
-__global__ __launch_bounds__(256) void scan_back_k(ScanArgs k) {
-  __shared__ float held[4][kScanT / R][64 * V];
+template <typename E, int V, bool WHOLE, int FORM, int R, bool ONCE, bool FEW>
+__global__ __launch_bounds__(64 * (FEW ? scan_few_waves(true) : 4)) void scan_back_k(ScanArgs k) {
+  constexpr int N = FEW ? scan_few_waves(true) : 4;
+  __shared__ float held[N][(FEW ? kScanFew / N : kScanT) / R][64 * V];
   const int groups = (k.width + 64 * V - 1) / (64 * V);
   const int64_t waves = (int64_t)k.chunks * groups, all = waves + (k.starts || k.length == 0 ? (int64_t)((k.seqs + 63) / 64) * groups : 0);
   const int me = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t wave = (int64_t)blockIdx.x * 4 + me;
-  if (wave >= all) return;
+  const int64_t wave = FEW ? scan_few_wave(k, N, groups, me) : (int64_t)blockIdx.x * 4 + me;
+  if (!FEW && wave >= all) return;
   if (wave >= waves) {
-    scan_empty<V, WHOLE>(k, wave - waves, k.dh_end, k.lddhe, k.dh0, k.lddh0);
+    if (wave < all) scan_empty<V, WHOLE>(k, wave - waves, k.dh_end, k.lddhe, k.dh0, k.lddh0);
     return;
   }
-  const ScanAt p = scan_at<V>(k, wave);
+  const ScanAt p = scan_at<V>(k, wave < 0 ? 0 : wave);
   const int64_t mine = (int64_t)p.chunk * k.width + p.c;
   float* const keep = held[me][0] + (threadIdx.x & 63) * V;          // a lane's own: nothing to wait for
-  float h[V], mu[V];
+  float h[V], mu[V], seed[FEW ? V : 1];
+  ScanRows rows;
   sc_zero<V>(h);
   sc_zero<V>(mu);
+  if constexpr (FEW) {
+    if (!scan_pass<E, V, WHOLE, FORM, true, R, N>(k, p, rows, wave, me, h, mu, seed)) return;
+  }
   ScanRaw<E, V> f[R], x[R], g[R], dy[R];
   const char *const qf = k.f + p.r0 * k.ldf, *const qx = k.x + p.r0 * k.ldx, *const qg = k.g + p.r0 * k.ldg, *const qdy = k.dy + p.r0 * k.lddy;
   char *const qdf = k.df + p.r0 * k.lddf, *const qdx = k.dx + p.r0 * k.lddx, *const qdg = k.dg + p.r0 * k.lddg;
   int flags = k.flags;
   if (p.left > 0) {
-    if (!(flags & SK_WHOLE)) {
+    if (!FEW && !(flags & SK_WHOLE)) {
       sc_load<float, V, WHOLE>(k.state + mine, p.left, h);
       sc_load<float, V, WHOLE>(k.back + mine, p.left, mu);
     }
     scan_ask<E, V, WHOLE, R>(qf, k.ldf, p, 0, f);
     scan_ask<E, V, WHOLE, R>(qx, k.ldx, p, 0, x);
   }
-  const ScanRows rows = scan_rows(k, p.r0, p.n);
+  if constexpr (!FEW) rows = scan_rows(k, p.r0, p.n);
   if (p.left <= 0) return;
   const uint64_t events = rows.events();
   const int t_end = (p.n - 1) / R * R;
@@ -521,7 +617,12 @@ __global__ __launch_bounds__(256) void scan_back_k(ScanArgs k) {
         if (!(rows.in >> t & 1)) continue;
         if (rows.last >> t & 1) {
           // of a sequence from a chunk in front: the copy of what arrives at its end
-          if ((flags & SK_DHEND) && !(flags & SK_WHOLE) && !(rows.first << (63 - t))) sc_load<float, V, WHOLE>(k.seed + mine, p.left, mu);
+          if ((flags & SK_DHEND) && !(flags & SK_WHOLE) && !(rows.first << (63 - t))) {
+            if constexpr (FEW)
+#pragma unroll
+              for (int e = 0; e < V; ++e) mu[e] = seed[e];
+            else sc_load<float, V, WHOLE>(k.seed + mine, p.left, mu);
+          }
           else scan_state<V, WHOLE>(k.dh_end, k.lddhe, rows.of(t), p, mu);
         }
         first = rows.first >> t & 1;
@@ -547,14 +648,13 @@ __global__ __launch_bounds__(256) void scan_back_k(ScanArgs k) {
   }
 }
 
-// Rows of a chunk.  Where whole sequences fit into one, no more than they have.  Otherwise by what the launches cost in steps of a row: rounds of wavefronts (eight to a SIMD forward, four
-// backward) of a chunk's rows and six steps' worth of beginning, and a step for each 64 chunks that the states are followed through (1500 x 333 fp32, forward and backward: chunks of 8
-// 32 us, of 32 51).
 static int scan_per(const ftp_scan_args& a, int V, bool backward, bool& whole) {
   const int64_t groups = (a.width + 64 * V - 1) / (64 * V), slots = backward ? 4096 : 8192;
   whole = a.starts ? a.rows <= kScanT : a.length <= kScanT;
   if (!a.starts && a.length > 0 && whole) return (int)(std::max<int64_t>(1, std::min<int64_t>(kScanT / a.length, a.seqs * groups / 4096)) * a.length);
   if (whole) return kScanT;
+  const int few = scan_few_waves(backward);
+  if (a.rows <= kScanFew) return (int)((a.rows + few * kScanR - 1) / (few * kScanR) * kScanR);
   int per = kScanT;
   int64_t least = INT64_MAX;
   for (int p = kScanT; p >= 8; p -= kScanR) {
@@ -593,7 +693,7 @@ static ScanArgs scan_plan(const ftp_scan_args& a, bool backward, size_t& bytes) 
   k.flags |= whole ? SK_WHOLE : 0;
   k.chunks = (int)((a.rows + k.per - 1) / k.per);
   bytes = 0;
-  if (whole) return k;
+  if (whole || a.rows <= kScanFew) return k;
   const size_t one = ((size_t)k.chunks * a.width * 4 + 255) & ~(size_t)255;
   const auto take = [&]() { float* p = (float*)((char*)a.ws + bytes); bytes += one; return p; };
   k.A = take();
@@ -618,14 +718,22 @@ static void scan_launch(hipStream_t st, const ScanArgs& k) {
   // what is read and written for the last time goes past the caches (16384 x 2048 bfloat16 forward 90 -> 82 us, both ways 281 -> 266)
   const bool once = past_the_caches((double)k.rows * k.width * sizeof(E) * (BWD ? 6 : 4));
   if (scan_blocks(k, V, true) >= 1u << 24) return launch_plan_failed("scan: more than 2^32 threads");
+  if (!(k.flags & SK_WHOLE) && k.rows <= kScanFew) {
+    constexpr int N = scan_few_waves(BWD);
+    const int groups = (k.width + 64 * V - 1) / (64 * V);
+    const int64_t blocks = groups + (k.starts ? ((int64_t)((k.seqs + 63) / 64) * groups + N - 1) / N : 0);
+    if (BWD) hipLaunchKernelGGL((scan_back_k<E, V, WHOLE, FORM, kScanFewR, false, true>), dim3((unsigned)blocks), dim3(64 * N), 0, st, k);
+    else hipLaunchKernelGGL((scan_walk_k<E, V, WHOLE, FORM, kScanFewR, false, true>), dim3((unsigned)blocks), dim3(64 * N), 0, st, k);
+    return;
+  }
   if (!(k.flags & SK_WHOLE)) {
     hipLaunchKernelGGL((scan_sums_k<E, V, WHOLE, FORM, BWD, kScanR>), dim3(scan_blocks(k, V, false)), dim3(256), 0, st, k);
     hipLaunchKernelGGL(scan_follow_k, dim3((k.width + 31) / 32, BWD ? 2 : 1), dim3(1024), 0, st, k);
   }
   const auto go = [&](auto f) { hipLaunchKernelGGL(f, dim3(scan_blocks(k, V, true)), dim3(256), 0, st, k); };
   constexpr bool ONCE = WHOLE && sizeof(E) * V == 4;
-  if (BWD) once ? go(scan_back_k<E, V, WHOLE, FORM, kScanR, ONCE>) : go(scan_back_k<E, V, WHOLE, FORM, kScanR, false>);
-  else once ? go(scan_walk_k<E, V, WHOLE, FORM, kScanR, ONCE>) : go(scan_walk_k<E, V, WHOLE, FORM, kScanR, false>);
+  if (BWD) once ? go(scan_back_k<E, V, WHOLE, FORM, kScanR, ONCE, false>) : go(scan_back_k<E, V, WHOLE, FORM, kScanR, false, false>);
+  else once ? go(scan_walk_k<E, V, WHOLE, FORM, kScanR, ONCE, false>) : go(scan_walk_k<E, V, WHOLE, FORM, kScanR, false, false>);
 }
 template <bool BWD, typename E, int V, bool WHOLE>
 static void scan_form(hipStream_t st, const ScanArgs& k, int form) {

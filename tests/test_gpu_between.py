@@ -364,6 +364,30 @@ def test_scan_long_memory(env):
     assert bool((df == 0).all())
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows", [63, 65, 100, 127, 128, 129, 160])
+def test_scan_few_rows(env, dtype, rows):
+    """up to 128 rows go in one launch: one sequence, several, and h_end and dh0 in their operands' buffers"""
+    scan_case(env, dtype, [rows], 130)
+    scan_case(env, dtype, [rows // 2, 0, rows - rows // 2 - 9, 5], 67, "unit", "gelu", front=1, behind=3)
+    scan_case(env, dtype, [rows - 20, 20], 64, in_place=True)
+    scan_case(env, dtype, [rows], 33, "add", "", uniform=True)
+
+
+@pytest.mark.parametrize("empty", [0, 61, 62, 63, 64, 65, 130])
+@pytest.mark.parametrize("tail", [1, 300])
+def test_scan_many_empty_sequences_together(env, empty, tail):
+    """around as many starts inside a chunk as a wavefront has lanes, with and without rows behind them"""
+    scan_case(env, "f32", [3] + [0] * empty + [1, 0, 20] + [0] * empty + [2, tail], 70, behind=3, front=2)
+    scan_case(env, "f32", [0] * empty + [tail] + [0] * empty, 70)
+
+
+@pytest.mark.parametrize("seqs", [63, 64, 65, 127, 129, 4095, 4097, 9000])
+def test_scan_starts_by_count(env, seqs):
+    """the search among as many starts as fill its steps, and one more or less"""
+    scan_case(env, "f32", [1 + (i % 7 == 3) for i in range(seqs)], 5, front=1)
+
+
 def test_scan_bad_starts_stay_inside(env):
     """starts that fall or lie outside: undefined results, and nothing else is touched"""
     torch, P, _ = env
