@@ -81,32 +81,36 @@ void bt_dropout(hipStream_t st, int dt, int64_t rows, int cols, const DropMask& 
 // Sum over the block's threads of one value or of two, the same in all of them: within a wavefront into its last lane, through LDS into groups of T / 64 lanes of all
 // wavefronts, and there once more.  `s` is used in turn by calls that follow one another.
 template <int N>
-__device__ __forceinline__ float lanes_sum(float v) {            // over N consecutive lanes, 2 .. 16
+__device__ __forceinline__ float lanes_sum(float v) {            // over N consecutive lanes, 2 .. 32
   v += dpp_move<0xB1>(v);
   if (N > 2) v += dpp_move<0x4E>(v);
   if (N > 4) v += dpp_move<0x141>(v);
   if (N > 8) v += dpp_move<0x140>(v);
+  if (N > 16) v += __shfl_xor(v, 16);
   return v;
 }
+constexpr int join_waves(int T) { return T < 64 ? 1 : T / 64; }
 template <int T>
-__device__ __forceinline__ float block_sum(float a, float2 (*s)[T / 64], int& turn) {
-  if (T == 64) return wave_sum(a);
+__device__ __forceinline__ float block_sum(float a, float2 (*s)[join_waves(T)], int& turn) {
+  if constexpr (T < 64) return lanes_sum<T>(a);
+  if constexpr (T == 64) return wave_sum(a);
   a = wave_sum_last(a);
   float2* const p = s[turn ^= 1];
   if ((threadIdx.x & 63) == 63) p[threadIdx.x >> 6].x = a;
   __syncthreads();
-  return lanes_sum<T / 64>(p[threadIdx.x & (T / 64 - 1)].x);
+  return lanes_sum<join_waves(T)>(p[threadIdx.x & (join_waves(T) - 1)].x);
 }
 template <int T>
-__device__ __forceinline__ float2 block_sum2(float a, float b, float2 (*s)[T / 64], int& turn) {
-  if (T == 64) return make_float2(wave_sum(a), wave_sum(b));
+__device__ __forceinline__ float2 block_sum2(float a, float b, float2 (*s)[join_waves(T)], int& turn) {
+  if constexpr (T < 64) return make_float2(lanes_sum<T>(a), lanes_sum<T>(b));
+  if constexpr (T == 64) return make_float2(wave_sum(a), wave_sum(b));
   a = wave_sum_last(a);
   b = wave_sum_last(b);
   float2* const p = s[turn ^= 1];
   if ((threadIdx.x & 63) == 63) p[threadIdx.x >> 6] = make_float2(a, b);
   __syncthreads();
-  const float2 t = p[threadIdx.x & (T / 64 - 1)];
-  return make_float2(lanes_sum<T / 64>(t.x), lanes_sum<T / 64>(t.y));
+  const float2 t = p[threadIdx.x & (join_waves(T) - 1)];
+  return make_float2(lanes_sum<join_waves(T)>(t.x), lanes_sum<join_waves(T)>(t.y));
 }
 
 // one row's operands, eight columns at a time
@@ -461,7 +465,7 @@ __device__ __forceinline__ void join_weight(const float* w, int c, int left, flo
 }
 // v (zeros past the row's end) less its mean (layer), and its inverse deviation
 template <int T, bool WHOLE>
-__device__ __forceinline__ float join_deviation(const JoinK& k, int flags, float inv, int left, float v[8], float2 (*s)[T / 64], int& turn) {
+__device__ __forceinline__ float join_deviation(const JoinK& k, int flags, float inv, int left, float v[8], float2 (*s)[join_waves(T)], int& turn) {
   if (flags & JK_LAYER) {
     float t = 0.f;
 #pragma unroll
@@ -476,14 +480,23 @@ __device__ __forceinline__ float join_deviation(const JoinK& k, int flags, float
   return 1.f / sqrtf(fmaf(block_sum<T>(q, s, turn), inv, k.eps));
 }
 
+// Rows of up to 128 columns take 16 lanes and those of up to 256 take 32: a wavefront has four rows or two at a time, each group of lanes its own range
+// (a wavefront a row: 65536 x 128 bfloat16, one norm, forward 23 us and both ways 89; so 12 and 46).
+template <int T>
+__device__ __forceinline__ int join_lane() { return T < 64 ? threadIdx.x & (T - 1) : threadIdx.x; }
+template <int T>
+__device__ __forceinline__ int64_t join_walker() { return T < 64 ? (int64_t)blockIdx.x * (64 / T) + threadIdx.x / T : blockIdx.x; }
+constexpr int join_walkers(int T) { return T < 64 ? 64 / T : 1; }        // of a block
+
 template <typename E, int T, int ROWS>
-__global__ __launch_bounds__(T) void join_row_k(JoinK k, DropMask m, int64_t per) {
+__global__ __launch_bounds__(64 * join_waves(T)) void join_row_k(JoinK k, DropMask m, int64_t per) {
   constexpr bool WHOLE = ROWS > 0, ONCE = ROWS == 2;
-  __shared__ float2 s[2][T / 64];
-  const int c = threadIdx.x * 8, left = k.width - c;
+  __shared__ float2 s[2][join_waves(T)];
+  const int me = join_lane<T>(), c = me * 8, left = k.width - c;
   const float inv = 1.f / (float)k.width;
   const MaskKey key = mask_key(m);
-  const int64_t r0 = blockIdx.x * per, r1 = r0 + per < k.rows ? r0 + per : k.rows;
+  const int64_t r0 = join_walker<T>() * per, r1 = r0 + per < k.rows ? r0 + per : k.rows;
+  if (T < 64 && r0 >= k.rows) return;
   int turn = 0, flags = k.flags;
   JoinWalk at = join_walk<false>(k, r0);
   JoinIn<E, false> in, next;
@@ -511,7 +524,7 @@ __global__ __launch_bounds__(T) void join_row_k(JoinK k, DropMask m, int64_t per
       join_open_gate<E, false>(k, flags, in, g);
       if (m.least) {
         uint32_t keep[8];
-        mask8(m, key, number, threadIdx.x, keep);
+        mask8(m, key, number, me, keep);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = dropped(v[e], keep[e]);
       }
@@ -531,16 +544,18 @@ __global__ __launch_bounds__(T) void join_row_k(JoinK k, DropMask m, int64_t per
   }
 }
 enum { kJoinHeld = 8192 };
-// blocks for `rows` rows: half the card's wavefronts at most (8192 x 4096 bfloat16, forward and backward, 208 us; all of them 212, of which the blocks' sums are more)
+// blocks for `rows` rows: half the card's wavefronts at most (with all of them the blocks' sums take longer: 4 us more of 195 for 8192 x 4096 bfloat16, forward and backward)
 static int64_t join_blocks(int64_t rows, int T) { return std::max<int64_t>(1, std::min<int64_t>(256 * 1024 / T, rows)); }
 static int join_threads(int width) {
-  int t = 64;
+  int t = 16;
   while (t * 8 < width) t *= 2;
   return t;
 }
 template <typename F>
 static void join_by_threads(int t, F f) {
-  if (t == 64) f(std::integral_constant<int, 64>());
+  if (t == 16) f(std::integral_constant<int, 16>());
+  else if (t == 32) f(std::integral_constant<int, 32>());
+  else if (t == 64) f(std::integral_constant<int, 64>());
   else if (t == 128) f(std::integral_constant<int, 128>());
   else if (t == 256) f(std::integral_constant<int, 256>());
   else if (t == 512) f(std::integral_constant<int, 512>());
@@ -556,7 +571,8 @@ void bt_join(hipStream_t st, const ftp_join_args& a, const DropMask& m) {
     const int t = join_threads(a.width);
     // forward there are no blocks' sums: twice the card's wavefronts (16384 x 1024 36 us, half of them 39)
     const int64_t want = std::min<int64_t>(a.rows, 256 * 4096 / t), per = (a.rows + want - 1) / want;
-    const dim3 g((unsigned)((a.rows + per - 1) / per)), b(t);
+    const int64_t walkers = (a.rows + per - 1) / per;
+    const dim3 g((unsigned)((walkers + join_walkers(t) - 1) / join_walkers(t))), b(64 * join_waves(t));
     join_by_threads(t, [&](auto tc) {
       constexpr int T = decltype(tc)::value;
       const JoinK k = join_k(a, m, false);
@@ -583,10 +599,12 @@ struct JoinRanges {
   int64_t group;       // rows that share a gate row (all of them where there is none, or one each)
   int parts;           // blocks of a group
   int blocks;
+  int sums;            // rows of the weights' sums: one of each block of threads, which may have several ranges
 };
 static JoinRanges join_ranges(const ftp_join_args& a) {
-  const int64_t blocks = join_blocks(a.rows, a.width <= kJoinHeld ? join_threads(a.width) : 1024), want = std::max<int64_t>(1, (a.rows + blocks - 1) / blocks);
-  JoinRanges r{want, 0, 1, 0};
+  const int t = a.width <= kJoinHeld ? join_threads(a.width) : 1024;
+  const int64_t blocks = join_blocks(a.rows, t), want = std::max<int64_t>(1, (a.rows + blocks - 1) / blocks);
+  JoinRanges r{want, 0, 1, 0, 0};
   r.group = a.gate && a.gate_rows > 1 ? std::min(a.gate_rows, a.rows) : 0;
   if (r.group == 0) {
     r.blocks = (int)((a.rows + want - 1) / want);
@@ -598,17 +616,18 @@ static JoinRanges join_ranges(const ftp_join_args& a) {
     r.per = (r.group + r.parts - 1) / r.parts;
     r.blocks = (int)((a.rows + r.group - 1) / r.group) * r.parts;
   }
+  r.sums = (r.blocks + join_walkers(t) - 1) / join_walkers(t);
   return r;
 }
 enum { JP_PRE_W, JP_PRE_BIAS, JP_POST_W, JP_POST_BIAS, JP_GATE, JP_ALL };
 struct JoinParts { float* p[JP_ALL]; };           // [blocks][width] each, or null
 
-__device__ __forceinline__ void join_range(const JoinRanges& g, int64_t rows, int64_t& r0, int64_t& r1) {
+__device__ __forceinline__ void join_range(const JoinRanges& g, int64_t walker, int64_t rows, int64_t& r0, int64_t& r1) {
   if (g.parts == 1) {
-    r0 = blockIdx.x * g.per;
+    r0 = walker * g.per;
     r1 = r0 + g.per;
   } else {
-    const int64_t first = (int64_t)(blockIdx.x / g.parts) * g.group, at = (int64_t)(blockIdx.x % g.parts) * g.per;
+    const int64_t first = (int64_t)((uint32_t)walker / g.parts) * g.group, at = (int64_t)((uint32_t)walker % g.parts) * g.per;
     r0 = first + at;
     r1 = first + (at + g.per < g.group ? at + g.per : g.group);
   }
@@ -639,7 +658,7 @@ __global__ __launch_bounds__(kJoinT) void join_wide_bwd_k(ftp_join_args a, JoinK
   JoinWide<E> w{JoinRow<E>{a, m, mask_key(m), 0, 0.f, 1.f}, a.width, 0, s};
   const int N = a.width;
   int64_t r0, r1;
-  join_range(g, a.rows, r0, r1);
+  join_range(g, blockIdx.x, a.rows, r0, r1);
   if (r0 >= r1) {                        // a part behind the last row
     for (int k = 0; k < JP_ALL; ++k)
       if (float* const p = parts.p[k]) w.columns([&](int c, int left) { const float z[8] = {}; tk_store8<float>(p + (int64_t)blockIdx.x * N + c, left, z); });
@@ -801,15 +820,16 @@ struct JoinSums {
 };
 // BIAS: sums of the biases as well, and a bias behind the block
 template <typename E, int T, bool BIAS, int ROWS, bool LDS, bool AHEAD, bool HOLD>
-__global__ __launch_bounds__(T, T == 512 && sizeof(E) == 2 ? 4 : 1) void join_row_bwd_k(JoinK k, DropMask m, JoinRanges gr, float* parts, int64_t part_size, int wanted) {
+__global__ __launch_bounds__(64 * join_waves(T), T == 512 && sizeof(E) == 2 ? 4 : 1) void join_row_bwd_k(JoinK k, DropMask m, JoinRanges gr, float* parts, int64_t part_size, int wanted) {
   constexpr bool WHOLE = ROWS > 0, ONCE = ROWS == 2;
-  __shared__ float2 s[2][T / 64];
+  __shared__ float2 s[2][join_waves(T)];
   extern __shared__ float4 held[];
-  const int c = threadIdx.x * 8, left = k.width - c;
+  const int me = join_lane<T>(), c = me * 8, left = k.width - c;
+  const int64_t walker = join_walker<T>();
   const float inv = 1.f / (float)k.width;
   const MaskKey key = mask_key(m);
   int64_t r0, r1;
-  join_range(gr, k.rows, r0, r1);
+  join_range(gr, walker, k.rows, r0, r1);
   JoinSums<T, LDS> sum;
   sum.start(wanted, held);
   int turn = 0, flags = k.flags, want = wanted;
@@ -855,7 +875,7 @@ __global__ __launch_bounds__(T, T == 512 && sizeof(E) == 2 ? 4 : 1) void join_ro
         }
         join_open_gate<E, true>(k, flags, in, g);
         if (m.least) {
-          mask8(m, key, number, threadIdx.x, keep);
+          mask8(m, key, number, me, keep);
 #pragma unroll
           for (int e = 0; e < 8; ++e) cc[e] = dropped(cc[e], keep[e]);
         }
@@ -939,14 +959,22 @@ __global__ __launch_bounds__(T, T == 512 && sizeof(E) == 2 ? 4 : 1) void join_ro
     }
   }
   if (left <= 0) return;
-  float* to = parts + (int64_t)blockIdx.x * k.width + c;
+  float* to = parts + c;
 #pragma unroll
   for (int j = 0; j < JP_ALL; ++j) {
     if (!(wanted >> j & 1)) continue;
     if ((BIAS || (j != JP_PRE_BIAS && j != JP_POST_BIAS)) && !(j == JP_GATE && gr.parts == 1)) {
       float v[8];
       sum.take(j, v);
-      tk_store8<float>(to, left, v);
+      if (T < 64 && j != JP_GATE) {      // the lanes' groups are added up
+#pragma unroll
+        for (int n = T; n < 64; n *= 2)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] += __shfl_xor(v[e], n);
+        if (threadIdx.x < T) tk_store8<float>(to + (int64_t)blockIdx.x * k.width, left, v);
+      } else if (T >= 64 || walker < gr.blocks) {
+        tk_store8<float>(to + walker * k.width, left, v);
+      }
     }
     to += part_size;
   }
@@ -962,7 +990,7 @@ __global__ __launch_bounds__(1024) void join_sum_k(JoinParts parts, JoinRanges g
     const bool gate = job >= JP_GATE;
     const float* const p = gate ? parts.p[JP_GATE] + (job - JP_GATE) * g.parts * N : parts.p[job];
     if (!p) continue;                    // the same for all threads
-    const int n = gate ? g.parts : g.blocks;
+    const int n = gate ? g.parts : g.sums;
     float v = 0.f;
     if (c < N) {
 #pragma unroll 16
@@ -1038,7 +1066,7 @@ void bt_join_bwd(hipStream_t st, const ftp_join_args& a, const DropMask& m) {
     join_by_threads(t, [&](auto tc) {
       constexpr int T = decltype(tc)::value;
       constexpr bool L = T >= 512;
-      const auto go = [&](auto f) { hipLaunchKernelGGL(f, dim3(r.blocks), dim3(T), L ? (size_t)sums * T * 32 : 0, st, k, m, r, (float*)a.ws, (int64_t)(join_part_bytes(a, r) / 4), want); };
+      const auto go = [&](auto f) { hipLaunchKernelGGL(f, dim3(r.sums), dim3(64 * join_waves(T)), L ? (size_t)sums * T * 32 : 0, st, k, m, r, (float*)a.ws, (int64_t)(join_part_bytes(a, r) / 4), want); };
       const auto by = [&](auto* e) {
         typedef std::remove_pointer_t<decltype(e)> E;
         if (a.width % 8) bias ? go(join_row_bwd_k<E, T, true, 0, L, !L, !L>) : go(join_row_bwd_k<E, T, false, 0, L, !L, !L>);

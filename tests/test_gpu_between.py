@@ -206,6 +206,21 @@ def test_join_of_the_longest_rows_that_are_held(env, dtype, width, layer, gate, 
     join_case(env, dtype, 37, width, layer, True, gate, 5, p=0.1, weights=weights, gate_f32=gate == "all")
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5, 7])
+@pytest.mark.parametrize("width", [7, 64, 121, 128, 129, 240, 256, 257])
+def test_join_rows_that_share_a_wavefront(env, dtype, rows, width):
+    """up to 128 columns four rows are in a wavefront, up to 256 two: some of them past the last row"""
+    join_case(env, dtype, rows, width, width % 3 == 0, rows % 2 == 0, "group", 3, p=0.25 if rows > 2 else 0.0)
+
+
+@pytest.mark.parametrize("width", [20, 32, 160])
+@pytest.mark.parametrize("gate,gate_rows", [("none", 0), ("row", 1), ("group", 3), ("group", 9), ("group", 5000), ("all", 0)])
+def test_join_ranges_that_share_a_wavefront(env, width, gate, gate_rows):
+    """more rows than there are ranges, so that a range has several and the last ones of a wavefront fewer or none"""
+    join_case(env, "f32", 18005, width, width == 20, True, gate, gate_rows, p=0.1)
+
+
 def test_join_in_place_and_twice(env):
     torch, P, _ = env
     for width in (200, 40000):
