@@ -544,8 +544,6 @@ __global__ __launch_bounds__(64 * join_waves(T)) void join_row_k(JoinK k, DropMa
   }
 }
 enum { kJoinHeld = 8192 };
-// blocks for `rows` rows: half the card's wavefronts at most (with all of them the blocks' sums take longer: 4 us more of 195 for 8192 x 4096 bfloat16, forward and backward)
-static int64_t join_blocks(int64_t rows, int T) { return std::max<int64_t>(1, std::min<int64_t>(256 * 1024 / T, rows)); }
 static int join_threads(int width) {
   int t = 16;
   while (t * 8 < width) t *= 2;
@@ -601,9 +599,18 @@ struct JoinRanges {
   int blocks;
   int sums;            // rows of the weights' sums: one of each block of threads, which may have several ranges
 };
+static bool join_biased(const ftp_join_args& a) { return a.dpre_bias || a.dpost_bias || (a.post && a.post_bias); }
+// Wavefronts that a SIMD holds of the kernel that a call takes.  As many blocks as the card holds go through their rows at once: a second, shorter round leaves most of it idle, and more
+// blocks are more sums (bfloat16 forward and backward with four to a SIMD where it holds three: 16384 x 1024 111 us instead of 102, 400000 x 128 271 instead of 231; float where it holds
+// two: 8000 x 1024 88 instead of 79)
+static int join_resident(const ftp_join_args& a, int t) {
+  if (t == 1024) return 4;
+  if (t == 512) return a.dtype == FTP_BF16 ? 4 : 2;
+  return a.dtype == FTP_BF16 && !join_biased(a) ? 3 : 2;
+}
 static JoinRanges join_ranges(const ftp_join_args& a) {
   const int t = a.width <= kJoinHeld ? join_threads(a.width) : 1024;
-  const int64_t blocks = join_blocks(a.rows, t), want = std::max<int64_t>(1, (a.rows + blocks - 1) / blocks);
+  const int64_t blocks = 256 * 4 * 64 * join_resident(a, t) / t, want = std::max<int64_t>(1, (a.rows + blocks - 1) / blocks);
   JoinRanges r{want, 0, 1, 0, 0};
   r.group = a.gate && a.gate_rows > 1 ? std::min(a.gate_rows, a.rows) : 0;
   if (r.group == 0) {
@@ -1062,7 +1069,7 @@ void bt_join_bwd(hipStream_t st, const ftp_join_args& a, const DropMask& m) {
   const bool held = a.width <= kJoinHeld && (sums < JP_ALL || join_threads(a.width) < 1024);
   if (held) {
     const int t = join_threads(a.width);
-    const bool bias = a.dpre_bias || a.dpost_bias || (a.post && a.post_bias);
+    const bool bias = join_biased(a);
     join_by_threads(t, [&](auto tc) {
       constexpr int T = decltype(tc)::value;
       constexpr bool L = T >= 512;
