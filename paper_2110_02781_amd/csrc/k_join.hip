@@ -567,8 +567,9 @@ void bt_join(hipStream_t st, const ftp_join_args& a, const DropMask& m) {
   const bool once = past_the_caches(bytes);
   if (a.width <= kJoinHeld) {
     const int t = join_threads(a.width);
-    // forward there are no blocks' sums: twice the card's wavefronts (16384 x 1024 36 us, half of them 39)
-    const int64_t want = std::min<int64_t>(a.rows, 256 * 4096 / t), per = (a.rows + want - 1) / want;
+    // forward there are no blocks' sums: four rounds of the wavefronts that the card holds (16384 x 1024 34 us, one round 37), sixteen where a wavefront has several rows (400000 x 128
+    // 72 us, four 85, one 99)
+    const int64_t want = std::min<int64_t>(a.rows, (t < 64 ? 1024 : 256) * 4096 / t), per = (a.rows + want - 1) / want;
     const int64_t walkers = (a.rows + per - 1) / per;
     const dim3 g((unsigned)((walkers + join_walkers(t) - 1) / join_walkers(t))), b(64 * join_waves(t));
     join_by_threads(t, [&](auto tc) {
