@@ -221,6 +221,15 @@ def test_join_ranges_that_share_a_wavefront(env, width, gate, gate_rows):
     join_case(env, "f32", 18005, width, width == 20, True, gate, gate_rows, p=0.1)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("tail", range(1, 8))
+@pytest.mark.parametrize("front", [8, 248, 1016])
+def test_join_last_columns(env, dtype, tail, front):
+    """a row's last columns, fewer than eight, with rows one behind another and with space between them"""
+    join_case(env, dtype, 9, front + tail, tail % 2 == 0, True, "row", p=0.1)
+    join_case(env, dtype, 5, front + tail, False, False, "group", 2, slack=tail, skip=tail % 3, gate_f32=True)
+
+
 def test_join_in_place_and_twice(env):
     torch, P, _ = env
     for width in (200, 40000):
