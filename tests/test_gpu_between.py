@@ -398,6 +398,15 @@ def test_scan_few_rows(env, dtype, rows):
     scan_case(env, dtype, [rows], 33, "add", "", uniform=True)
 
 
+@pytest.mark.parametrize("width", [1, 2, 3, 5, 63, 65, 127, 129, 131, 255, 257, 385])
+def test_scan_odd_widths(env, width):
+    """a last column without a second one: beside others in its wavefront, alone in it, alone altogether; states in their operands' buffers"""
+    scan_case(env, "bf16", [40, 0, 3, 90], width, slack=1, in_place=True)
+    scan_case(env, "bf16", [1] * 20, width, "unit", "gelu", in_place=True, uniform=True)
+    scan_case(env, "bf16", [300, 17], width, "add", "", front=2, behind=1)
+    scan_case(env, "bf16", [50, 0, 60], width, "mix", "relu", slack=2, skip=1, in_place=True)
+
+
 @pytest.mark.parametrize("empty", [0, 61, 62, 63, 64, 65, 130])
 @pytest.mark.parametrize("tail", [1, 300])
 def test_scan_many_empty_sequences_together(env, empty, tail):
