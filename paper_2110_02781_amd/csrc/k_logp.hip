@@ -243,10 +243,11 @@ __global__ __launch_bounds__(T, 1) void logp_k(ftp_logp_args a, LogpPlan p) {
     m = most[0];
 #pragma unroll
     for (int i = 1; i < T / 64; ++i) m = fmaxf(m, most[i]);
-    // e^t = 2^d, d = k z - k m with one rounding, which leaves the rounding of k m in all of them: taken off the sum below.  Where k m is not a number that can be taken off
-    // (infinite, or nothing but -inf) d = k (z - m)
+    // e^t = 2^d, d = k z - k m with one rounding, which leaves the rounding of k m, `off`, in all of them: taken off the sums below to first order.  |off| is at most half a step of k m, below
+    // 4096 at most 2^-13, and what is left out, (off ln 2)^2 / 2, 2^-28 of a sum.  From there on (at 1e9 off is 18), or where k m is no number, d = k (z - m): an operation a value
+    // more, and no error that grows with m
     const float k = a.scale * FTP_LOG2E, km = m * k;
-    const bool plain = fabsf(km) < 1e30f;
+    const bool plain = fabsf(km) < 4096.f;
     float s1 = 0.f, s2 = 0.f;
     const auto add = [&](auto fused) __attribute__((always_inline)) {
 #pragma unroll

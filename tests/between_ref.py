@@ -3,12 +3,15 @@
 A number of type V is a value and its bound; every operation on two of them rounds once to 32 bits (u = 2^-24 of the result) and passes its operands' bounds on.
 Sums over n values of a row are made by 64 lanes at least, n / 64 additions one behind the other and some thirty between lanes, chains and blocks: (n / 64 + 32) u of the sum
 of magnitudes, whatever their order.  Square roots, divisions and reciprocals are off by 2 u at most, exponentials by 2 u and by the rounding of their
-argument, twice: 2 u of it.  A value stored in type t is off by half a step more (token_ref.HALF)."""
+argument, twice: 2 u of it.  A value stored in type t is off by half a step more (token_ref.HALF).  Below 2^-126 steps are no smaller than there, 2^-149 in fp32 and 2^-133 in
+bfloat16: half of one of the latter where it is stored, and of the former there and at the multiplication in front (SMALLEST)."""
 import math
 
 import torch
 
 from token_ref import HALF, U, close, f64  # noqa: F401
+
+SMALLEST = {torch.float32: 2.0 ** -149, torch.bfloat16: 2.0 ** -134 + 2.0 ** -149}
 
 
 class V:
@@ -46,7 +49,7 @@ class V:
         return V(torch.where(cond, self.v, z), torch.where(cond, self.e, z))
 
     def stored(self, dtype):
-        return self.v, self.e + HALF[dtype] * (self.v.abs() + self.e)
+        return self.v, self.e + HALF[dtype] * (self.v.abs() + self.e) + SMALLEST[dtype]
 
 
 def check(got, want, what):
