@@ -510,7 +510,8 @@ int ftp_join_backward(const ftp_join_args*, void* stream);
  * with c = 1 (FTP_SCAN_ADD), 1 - a (FTP_SCAN_MIX) or sqrt(1 - a^2) (FTP_SCAN_UNIT).  Sequence s has the rows starts[s] ..
  * starts[s+1] - 1 (int32 [seqs + 1] in device memory, not falling, within 0 .. rows; where they are neither, results are undefined but
  * nothing outside the buffers is touched), or with starts NULL the rows s * length .. of rows = seqs * length.  A sequence may
- * be empty; rows of no sequence stay as they were in every result.
+ * be empty; rows of no sequence stay as they were in every result.  An infinity or NaN stays in its sequence: results of the others are what they
+ * are without it.
  * h0: states in front of the sequences, fp32 [seqs], NULL: 0; h_end: those behind them, where wanted, may be h0's buffer (a step of one
  * token for each of seqs requests is length = 1).  States inside a call are fp32.
  * Backward, from f, x, g, h0 (states are computed again): of dy (and dh_end, fp32, NULL: 0) df, dx, dg (with g) and dh0, each where

@@ -210,13 +210,27 @@ __device__ __forceinline__ void scan_state(const float* m, int ld, int seq, cons
   else sc_zero<V>(h);
 }
 
+// Past a chunk: what comes out of it for h that goes in; and two factors as one.  Of a chunk where a sequence begins or ends A is kScanCut, and what goes in does not count, whatever it
+// is: a factor 0 would make NaN of an infinity or NaN, and one spoiled sequence spoil all others of its batch.  Other factors are products of sigmoids, 0 .. 1; where one is NaN, so are B and C.
+#define kScanCut -1.f
+__device__ __forceinline__ float scan_past(float A, float h, float B) { return A < 0.f ? B : fmaf(A, h, B); }
+__device__ __forceinline__ float scan_both(float a, float b) { return a < 0.f || b < 0.f ? kScanCut : a * b; }
+
 // A and B of a chunk; backward: C too.  `seed` (true is returned where there is one): the state in front of the last sequence that begins here, or what arrives at the end of one from a
 // chunk in front, read before another chunk writes its result into the same memory.
 template <typename E, int V, bool WHOLE, int FORM, bool BWD, int R>
 __device__ __forceinline__ bool scan_sums(const ScanArgs& k, const ScanAt& p, ScanRows& rows, float A[V], float B[V], float C[V], float seed[V]) {
-  bool seeded = false;
+  bool seeded = false, open = true;      // open: no sequence has begun or ended yet
+  float own[V];                          // C up to there
 #pragma unroll
-  for (int e = 0; e < V; ++e) { A[e] = 1.f; B[e] = C[e] = 0.f; }
+  for (int e = 0; e < V; ++e) { A[e] = 1.f; B[e] = C[e] = own[e] = 0.f; }
+  const auto close = [&]() __attribute__((always_inline)) {
+    if (BWD && open) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) own[e] = C[e];
+    }
+    open = false;
+  };
   ScanRaw<E, V> f[R], x[R], g[R], dy[R];
   const char *const qf = k.f + p.r0 * k.ldf, *const qx = k.x + p.r0 * k.ldx, *const qg = k.g + p.r0 * k.ldg, *const qdy = k.dy + p.r0 * k.lddy;
   int flags = k.flags;
@@ -259,12 +273,12 @@ __device__ __forceinline__ bool scan_sums(const ScanArgs& k, const ScanAt& p, Sc
       bool last = false;
       if (event) {
         if (!(rows.in >> t & 1)) {     // of no sequence, or behind the chunk: nothing goes through
-          if (t < p.n) sc_zero<V>(A);
+          if (t < p.n) close();
           continue;
         }
         if (rows.first >> t & 1) {
           scan_state<V, WHOLE>(k.h0, k.ldh0, rows.of(t), p, B);
-          sc_zero<V>(A);
+          close();
           if (!BWD) {
             seeded = true;
 #pragma unroll
@@ -291,7 +305,14 @@ __device__ __forceinline__ bool scan_sums(const ScanArgs& k, const ScanAt& p, Sc
         A[e] *= s.a;
         if (BWD) C[e] = fmaf(A[e], into[i][e], C[e]);
       }
-      if (BWD && last) sc_zero<V>(A);
+      if (BWD && last) close();
+    }
+  }
+  if (!open) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      A[e] = kScanCut;
+      if (BWD) C[e] = own[e];
     }
   }
   return seeded;
@@ -335,15 +356,15 @@ __global__ __launch_bounds__(1024) void scan_follow_k(ScanArgs k) {
       }
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
-        b = fmaf(u[q], b, v[q]);
-        a *= u[q];
+        b = scan_past(u[q], b, v[q]);
+        a = scan_both(a, u[q]);
       }
     } else {
 #pragma unroll 8
       for (int i = i0; i < i1; ++i) {
         const float p = A[at(i)], q = B[at(i)];
-        b = fmaf(p, b, q);
-        a *= p;
+        b = scan_past(p, b, q);
+        a = scan_both(a, p);
       }
     }
   }
@@ -354,8 +375,8 @@ __global__ __launch_bounds__(1024) void scan_follow_k(ScanArgs k) {
     sb[ty][lane] = b;
     __syncthreads();
     if (ty >= d) {
-      b = fmaf(a, sb[ty - d][lane], b);
-      a *= sa[ty - d][lane];
+      b = scan_past(a, sb[ty - d][lane], b);
+      a = scan_both(a, sa[ty - d][lane]);
     }
     __syncthreads();
   }
@@ -368,14 +389,14 @@ __global__ __launch_bounds__(1024) void scan_follow_k(ScanArgs k) {
     for (int q = 0; q < 8; ++q) {
       if (i0 + q >= i1) break;
       out[at(i0 + q)] = h;
-      h = fmaf(u[q], h, v[q]);
+      h = scan_past(u[q], h, v[q]);
     }
   } else {
 #pragma unroll 8
     for (int i = i0; i < i1; ++i) {
       const float p = A[at(i)], q = B[at(i)];
       out[at(i)] = h;
-      h = fmaf(p, h, q);
+      h = scan_past(p, h, q);
     }
   }
 }
@@ -429,11 +450,11 @@ __device__ __forceinline__ bool scan_pass(const ScanArgs& k, const ScanAt& p, Sc
   if (wave < 0) return false;
   for (int j = 0; j < me; ++j)
 #pragma unroll
-    for (int e = 0; e < V; ++e) h[e] = fmaf(sA[j][at + e], h[e], sB[j][at + e]);
+    for (int e = 0; e < V; ++e) h[e] = scan_past(sA[j][at + e], h[e], sB[j][at + e]);
   if (BWD)
     for (int j = k.chunks - 1; j > me; --j)
 #pragma unroll
-      for (int e = 0; e < V; ++e) mu[e] = fmaf(sA[j][at + e], mu[e], sC[j][at + e]);
+      for (int e = 0; e < V; ++e) mu[e] = scan_past(sA[j][at + e], mu[e], sC[j][at + e]);
   return true;
 }
 

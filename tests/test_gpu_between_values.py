@@ -4,7 +4,8 @@ import math
 
 import pytest
 
-from test_gpu_between import DTYPES, env, gen_of, logp_case  # noqa: F401
+from test_gpu_between import ACT_CODE, DTYPES, env, gen_of, logp_case, put, stream  # noqa: F401
+from test_gpu_token import given, matrix, types
 
 pytestmark = pytest.mark.gpu
 ROWS = [(4, 1000, 0), (3, 5000, 20), (300, 700, 5), (2, 40000, 0), (5, 33001, 3)]              # rows by one block and by several, with and without alternatives
@@ -39,3 +40,69 @@ def test_logp_of_ordinary_logits_with_a_large_scale(env, dtype, scale, rows, voc
     g = gen_of(env[0], rows, vocab, scale)
     z = 4 + env[0].randint(0, 40, (rows, vocab), generator=g, device="cuda").double() * step(dtype, 4.0)           # neighbours, so that more than one counts
     logp_case(env, dtype, rows, vocab, k, scale=scale, logits=z)
+
+
+# ---- the recurrence ------------------------------------------------------------------------------------------------------
+def scan_both(env, a, names, rows, seqs, width, dt):
+    """results of the forward and the backward, each in a buffer of its own"""
+    torch, P, _ = env
+    res = {}
+    for name, ld in names:
+        res[name] = torch.full((seqs, width), 777.0, device="cuda") if name in ("h_end", "dh0") else torch.full((rows, width), 777.0, dtype=dt, device="cuda")
+        put(a, **{name: res[name], ld: width})
+    for back, call in ((False, P.scan_forward), (True, P.scan_backward)):
+        ws, ok = given(a, torch, P.scan_workspace(a, back))
+        call(a, stream(torch))
+        torch.cuda.synchronize()
+        ok()
+    return res
+
+
+# sequences in one chunk, in several, in one launch, in three, in more chunks than a column's threads keep; long ones in front, in the middle and behind
+PACKED = [([5, 10, 6], 20), ([1] * 40, 9), ([30, 0, 33, 20], 66), ([100, 28], 131), ([200, 150, 300], 70), ([3, 700, 2, 60], 20), ([600, 1, 600], 130), ([0, 90, 0, 0, 400, 31, 0], 33), ([64, 64, 64], 40),
+          ([5000, 70, 4000], 4), ([9000, 9000], 3)]
+EVEN = [([1] * 40, 9), ([10] * 3, 20), ([64] * 2, 131), ([64] * 3, 40), ([600] * 3, 130), ([9000] * 2, 3)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("form", ["add", "mix", "unit"])
+@pytest.mark.parametrize("lens,width,uniform", [(*c, False) for c in PACKED] + [(*c, True) for c in EVEN], ids=lambda v: str(v).replace(" ", "")[:40])
+def test_scan_keeps_what_is_not_finite_in_its_sequence(env, dtype, form, lens, width, uniform):
+    """an infinity or NaN in any operand of one sequence: all others have the bits that they have without it"""
+    torch, P, _ = env
+    tdt, code = types(P, torch, dtype)
+    starts = [0 if uniform else 2]
+    for n in lens:
+        starts.append(starts[-1] + n)
+    rows, seqs, act = starts[-1] + (0 if uniform else 3), len(lens), "" if form == "mix" else "silu"
+    g = gen_of(torch, lens, width, form)
+    m = {k: matrix(torch, g, rows, width, tdt, 2.0 if k == "f" else 1.0) for k in ("f", "x", "g", "dy")}
+    m.update({k: matrix(torch, g, seqs, width, torch.float32) for k in ("h0", "dh_end")})
+    dev = torch.tensor(starts, dtype=torch.int32, device="cuda")
+    a = P.scan_args(rows=rows, width=width, seqs=seqs, dtype=code, form={"add": P.SCAN_ADD, "mix": P.SCAN_MIX, "unit": P.SCAN_UNIT}[form], act=ACT_CODE[act or "none"])
+    put(a, **({"length": lens[0]} if uniform else {"starts": dev}))
+    if not act:
+        del m["g"]
+    for k, ld in (("f", "ldf"), ("x", "ldx"), ("g", "ldg"), ("dy", "lddy"), ("h0", "ldh0"), ("dh_end", "lddhe")):
+        if k in m:
+            put(a, **{k: m[k], ld: width})
+    names = [("y", "ldy"), ("h_end", "ldhe"), ("df", "lddf"), ("dx", "lddx"), ("dh0", "lddh0")] + [("dg", "lddg")] * bool(act)
+    want = scan_both(env, a, names, rows, seqs, width, tdt)
+    assert all(bool(v.isfinite().all()) for v in want.values())
+    for s in sorted({0, seqs // 2, seqs - 1}):
+        if not lens[s]:
+            continue
+        b, e = starts[s], starts[s + 1]
+        others = torch.ones(rows, dtype=torch.bool, device="cuda")
+        others[b:e] = False
+        for k in m:
+            for bad in (math.nan, math.inf, -math.inf):
+                states = k in ("h0", "dh_end")
+                at = (s if states else b if bad != bad else (b + e) // 2 if bad > 0 else e - 1)
+                old = m[k][at].clone()
+                m[k][at] = bad
+                got = scan_both(env, a, names, rows, seqs, width, tdt)
+                m[k][at] = old
+                for name, r in got.items():
+                    same = [q for q in range(seqs) if q != s] if name in ("h_end", "dh0") else others
+                    assert torch.equal(r[same], want[name][same]), (name, k, bad, s)
