@@ -26,7 +26,7 @@ int check_same(const char* who, const char* out, const void* o, int64_t ldo, con
 }
 template <typename A>
 int check_mask(const char* who, const A* a) {
-  NEED(std::isfinite(a->p) && a->p >= 0.f && drop_least(a->p) < 65536, FTP_ERR_VALUE, "%s: p must be in [0, 1), with some of 2^-16 left", who);
+  NEED(a->p >= 0.f && a->p < 1.f && drop_least(a->p) < 65536, FTP_ERR_VALUE, "%s: p must be in [0, 1), with some of 2^-16 left", who);
   NEED(a->row0 >= 0 && a->row0 <= INT64_MAX - a->rows, FTP_ERR_ARG, "%s: row0 must not be negative or too large", who);
   NEED((uintptr_t)a->seed_dev % 8 == 0, FTP_ERR_ARG, "%s: seed_dev is not aligned to its element", who);
   return FTP_OK;

@@ -14,6 +14,7 @@ struct DropMask {
   const uint64_t* seed_dev;
   int64_t row0;
 };
+// of p in [0, 1): a larger one may be past what 32 bits hold
 static inline uint32_t drop_least(float p) { return (uint32_t)((double)p * 65536.0 + 0.5); }
 
 void bt_dropout(hipStream_t st, int dt, int64_t rows, int cols, const DropMask& m, const void* x, int64_t ldx, const void* r, int64_t ldr, void* y, int64_t ldy);

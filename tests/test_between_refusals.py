@@ -210,3 +210,11 @@ def test_results_in_an_operands_buffer_have_its_rows(P):
     refused(P, P.join_backward, join(P, dx=B, dy=B, lddy=17))
     refused(P, P.scan_backward, scan(P, dh0=B, dh_end=B, lddhe=17))
     refused(P, P.logp_backward, logp(P, dlogits=B, logits=B, lddl=11))
+
+
+@pytest.mark.parametrize("p", [1.5, 2.0, 65535.99, 65536.0, 65536.5, 131072.0, 1e10, 1e20, 1e30, 3e38, INF, -INF])
+def test_probabilities_past_one(P, p):
+    """also those that no whole number of 32 bits holds; without rows, so that a call that is let through launches nothing"""
+    for call, a in ((P.dropout_forward, dropout(P, rows=0, p=p)), (P.dropout_backward, dropout(P, rows=0, p=p)), (P.join_forward, join(P, rows=0, p=p)), (P.join_backward, join(P, rows=0, p=p, dpost_w=0, dpre_w=0)),
+                    (lambda r, _: P.join_workspace(r), join(P, rows=0, p=p))):
+        refused(P, call, a, -5)
