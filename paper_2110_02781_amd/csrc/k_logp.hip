@@ -244,8 +244,8 @@ __global__ __launch_bounds__(T, 1) void logp_k(ftp_logp_args a, LogpPlan p) {
 #pragma unroll
     for (int i = 1; i < T / 64; ++i) m = fmaxf(m, most[i]);
     // e^t = 2^d, d = k z - k m with one rounding, which leaves the rounding of k m, `off`, in all of them: taken off the sums below to first order.  |off| is at most half a step of k m, below
-    // 4096 at most 2^-13, and what is left out, (off ln 2)^2 / 2, 2^-28 of a sum.  From there on (at 1e9 off is 18), or where k m is no number, d = k (z - m): an operation a value
-    // more, and no error that grows with m
+    // 4096 at most 2^-13, and what is left out, (off ln 2)^2 / 2, 2^-28 of a sum.  From there on (at 1e9 off is 18), or where k m is no number, d = log2 e (scale (z - m)): two
+    // operations a value more, no error that grows with m, and no k, which is infinite for a scale of 2.4e38
     const float k = a.scale * FTP_LOG2E, km = m * k;
     const bool plain = fabsf(km) < 4096.f;
     float s1 = 0.f, s2 = 0.f;
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(T, 1) void logp_k(ftp_logp_args a, LogpPlan p) {
         logp_anew<E>(r[v]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float z = logp_at<E>(r[v], e), d = fused.value ? fmaf(z, k, -km) : (z - m) * k, x = __builtin_amdgcn_exp2f(d);
+          const float z = logp_at<E>(r[v], e), d = fused.value ? fmaf(z, k, -km) : (z - m) * a.scale * FTP_LOG2E, x = __builtin_amdgcn_exp2f(d);
           s1 += x;
           s2 = fmaf(x, fmaxf(d, -300.f), s2);
         }

@@ -42,6 +42,17 @@ def test_logp_of_ordinary_logits_with_a_large_scale(env, dtype, scale, rows, voc
     logp_case(env, dtype, rows, vocab, k, scale=scale, logits=z)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,vocab,k", ROWS)
+def test_logp_of_a_scale_next_to_the_types_largest(env, dtype, rows, vocab, k):
+    """log2 e times it is no number of 32 bits any more; logits so small that they are a few units apart all the same"""
+    torch = env[0]
+    g = gen_of(torch, rows, vocab)
+    z = 2.0 ** -126 * torch.randint(0, 12, (rows, vocab), generator=g, device="cuda").double()
+    z[-1] = 0
+    logp_case(env, dtype, rows, vocab, k, scale=1.5 * 2.0 ** 127, logits=z, dlogp_there=False, dent_there=False)
+
+
 # ---- the recurrence ------------------------------------------------------------------------------------------------------
 def scan_both(env, a, names, rows, seqs, width, dt):
     """results of the forward and the backward, each in a buffer of its own"""
