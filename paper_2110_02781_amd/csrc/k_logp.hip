@@ -67,6 +67,11 @@ __device__ __forceinline__ LogpGiven logp_given(const ftp_logp_args& a, int64_t 
   if (id >= 0 && id < a.vocab) g.z = to_f32(((const E*)a.logits)[row * a.ldl + id]);
   return g;
 }
+// scale (z - m) by halves: the difference itself may be past the type's range where the scale brings it back
+__device__ __forceinline__ float logp_t(float z, float m, float scale) {
+  const float h = fmaf(z, 0.5f, -0.5f * m) * scale;
+  return h + h;
+}
 // a row's results but the likeliest; one thread
 __device__ __forceinline__ void logp_finish(const ftp_logp_args& a, int64_t row, LogpSum s, LogpGiven g) {
   const float l = __builtin_amdgcn_logf(s.s1) * FTP_LN2;         // nothing but -inf: -inf
@@ -74,13 +79,13 @@ __device__ __forceinline__ void logp_finish(const ftp_logp_args& a, int64_t row,
   if (a.lse) a.lse[row] = none ? l : fmaf(s.m, a.scale, l);
   if (a.stats) { a.stats[2 * row] = s.m; a.stats[2 * row + 1] = l; }
   if (a.entropy) a.entropy[row] = none ? 0.f : l - s.s2 / s.s1;
-  if (a.logp) a.logp[row] = g.pad ? 0.f : g.z != g.z ? g.z : none ? l : (g.z - s.m) * a.scale - l;
+  if (a.logp) a.logp[row] = g.pad ? 0.f : g.z != g.z ? g.z : none ? l : logp_t(g.z, s.m, a.scale) - l;
 }
 // place t of the likeliest
 __device__ __forceinline__ void logp_place(const ftp_logp_args& a, int64_t row, int t, unsigned long long key, LogpSum s) {
   const bool nan = s.s1 != s.s1;
   a.top_ids[row * a.top + t] = key ? logp_col(key) : -1;
-  a.top_logp[row * a.top + t] = nan ? s.s1 : key ? (logp_value(key) - s.m) * a.scale - __builtin_amdgcn_logf(s.s1) * FTP_LN2 : -__builtin_inff();
+  a.top_logp[row * a.top + t] = nan ? s.s1 : key ? logp_t(logp_value(key), s.m, a.scale) - __builtin_amdgcn_logf(s.s1) * FTP_LN2 : -__builtin_inff();
 }
 
 __device__ __forceinline__ float wave_max_last(float x) {        // in the last lane

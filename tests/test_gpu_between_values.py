@@ -53,6 +53,21 @@ def test_logp_of_a_scale_next_to_the_types_largest(env, dtype, rows, vocab, k):
     logp_case(env, dtype, rows, vocab, k, scale=1.5 * 2.0 ** 127, logits=z, dlogp_there=False, dent_there=False)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,vocab", [(4, 30), (300, 60), (2, 5000)])
+def test_logp_of_logits_farther_apart_than_the_type_reaches(env, dtype, rows, vocab):
+    """3e38 and -3e38: the log probability, a quarter of their difference, is a number all the same"""
+    torch = env[0]
+    z = torch.zeros(rows, vocab, device="cuda")
+    z[:, 1], z[:, 2::2], z[:, -1] = 3e38, -3e38, -math.inf
+    z[0, 1] = -3e38
+    ids = torch.arange(rows, device="cuda") % 4
+    ids[1] = vocab - 1
+    for k in (0, min(vocab, 64)):
+        logp_case(env, dtype, rows, vocab, k, scale=0.25, logits=z, ids=ids)
+    logp_case(env, dtype, rows, vocab, 3, scale=1e-37, logits=z, ids=ids)
+
+
 # ---- the recurrence ------------------------------------------------------------------------------------------------------
 def scan_both(env, a, names, rows, seqs, width, dt):
     """results of the forward and the backward, each in a buffer of its own"""
