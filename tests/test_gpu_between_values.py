@@ -132,3 +132,27 @@ def test_scan_keeps_what_is_not_finite_in_its_sequence(env, dtype, form, lens, w
                 for name, r in got.items():
                     same = [q for q in range(seqs) if q != s] if name in ("h_end", "dh0") else others
                     assert torch.equal(r[same], want[name][same]), (name, k, bad, s)
+
+
+@pytest.mark.parametrize("form", ["add", "mix", "unit"])
+def test_scan_gates_keep_their_places(env, form):
+    """a, 1 - a and c(a) of gates from one end to the other in single precision, and their derivatives, from single steps.  e^-|f| is off by 2 u of the exponential, one rounding and 0.05 |f| u
+    (4 u at 80), its quotient by 1 + e by 4 u more, c by no more than that and a root's 2 u; two products and the store round: 16 u of a result that is one product, and of the sum of the
+    magnitudes of two.  Below 2^-100 a product's operands may have lost places."""
+    torch, P, B = env
+    f = torch.cat([torch.linspace(-80, 80, 4001, device="cuda"), torch.randn(4095, device="cuda") * 8])[None].contiguous()
+    n = f.shape[1]
+    g = gen_of(torch, form)
+    x, h0, dy = (torch.randn(1, n, generator=g, device="cuda") for _ in range(3))
+    y, end, df, dx, dh0 = (torch.empty(1, n, device="cuda") for _ in range(5))
+    a = P.scan_args(rows=1, length=1, seqs=1, width=n, dtype=P.F32, form={"add": P.SCAN_ADD, "mix": P.SCAN_MIX, "unit": P.SCAN_UNIT}[form], f=f, ldf=n, x=x, ldx=n, h0=h0, ldh0=n, y=y, ldy=n,
+                    h_end=end, ldhe=n, dy=dy, lddy=n, df=df, lddf=n, dx=dx, lddx=n, dh0=dh0, lddh0=n)
+    P.scan_forward(a, stream(torch))
+    P.scan_backward(a, stream(torch))
+    torch.cuda.synchronize()
+    z, x, h0, dy = (t.double() for t in (f, x, h0, dy))
+    s, r = torch.sigmoid(z), torch.sigmoid(-z)
+    c = {"add": torch.ones_like(s), "mix": r, "unit": (r * (1 + s)).sqrt()}[form]
+    dc = {"add": torch.zeros_like(s), "mix": -s * r, "unit": -s * s * (r / (1 + s)).sqrt()}[form]
+    for name, got, terms in (("y", y, (s * h0, c * x)), ("h_end", end, (s * h0, c * x)), ("dx", dx, (dy * c,)), ("dh0", dh0, (dy * s,)), ("df", df, (dy * s * r * h0, dy * dc * x))):
+        B.close(got, sum(terms), 16 * B.U * sum(t.abs() for t in terms) + 2.0 ** -124, name)
