@@ -463,6 +463,7 @@ int ftp_dropout_backward(const ftp_dropout_args*, void* stream);
 /* Between two blocks of a model: with the stream x, the block's output b and norm(v) = (v - mean) / sqrt(var + eps) of a row
  * (FTP_NORM_LAYER) or v / sqrt(mean of squares + eps) (FTP_NORM_RMS),
  *   c = norm(b) * post_w + post_bias (with `post`; otherwise b),   y = x + scale * gate * dropped c,   n = norm(y) * pre_w + pre_bias.
+ * Means and means of squares are fp32: a row whose squares add up to more than its range has the norm 0.
  * x NULL: 0; b NULL: y = x (and n is x normed: the call in front of the first block).  Weights fp32 [width], NULL: 1; biases NULL: 0.
  * gate [ceil(rows / gate_rows)][width] of gate_dtype (fp32 or dtype): row t takes row t / gate_rows; NULL: 1.
  * y and n each where wanted; n is of y before it is rounded.  y may be the buffer of x or of b.
@@ -501,8 +502,10 @@ typedef struct {
   int32_t accumulate;
   void* ws; size_t ws_bytes;
 } ftp_join_args;
-int ftp_join_forward(const ftp_join_args*, void* stream);              /* without a workspace */
-int ftp_join_workspace(const ftp_join_args*, size_t* bytes);           /* the backward's      */
+int ftp_join_forward(const ftp_join_args*, void* stream);
+/* The backward's: for each column sum that is asked for a row of fp32 from each block, 8 MiB in all or less up to 8192 columns, and 1 KiB a column past them (1 GiB at 2^20); up to
+ * twice that where a gate's groups do not divide the rows evenly.  The forward has none. */
+int ftp_join_workspace(const ftp_join_args*, size_t* bytes);
 int ftp_join_backward(const ftp_join_args*, void* stream);
 
 /* Gated linear recurrence, column by column along each sequence:

@@ -369,8 +369,8 @@ __global__ __launch_bounds__(256) void logp_join_k(ftp_logp_args a, LogpPlan p) 
   }
 }
 
-// Segments and blocks: a row by one block where there are rows for all CUs, otherwise as many segments as make 256 blocks, of 2048 columns at least.  Blocks of 256 threads, of which
-// several share a CU and wait at different times, until their registers are full.
+// Segments and blocks: a row by one block where there are rows for all CUs, otherwise as many segments as make 256 blocks, but no more than leave them
+// over 1024 columns (2049 of one row: two segments, of 1032 and 1017).  Blocks of 256 threads, of which several share a CU and wait at different times, until their registers are full.
 static LogpPlan logp_plan(const ftp_logp_args& a) {
   LogpPlan p{};
   // with the likeliest, half as many columns a thread: twice would leave two wavefronts to a SIMD (2048 x 32000 bfloat16 with 5 alternatives 50 us, so 44)

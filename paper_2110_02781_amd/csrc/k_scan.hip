@@ -11,7 +11,7 @@
 
 namespace ftp {
 
-enum { kScanT = 32, kScanR = 4 };     // rows of a chunk; rows that are asked for together (eight: 96 us instead of 92 for a forward of 16384 x 2048)
+enum { kScanT = 32, kScanR = 4 };     // rows of a chunk; rows that are asked for together (eight: 89 us instead of 83 for a forward of 16384 x 2048)
 // What the kernels need of a call's record, in few scalar registers: row distances of the matrices in bytes, questions as bits that are tested where they are asked (SK_...)
 struct ScanArgs {
   const char *f, *x, *g, *dy;
