@@ -94,7 +94,7 @@ EVEN = [([1] * 40, 9), ([10] * 3, 20), ([64] * 2, 131), ([64] * 3, 40), ([600] *
 @pytest.mark.parametrize("form", ["add", "mix", "unit"])
 @pytest.mark.parametrize("lens,width,uniform", [(*c, False) for c in PACKED] + [(*c, True) for c in EVEN], ids=lambda v: str(v).replace(" ", "")[:40])
 def test_scan_keeps_what_is_not_finite_in_its_sequence(env, dtype, form, lens, width, uniform):
-    """an infinity or NaN in any operand of one sequence: all others have the bits that they have without it"""
+    """an infinity or NaN in any operand of one sequence: all others have the bits that they have without it; rows of no sequence hold NaN"""
     torch, P, _ = env
     tdt, code = types(P, torch, dtype)
     starts = [0 if uniform else 2]
@@ -104,6 +104,8 @@ def test_scan_keeps_what_is_not_finite_in_its_sequence(env, dtype, form, lens, w
     g = gen_of(torch, lens, width, form)
     m = {k: matrix(torch, g, rows, width, tdt, 2.0 if k == "f" else 1.0) for k in ("f", "x", "g", "dy")}
     m.update({k: matrix(torch, g, seqs, width, torch.float32) for k in ("h0", "dh_end")})
+    for k in ("f", "x", "g", "dy"):                                 # rows of no sequence
+        m[k][:starts[0]], m[k][starts[-1]:] = math.nan, math.nan
     dev = torch.tensor(starts, dtype=torch.int32, device="cuda")
     a = P.scan_args(rows=rows, width=width, seqs=seqs, dtype=code, form={"add": P.SCAN_ADD, "mix": P.SCAN_MIX, "unit": P.SCAN_UNIT}[form], act=ACT_CODE[act or "none"])
     put(a, **({"length": lens[0]} if uniform else {"starts": dev}))
